@@ -4,9 +4,11 @@
  * SDGP (Structured Data Gradient Pruning, arXiv 2202.00774) keeps n of every m
  * consecutive channels of the output data gradient dL/dO and zeroes the rest
  * (Alg. 1, Sec. III-A), then computes the input data gradient dL/dD from the
- * pruned tensor (Fig. 1, Fig. 2, Sec. II-A).  This library is that path and
- * nothing else: the prune primitive, and the backward-data product for linear
- * and convolution layers with the prune fused in.
+ * pruned tensor (Fig. 1, Fig. 2, Sec. II-A).  This library is that path: the
+ * prune primitive, and the backward-data product for linear and convolution
+ * layers with the prune fused in; and what a training step of a language model
+ * with such layers needs around it: the loss that dL/dO starts from, the norms
+ * between blocks and the optimizer step.
  *
  * Conventions that hold for every entry point
  *   - Every tensor pointer is a DEVICE pointer owned by the caller.  The library
@@ -44,7 +46,8 @@ typedef enum {
     SDGP_ERR_DTYPE = -4,     /* dtype is not an sdgp_dtype                                   */
     SDGP_ERR_RANKER = -5,    /* ranker is not an sdgp_ranker                                 */
     SDGP_ERR_WORKSPACE = -6, /* workspace is NULL or smaller than the size query returns     */
-    SDGP_ERR_HIP = -7        /* the HIP runtime refused a launch (the HIP error is consumed) */
+    SDGP_ERR_HIP = -7,       /* the HIP runtime refused a launch (the HIP error is consumed) */
+    SDGP_ERR_VALUE = -8      /* a scalar (scale, eps, rate, step) outside its range          */
 } sdgp_status;
 
 typedef enum {
@@ -327,6 +330,98 @@ size_t sdgp_conv_bwd_weight_workspace(int64_t B, int64_t H, int64_t Wd, int64_t 
 int sdgp_conv_bwd_weight(const void* D, const void* dO, float* dW, int64_t B, int64_t H, int64_t Wd,
                          int64_t C_in, int64_t C_out, int R, int S, int stride, int pad, int dt,
                          void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * sdgp_token_logprobs -- log probabilities of given tokens, entropy and best alternatives of every row of logits.
+ *
+ *   logits    [rows, V] of `dt`, row stride ld >= V elements (a vocabulary cut out of padded logits), last stride 1
+ *   tokens    [rows] int32 or int64 (token_bits), NULL with logp NULL.  A token < 0 is none: its log probability is 0
+ *             and no gradient comes from it.  A token >= V gives NaN (and a row of NaN as gradient).
+ *   scale     > 0, what the logits are multiplied with first (one over the temperature)
+ *   logp      [rows] fp32 or NULL: ln p(token), p = softmax(scale * logits)
+ *   entropy   [rows] fp32: -sum p ln p, in nats; 0 ln 0 = 0
+ *   top_ids, top_logp  [rows, top] int64 and fp32, 0 <= top <= min(64, V): the most probable tokens, best first, equal
+ *             logits in the order of their index, and their ln p.  Logits of -inf are no alternatives: places left over
+ *             hold the index -1 and -inf.
+ *   stats     [rows, 2] fp32: the largest logit and ln of the sum of exp(scale * (logit - largest)), for the gradient
+ *
+ * Sums are fp32.  -inf (a token that is not allowed) and the type's lowest value are fine anywhere.  A row that leaves
+ * nothing (-inf throughout) has ln p = -inf, entropy 0 and no alternatives; its gradient is 0.  A row with a NaN or +inf
+ * has NaN in every number and -1 in every index.
+ *
+ * sdgp_token_logprobs_bwd -- dL/dlogits from dL/dlogp and dL/dentropy (either may be NULL; the alternatives have none):
+ *   dlogits[j] = scale * (g (j == token) - g p_j - h p_j (ln p_j + entropy)), row stride ld_out; dlogits may be logits.
+ *   stats, entropy: what the forward call left.  This is the dL/dO that the last linear layer's
+ *   sdgp_linear_bwd_data takes.
+ *
+ * workspace: sdgp_token_logprobs_workspace(...) bytes, 16-byte aligned, contents undefined afterwards ((size_t)-1 for
+ * invalid arguments; 0 where the call needs none).
+ */
+size_t sdgp_token_logprobs_workspace(int64_t rows, int64_t V, int dt, int top);
+int sdgp_token_logprobs(const void* logits, int64_t ld, const void* tokens, int token_bits, float* logp, float* entropy,
+                        float* top_logp, int64_t* top_ids, float* stats, int64_t rows, int64_t V, int dt, int top,
+                        float scale, void* workspace, size_t workspace_bytes, void* hip_stream);
+int sdgp_token_logprobs_bwd(const void* logits, int64_t ld, const void* tokens, int token_bits, const float* stats,
+                            const float* entropy, const float* g_logp, const float* g_entropy, void* dlogits,
+                            int64_t ld_out, int64_t rows, int64_t V, int dt, float scale, void* hip_stream);
+
+/*
+ * sdgp_block_norm -- the norm after a block, its gate, the scaled residual and the norm before the next block.
+ *
+ *   a = u / sqrt(mean(u^2) + eps)                     u [rows, D]: the block's output
+ *   y = residual_scale * x + gate * (a * w_post)      x [rows, D]: the residual stream; y its next value, as stored
+ *   h = y / sqrt(mean(y^2) + eps) * w_pre             h: what the next block reads, from y as stored
+ *
+ *   u         NULL: there is no block yet; y is x (pass y NULL), h its norm
+ *   gate      [groups, D] of `dt`, row r uses gate r / (rows / groups): one for all rows (groups 1), one a sample, one a row
+ *             (groups == rows); NULL with groups 0
+ *   w_post, w_pre  [D] of `wdt` (fp32 or bf16), or NULL for ones
+ *   h         NULL: no norm follows (then w_pre is NULL too)
+ *   stats     [2, rows] fp32: the two norms' factors 1/sqrt(...), for the gradient
+ *   x, u, y, h, gate `dt`; arithmetic fp32.  rows % groups == 0, D >= 1.  Outputs overlap no input.
+ *
+ * sdgp_block_norm_bwd -- dL/dx, dL/du, dL/dgate and the weights' gradients from dy (of the stored y; NULL: 0) and dh (NULL
+ * with h NULL).  y is x where there was no block.  dx, du, dgate `dt`; dw_post, dw_pre [D] fp32, present exactly where the
+ * weight is, 0 for no rows.  The sums over rows are fp32 in a fixed order: the same bits from call to call.
+ *
+ * workspace: sdgp_block_norm_bwd_workspace(...) bytes, 16-byte aligned, contents undefined afterwards.
+ */
+int sdgp_block_norm(const void* x, const void* u, const void* gate, const void* w_post, const void* w_pre, void* y,
+                    void* h, float* stats, int64_t rows, int64_t D, int64_t groups, int dt, int wdt,
+                    float residual_scale, float eps, void* hip_stream);
+size_t sdgp_block_norm_bwd_workspace(int64_t rows, int64_t D, int64_t groups, int dt);
+int sdgp_block_norm_bwd(const void* dy, const void* dh, const void* y, const void* u, const void* gate,
+                        const void* w_post, const void* w_pre, const float* stats, void* dx, void* du, void* dgate,
+                        float* dw_post, float* dw_pre, int64_t rows, int64_t D, int64_t groups, int dt, int wdt,
+                        float residual_scale, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * sdgp_adamw_step -- one AdamW step over `count` tensors, in place.
+ *
+ *   g = grad * grad_scale;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
+ *   p = p (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
+ *
+ *   params, grads, exp_avg, exp_avg_sq, exp_avg_scale, exp_avg_sq_scale, copies, numel: HOST arrays of `count` entries
+ *   (read before the call returns) of device pointers and element counts; every tensor contiguous.
+ *   params      `param_dt`; grads `grad_dt`
+ *   copies      bf16 copies of fp32 parameters, written beside them, or NULL
+ *   state_bits  32: exp_avg, exp_avg_sq hold m and v in fp32, the scale arrays are NULL.
+ *               8:  they hold m and sqrt(v) as e4m3 codes (uint8), one scale for 256 consecutive elements in
+ *               exp_avg_scale / exp_avg_sq_scale (fp32, ceil(numel / 256) of them, powers of two: the smallest 2^k >=
+ *               2^-126 with the block's largest finite magnitude <= 448 * 2^k, 1 for a block of zeros).  Values are
+ *               rounded to one of the two codes around them, up where u exceeds what is cut off: u is the low (m) and the
+ *               high (sqrt(v)) 16 bits of the word below, over 2^16.  sqrt(v) > 0 is not stored as 0.  Infinite and NaN
+ *               values are stored as NaN.
+ *                 v = mix(seed) ^ low word of e ^ (high word of e * 0xBB67AE85), mixed as the random ranker's hash does;
+ *               e counts the elements of the call, each tensor from the next multiple of 256.
+ *   step        1 for the first one;  seed: another for every step (8-bit states only)
+ *   grad_scale  device pointer to one fp32, or NULL for 1: what clipping or loss scaling leaves, read on the stream
+ */
+int sdgp_adamw_step(int count, void* const* params, const void* const* grads, void* const* exp_avg,
+                    void* const* exp_avg_sq, float* const* exp_avg_scale, float* const* exp_avg_sq_scale,
+                    void* const* copies, const int64_t* numel, int param_dt, int grad_dt, int state_bits, double lr,
+                    double beta1, double beta2, double eps, double weight_decay, int64_t step, const float* grad_scale,
+                    uint64_t seed, void* hip_stream);
 
 /*
  * Measurement aid: what the GPU sustains on the two resources the path is bound by (the benchmark reports its

@@ -28,6 +28,8 @@ EXPORTS = ("sdgp_prune", "sdgp_linear_bwd_data", "sdgp_conv_bwd_data", "sdgp_con
            "sdgp_conv_bwd_data_compact_workspace", "sdgp_conv_bwd_data_compact",
            "sdgp_conv_bwd_data_grouped_workspace", "sdgp_conv_bwd_data_grouped",
            "sdgp_conv_fwd_workspace", "sdgp_conv_fwd", "sdgp_conv_bwd_weight_workspace", "sdgp_conv_bwd_weight",
+           "sdgp_token_logprobs_workspace", "sdgp_token_logprobs", "sdgp_token_logprobs_bwd",
+           "sdgp_block_norm", "sdgp_block_norm_bwd_workspace", "sdgp_block_norm_bwd", "sdgp_adamw_step",
            "sdgp_peak_probe", "sdgp_status_string", "sdgp_version")
 
 
@@ -97,6 +99,21 @@ def load():
             lib.sdgp_conv_bwd_weight_workspace.argtypes = geom
             lib.sdgp_conv_bwd_weight.restype = i32
             lib.sdgp_conv_bwd_weight.argtypes = [vp, vp, vp] + geom + [vp, sz, vp]
+            f32, f64 = ctypes.c_float, ctypes.c_double
+            lib.sdgp_token_logprobs_workspace.restype = sz
+            lib.sdgp_token_logprobs_workspace.argtypes = [i64, i64, i32, i32]
+            lib.sdgp_token_logprobs.restype = i32
+            lib.sdgp_token_logprobs.argtypes = [vp, i64, vp, i32, vp, vp, vp, vp, vp, i64, i64, i32, i32, f32, vp, sz, vp]
+            lib.sdgp_token_logprobs_bwd.restype = i32
+            lib.sdgp_token_logprobs_bwd.argtypes = [vp, i64, vp, i32, vp, vp, vp, vp, vp, i64, i64, i64, i32, f32, vp]
+            lib.sdgp_block_norm.restype = i32
+            lib.sdgp_block_norm.argtypes = [vp] * 8 + [i64, i64, i64, i32, i32, f32, f32, vp]
+            lib.sdgp_block_norm_bwd_workspace.restype = sz
+            lib.sdgp_block_norm_bwd_workspace.argtypes = [i64, i64, i64, i32]
+            lib.sdgp_block_norm_bwd.restype = i32
+            lib.sdgp_block_norm_bwd.argtypes = [vp] * 13 + [i64, i64, i64, i32, i32, f32, vp, sz, vp]
+            lib.sdgp_adamw_step.restype = i32
+            lib.sdgp_adamw_step.argtypes = [i32] + [vp] * 8 + [i32, i32, i32, f64, f64, f64, f64, f64, i64, vp, u64, vp]
             lib.sdgp_peak_probe.restype = i32
             lib.sdgp_peak_probe.argtypes = [i32, vp, vp, sz, i32, ctypes.POINTER(ctypes.c_double), vp]
             lib.sdgp_status_string.restype = ctypes.c_char_p
@@ -468,3 +485,199 @@ def sdgp_conv_bwd_weight(D: torch.Tensor, dO: torch.Tensor, R: int, S: int, stri
     if rc != 0:
         raise SdgpError(rc, "sdgp_conv_bwd_weight")
     return out
+
+
+# ---------------------------------------------- around the pruned layers: the loss, the norms between blocks
+
+def _row_stride(t: torch.Tensor, name: str) -> int:
+    """The distance of two rows of ``t`` ([..., V], last stride 1, leading axes evenly spaced)."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must live on the GPU")
+    if t.is_contiguous():
+        return t.shape[-1]
+    if t.dim() == 2 and t.stride(1) == 1 and t.stride(0) >= t.shape[1]:
+        return t.stride(0)
+    V = t.shape[-1]
+    expect = None
+    for size, stride in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if size == 1:
+            continue
+        if expect is None:
+            ld, expect = stride, stride * size
+        elif stride == expect:
+            expect *= size
+        else:
+            raise ValueError(f"the rows of {name} must be evenly spaced")
+    if expect is None:
+        ld = V
+    if (V > 1 and t.stride(-1) != 1) or ld < V:
+        raise ValueError(f"{name} must have rows with stride 1 that do not overlap")
+    return ld
+
+
+def _per_row(t: torch.Tensor, shape, name: str, dtypes) -> torch.Tensor:
+    _dev(t, name)
+    if t.shape != shape or t.dtype not in dtypes:
+        raise ValueError(f"{name} must be {' or '.join(str(d) for d in dtypes)} {tuple(shape)}")
+    return t
+
+
+_FLOAT, _INTS = (torch.float32,), (torch.int64, torch.int32)
+
+
+def sdgp_token_logprobs(logits: torch.Tensor, tokens: torch.Tensor | None, *, top: int = 0, scale: float = 1.0,
+                        workspace: torch.Tensor | None = None):
+    """Log probabilities of ``tokens`` ([...], < 0 for none) under softmax(scale * logits) ([..., V]), each row's entropy
+    and its ``top`` best alternatives.  Returns ``(logp, entropy, top_logp, top_ids, stats)``; what is not asked for is
+    None, ``stats`` is for ``sdgp_token_logprobs_bwd``."""
+    if logits.dim() < 1:
+        raise ValueError("expected logits [..., V]")
+    ld, dt = _row_stride(logits, "logits"), _dtype_code(logits)
+    shape, V = logits.shape[:-1], logits.shape[-1]
+    rows = shape.numel()
+    bits = 64
+    if tokens is not None:
+        _per_row(tokens, shape, "tokens", _INTS)
+        bits = 64 if tokens.dtype == torch.int64 else 32
+    lib = load()
+    need = _need("sdgp_token_logprobs_workspace", rows, V, dt, top)
+    if need == _INVALID:
+        raise SdgpError(-3, "sdgp_token_logprobs")
+    wbytes = 0
+    if need:
+        workspace, wbytes = _workspace(need, workspace, logits.device, "sdgp_token_logprobs_workspace")
+    new = functools.partial(torch.empty, dtype=torch.float32, device=logits.device)
+    logp = None if tokens is None else new(shape)
+    entropy, stats = new(shape), new((*shape, 2))
+    top_logp = top_ids = None
+    if top:
+        top_logp, top_ids = new((*shape, top)), torch.empty((*shape, top), dtype=torch.int64, device=logits.device)
+    rc = lib.sdgp_token_logprobs(_ptr(logits), ld, _ptr(tokens), bits, _ptr(logp), _ptr(entropy), _ptr(top_logp), _ptr(top_ids),
+                                 _ptr(stats), rows, V, dt, top, scale, _ptr(workspace) if need else None, wbytes, _stream(logits))
+    if rc != 0:
+        raise SdgpError(rc, "sdgp_token_logprobs")
+    return logp, entropy, top_logp, top_ids, stats
+
+
+def sdgp_token_logprobs_bwd(logits: torch.Tensor, tokens: torch.Tensor | None, stats: torch.Tensor, entropy: torch.Tensor | None,
+                            g_logp: torch.Tensor | None, g_entropy: torch.Tensor | None = None, *, scale: float = 1.0,
+                            out: torch.Tensor | None = None) -> torch.Tensor:
+    """dL/dlogits from dL/dlogp and dL/dentropy (fp32 [...], either may be None): what ``sdgp_linear_bwd_data`` takes as
+    dO.  ``out`` may be ``logits`` itself."""
+    ld, dt = _row_stride(logits, "logits"), _dtype_code(logits)
+    shape, V = logits.shape[:-1], logits.shape[-1]
+    if g_logp is None and g_entropy is None:
+        raise ValueError("one of g_logp and g_entropy is needed")
+    _per_row(stats, (*shape, 2), "stats", _FLOAT)
+    bits = 64
+    if g_logp is not None:
+        if tokens is None:
+            raise ValueError("g_logp needs tokens")
+        _per_row(g_logp, shape, "g_logp", _FLOAT)
+        _per_row(tokens, shape, "tokens", _INTS)
+        bits = 64 if tokens.dtype == torch.int64 else 32
+    if g_entropy is not None:
+        if entropy is None:
+            raise ValueError("g_entropy needs entropy")
+        _per_row(g_entropy, shape, "g_entropy", _FLOAT)
+        _per_row(entropy, shape, "entropy", _FLOAT)
+    if out is None:
+        out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    if out.shape != logits.shape or out.dtype != logits.dtype:
+        raise ValueError("out must have the shape and dtype of logits")
+    rc = load().sdgp_token_logprobs_bwd(_ptr(logits), ld, _ptr(tokens), bits, _ptr(stats), _ptr(entropy), _ptr(g_logp),
+                                        _ptr(g_entropy), _ptr(out), _row_stride(out, "out"), shape.numel(), V, dt, scale,
+                                        _stream(logits))
+    if rc != 0:
+        raise SdgpError(rc, "sdgp_token_logprobs_bwd")
+    return out
+
+
+def _like(t, x: torch.Tensor, name: str):
+    if t is not None:
+        _dev(t, name)
+        if t.shape != x.shape or t.dtype != x.dtype:
+            raise ValueError(f"{name} must have the shape and dtype of the residual stream")
+
+
+def _gate_and_weights(D: int, rows: int, dtype, gate, w_post, w_pre):
+    """(groups, code of the weights' dtype) of checked arguments."""
+    groups = 0
+    if gate is not None:
+        _dev(gate, "gate")
+        if gate.shape[-1] != D or gate.dtype != dtype:
+            raise ValueError("gate must be [..., D] of the residual stream's dtype")
+        groups = gate.numel() // D
+        if groups == 0 and rows or groups and rows % groups:
+            raise ValueError("the rows must be a multiple of the gate's")
+    wdt = F32
+    for w, name in ((w_post, "w_post"), (w_pre, "w_pre")):
+        if w is not None:
+            _dev(w, name)
+            if w.shape != (D,):
+                raise ValueError(f"{name} must be [D]")
+            wdt = _dtype_code(w)
+    if w_post is not None and w_pre is not None and w_post.dtype != w_pre.dtype:
+        raise ValueError("w_post and w_pre must have one dtype")
+    return groups, wdt
+
+
+def sdgp_block_norm(x: torch.Tensor, u: torch.Tensor | None = None, gate: torch.Tensor | None = None,
+                    w_post: torch.Tensor | None = None, w_pre: torch.Tensor | None = None, *, residual_scale: float = 1.0,
+                    eps: float = 1e-6, pre: bool = True):
+    """y = residual_scale * x + gate * (rms_norm(u) * w_post) and h = rms_norm(y) * w_pre over the last axis, in one pass.
+
+    ``u``: the block's output, None where there is none yet (y is then ``x`` itself).  ``gate``: [D], or [G, D] with row r
+    of the flattened x using gate r // (rows / G).  ``pre=False``: no norm follows, h is None.  Returns ``(y, h, stats)``;
+    ``stats`` is for ``sdgp_block_norm_bwd``."""
+    _dev(x, "x")
+    if x.dim() < 1 or x.shape[-1] < 1:
+        raise ValueError("expected x [..., D]")
+    _like(u, x, "u")
+    if u is None and (gate is not None or w_post is not None or not pre):
+        raise ValueError("gate and w_post belong to a block's output, and without one there is only the norm")
+    if not pre and w_pre is not None:
+        raise ValueError("w_pre is the weight of the norm that pre=False leaves out")
+    D = x.shape[-1]
+    rows = x.numel() // D
+    groups, wdt = _gate_and_weights(D, rows, x.dtype, gate, w_post, w_pre)
+    y = x if u is None else torch.empty_like(x)
+    h = torch.empty_like(x) if pre else None
+    stats = torch.empty((2, rows), dtype=torch.float32, device=x.device)
+    rc = load().sdgp_block_norm(_ptr(x), _ptr(u), _ptr(gate), _ptr(w_post), _ptr(w_pre), None if u is None else _ptr(y), _ptr(h),
+                                _ptr(stats), rows, D, groups, _dtype_code(x), wdt, residual_scale, eps, _stream(x))
+    if rc != 0:
+        raise SdgpError(rc, "sdgp_block_norm")
+    return y, h, stats
+
+
+def sdgp_block_norm_bwd(dy: torch.Tensor | None, dh: torch.Tensor | None, y: torch.Tensor, stats: torch.Tensor,
+                        u: torch.Tensor | None = None, gate: torch.Tensor | None = None, w_post: torch.Tensor | None = None,
+                        w_pre: torch.Tensor | None = None, *, residual_scale: float = 1.0, workspace: torch.Tensor | None = None):
+    """Gradients of ``sdgp_block_norm``: ``(dx, du, dgate, dw_post, dw_pre)``, the weights' in fp32, None for what was not
+    given.  ``dh`` is None exactly where the call left h out; ``dy`` None counts as 0."""
+    _dev(y, "y")
+    for t, name in ((dy, "dy"), (dh, "dh"), (u, "u")):
+        _like(t, y, name)
+    if dy is None and dh is None:
+        raise ValueError("one of dy and dh is needed")
+    if u is None and (gate is not None or w_post is not None) or dh is None and w_pre is not None:
+        raise ValueError("gate and w_post belong to a block's output, w_pre to the norm behind it")
+    D = y.shape[-1]
+    rows = y.numel() // D
+    _per_row(stats, (2, rows), "stats", _FLOAT)
+    groups, wdt = _gate_and_weights(D, rows, y.dtype, gate, w_post, w_pre)
+    dt = _dtype_code(y)
+    lib = load()
+    workspace, wbytes = _workspace(_need("sdgp_block_norm_bwd_workspace", rows, D, groups, dt), workspace, y.device,
+                                   "sdgp_block_norm_bwd_workspace")
+    dx = torch.empty_like(y)
+    du = None if u is None else torch.empty_like(y)
+    dgate = None if gate is None else torch.empty_like(gate)
+    dw_post, dw_pre = (None if w is None else torch.empty(D, dtype=torch.float32, device=y.device) for w in (w_post, w_pre))
+    rc = lib.sdgp_block_norm_bwd(_ptr(dy), _ptr(dh), _ptr(y), _ptr(u), _ptr(gate), _ptr(w_post), _ptr(w_pre), _ptr(stats), _ptr(dx),
+                                 _ptr(du), _ptr(dgate), _ptr(dw_post), _ptr(dw_pre), rows, D, groups, dt, wdt, residual_scale,
+                                 _ptr(workspace), wbytes, _stream(y))
+    if rc != 0:
+        raise SdgpError(rc, "sdgp_block_norm_bwd")
+    return dx, du, dgate, dw_post, dw_pre

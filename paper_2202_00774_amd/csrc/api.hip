@@ -585,6 +585,7 @@ const char* sdgp_status_string(int status) {
         case SDGP_ERR_RANKER: return "unknown ranker";
         case SDGP_ERR_WORKSPACE: return "workspace missing or too small";
         case SDGP_ERR_HIP: return "the HIP runtime reported an error";
+        case SDGP_ERR_VALUE: return "a scalar argument is outside its range";
         default: return "unknown status";
     }
 }
