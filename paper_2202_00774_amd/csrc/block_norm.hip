@@ -9,7 +9,10 @@
 //   da = dY * gate * w_post;  du = r_u (da - a mean(da a))
 //   dw_pre = sum_rows dh t;  dw_post = sum_rows dY gate a;  dgate = sum over a gate's rows of dY a w_post
 // Everything between a load and its store is fp32.  The sums over rows have a fixed order: no atomics.
-#include "common.h"
+//
+// Rows that fit the registers of a workgroup go to the kernels of block_norm_rows.h; the ones here take any width and
+// read a row again for each sum.  Backward, either kind leaves sums over slabs of rows, which norm_grad_finish adds up.
+#include "block_norm.h"
 
 namespace sdgp {
 
@@ -42,16 +45,7 @@ __device__ __forceinline__ float block_sum(float v, float* lds) {
     return (lds[0] + lds[1]) + (lds[2] + lds[3]);
 }
 
-struct Norm {
-    const void *x, *u, *gate, *w_post, *w_pre;
-    void *y, *h;
-    float* stats;
-    int64_t rows, per_gate;   // rows that share a gate
-    int D, dt, wdt;
-    float residual_scale, eps;
-};
-
-__global__ void __launch_bounds__(kBlock) norm_rows(const Norm n) {
+__global__ void __launch_bounds__(kBlock) norm_long_rows(const Norm n) {
     __shared__ float lds[kWaves];
     for (int64_t r = blockIdx.x; r < n.rows; r += gridDim.x) {
     const int64_t base = r * n.D;
@@ -92,17 +86,6 @@ __global__ void __launch_bounds__(kBlock) norm_rows(const Norm n) {
     }
 }
 
-struct NormGrad {
-    const void *dy, *dh, *y, *u, *gate, *w_post, *w_pre;
-    const float* stats;
-    void *dx, *du, *dgate;
-    float *dw_post, *dw_pre;
-    float* mean;              // [rows]: mean(dn t), for the sums over rows
-    int64_t rows, per_gate, groups;
-    int D, dt, wdt;
-    float residual_scale;
-};
-
 __device__ __forceinline__ float weight(const void* w, int dt, int64_t i) { return w ? load1(w, dt, i) : 1.0f; }
 
 // dY of one element, dL/dy with the norm behind it taken in.
@@ -115,7 +98,7 @@ __device__ __forceinline__ float grad_y(const NormGrad& n, int64_t i, int d, flo
     return v;
 }
 
-__global__ void __launch_bounds__(kBlock) norm_grad_rows(const NormGrad n) {
+__global__ void __launch_bounds__(kBlock) norm_grad_long_rows(const NormGrad n, float* __restrict__ means) {
     __shared__ float lds[kWaves];
     for (int64_t r = blockIdx.x; r < n.rows; r += gridDim.x) {
     const int64_t base = r * n.D;
@@ -128,7 +111,7 @@ __global__ void __launch_bounds__(kBlock) norm_grad_rows(const NormGrad n) {
             sum += load1(n.dh, n.dt, base + d) * weight(n.w_pre, n.wdt, d) * (load1(n.y, n.dt, base + d) * ry);
         mean = block_sum(sum, lds) / n.D;
     }
-    if (tid == 0) n.mean[r] = mean;
+    if (tid == 0) means[r] = mean;
     float ru = 0.0f, mean_a = 0.0f;
     const int64_t gbase = n.gate ? r / n.per_gate * n.D : 0;
     if (n.u) {
@@ -151,27 +134,98 @@ __global__ void __launch_bounds__(kBlock) norm_grad_rows(const NormGrad n) {
     }
 }
 
-// Sums over rows, one thread a column.
-__global__ void __launch_bounds__(kBlock) norm_grad_columns(const NormGrad n) {
+// The slabs' sums over rows of any width, one thread a column.
+__global__ void __launch_bounds__(kBlock) norm_grad_columns(const NormGrad n, const float* __restrict__ means) {
     const int d = blockIdx.x * kBlock + threadIdx.x;
     if (d >= n.D) return;
-    float pre = 0.0f, post = 0.0f, gate = 0.0f;
-    for (int64_t r = 0; r < n.rows; ++r) {
+    const int64_t slab = blockIdx.y;
+    const float w = weight(n.w_post, n.wdt, d);
+    int64_t first, end;
+    if (n.slabs.kind == kWholeGroups) {
+        first = slab * n.slabs.len * n.per_gate;
+        end = first + n.slabs.len * n.per_gate < n.rows ? first + n.slabs.len * n.per_gate : n.rows;
+    } else {
+        const int64_t gate0 = slab / n.slabs.parts * n.per_gate;
+        first = gate0 + slab % n.slabs.parts * n.slabs.len;
+        end = first + n.slabs.len < gate0 + n.per_gate ? first + n.slabs.len : gate0 + n.per_gate;
+    }
+    float pre = 0.0f, post = 0.0f, sum = 0.0f;
+    for (int64_t r = first; r < end; ++r) {
         const int64_t i = r * n.D + d;
         const float ry = n.dh ? n.stats[n.rows + r] : 0.0f;
         if (n.dh) pre += load1(n.dh, n.dt, i) * (load1(n.y, n.dt, i) * ry);
         if (!n.u) continue;
-        const float da = grad_y(n, i, d, ry, n.mean[r]) * (load1(n.u, n.dt, i) * n.stats[r]);
-        const int64_t g = n.gate ? r / n.per_gate : 0;
-        post += da * weight(n.gate, n.dt, g * n.D + d);
-        gate += da;
-        if (n.gate && (r + 1) % n.per_gate == 0) {
-            store1(n.dgate, n.dt, g * n.D + d, gate * weight(n.w_post, n.wdt, d));
-            gate = 0.0f;
+        sum += grad_y(n, i, d, ry, means[r]) * (load1(n.u, n.dt, i) * n.stats[r]);
+        if (n.slabs.kind == kWholeGroups && (r + 1) % n.per_gate == 0) {
+            const int64_t g = (r / n.per_gate) * n.D + d;
+            store1(n.dgate, n.dt, g, sum * w);
+            post += sum * load1(n.gate, n.dt, g);
+            sum = 0.0f;
         }
     }
-    if (n.dw_pre) n.dw_pre[d] = pre;
-    if (n.dw_post) n.dw_post[d] = post;
+    if (n.part_pre) n.part_pre[slab * n.D + d] = pre;
+    if (n.part_post) n.part_post[slab * n.D + d] = n.slabs.kind == kWholeGroups ? post : sum;
+}
+
+// Adds up the slabs' sums: 32 columns a workgroup, 32 threads down each.  In kInGroup a gate's slabs are added first, to
+// dgate, and the gates' sums times the gate to dw_post.  Fixed order throughout.
+constexpr int kCols = 32, kDown = 32;
+
+__device__ __forceinline__ float add_down(float v, float (*lds)[kCols + 1]) {
+    const int col = threadIdx.x % kCols, down = threadIdx.x / kCols;
+    __syncthreads();
+    lds[down][col] = v;
+    __syncthreads();
+    for (int o = kDown / 2; o > 0; o /= 2) {
+        if (down < o) lds[down][col] += lds[down + o][col];
+        __syncthreads();
+    }
+    return lds[0][col];
+}
+
+__device__ __forceinline__ float add_slabs(const float* part, int D, int64_t first, int64_t end, int64_t step, int d) {
+    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    int64_t i = first;
+    for (; i + 3 * step < end; i += 4 * step)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) s[k] += part[(i + k * step) * D + d];
+    for (; i < end; i += step) s[0] += part[i * D + d];
+    return (s[0] + s[1]) + (s[2] + s[3]);
+}
+
+__global__ void __launch_bounds__(kCols* kDown) norm_grad_finish(const NormGrad n) {
+    __shared__ float lds[kDown][kCols + 1];
+    const int d = blockIdx.x * kCols + threadIdx.x % kCols, down = threadIdx.x / kCols;
+    const bool in = d < n.D;
+    if (n.part_pre) {
+        const float s = add_down(in ? add_slabs(n.part_pre, n.D, down, n.slabs.count, kDown, d) : 0.0f, lds);
+        if (in && down == 0) n.dw_pre[d] = s;
+    }
+    if (!n.part_post) return;
+    float post = 0.0f;
+    if (n.slabs.kind == kWholeGroups || !n.gate) {
+        post = add_down(in ? add_slabs(n.part_post, n.D, down, n.slabs.count, kDown, d) : 0.0f, lds);
+    } else {
+        const float w = in ? weight(n.w_post, n.wdt, d) : 0.0f;
+        const int64_t parts = n.slabs.parts;
+        if (parts >= kDown) {          // many slabs a gate: all threads of a column on one gate
+            for (int64_t g = 0; g < n.groups; ++g) {
+                const float s = add_down(in ? add_slabs(n.part_post, n.D, g * parts + down, (g + 1) * parts, kDown, d) : 0.0f, lds);
+                if (!in || down != 0) continue;
+                store1(n.dgate, n.dt, g * n.D + d, s * w);
+                post += s * load1(n.gate, n.dt, g * n.D + d);
+            }
+        } else {                       // few: a gate a thread
+            if (in)
+                for (int64_t g = down; g < n.groups; g += kDown) {
+                    const float s = add_slabs(n.part_post, n.D, g * parts, (g + 1) * parts, 1, d);
+                    store1(n.dgate, n.dt, g * n.D + d, s * w);
+                    post += s * load1(n.gate, n.dt, g * n.D + d);
+                }
+            post = add_down(post, lds);
+        }
+    }
+    if (in && down == 0 && n.dw_post) n.dw_post[d] = post;
 }
 
 __global__ void __launch_bounds__(kBlock) clear_words(uint16_t* __restrict__ p, int64_t n) {
@@ -196,13 +250,46 @@ int block_norm_bwd_no_rows(void* dgate, int64_t gate_elements, int dt, float* dw
     return SDGP_OK;
 }
 
-size_t block_norm_bwd_workspace(int64_t rows, int64_t, int64_t, int) { return (size_t)rows * 4; }
+// A slab costs its columns' sums written and read again, so it holds eight rows for each that a workgroup has in hand,
+// unless that leaves fewer than 256 workgroups, one a CU; more than 1024 hide no more latency.  Gates of up to 32 rows
+// that are many (2048) are finished by the slab that holds them.
+static Slabs make_slabs(int64_t rows, int64_t D, int64_t groups, int dt) {
+    const RowShape shape = row_shape(D, dt);
+    const int64_t at_once = shape.threads == 0 || shape.threads >= 256 ? 1 : 256 / shape.threads;
+    const int64_t g = groups > 0 ? groups : 1, per_gate = rows / g;
+    Slabs s;
+    int64_t want = rows / (8 * at_once);
+    want = want < 256 ? 256 : want > 1024 ? 1024 : want;
+    if (groups > 0 && (per_gate == 1 || (per_gate <= 32 && groups >= 2048))) {
+        s.kind = kWholeGroups;
+        s.len = ((groups + want - 1) / want + at_once - 1) / at_once * at_once;
+        s.parts = 1;
+        s.count = (groups + s.len - 1) / s.len;
+    } else {
+        s.kind = kInGroup;
+        int64_t parts = want / g;
+        const int64_t most = (per_gate + at_once - 1) / at_once;
+        parts = parts < 1 ? 1 : parts > most ? most : parts;
+        s.len = ((per_gate + parts - 1) / parts + at_once - 1) / at_once * at_once;
+        s.parts = (per_gate + s.len - 1) / s.len;
+        s.count = s.parts * g;
+    }
+    return s;
+}
+
+size_t block_norm_bwd_workspace(int64_t rows, int64_t D, int64_t groups, int dt) {
+    const size_t sums = (size_t)make_slabs(rows, D, groups, dt).count * (size_t)D * 2 * sizeof(float);
+    return sums + (row_shape(D, dt).threads == 0 ? (size_t)rows * sizeof(float) : 0);
+}
 
 int block_norm_launch(const void* x, const void* u, const void* gate, const void* w_post, const void* w_pre, void* y, void* h,
                       float* stats, int64_t rows, int64_t D, int64_t groups, int dt, int wdt, float residual_scale, float eps,
                       hipStream_t stream) {
     const Norm n = {x, u, gate, w_post, w_pre, y, h, stats, rows, groups > 0 ? rows / groups : rows, (int)D, dt, wdt, residual_scale, eps};
-    hipLaunchKernelGGL(norm_rows, dim3((unsigned)(rows < 65536 ? rows : 65536)), dim3(kBlock), 0, stream, n);
+    const RowShape shape = row_shape(D, dt);
+    if (shape.threads > 0)
+        return dt == SDGP_BF16 ? norm_rows_launch<SDGP_BF16>(n, shape, stream) : norm_rows_launch<SDGP_F32>(n, shape, stream);
+    hipLaunchKernelGGL(norm_long_rows, dim3((unsigned)(rows < 65536 ? rows : 65536)), dim3(kBlock), 0, stream, n);
     return launch_status();
 }
 
@@ -210,12 +297,28 @@ int block_norm_bwd_launch(const void* dy, const void* dh, const void* y, const v
                           const void* w_pre, const float* stats, void* dx, void* du, void* dgate, float* dw_post, float* dw_pre,
                           int64_t rows, int64_t D, int64_t groups, int dt, int wdt, float residual_scale, void* workspace,
                           hipStream_t stream) {
-    const NormGrad n = {dy, dh, y, u, gate, w_post, w_pre, stats, dx, du, dgate, dw_post, dw_pre, static_cast<float*>(workspace), rows,
-                        groups > 0 ? rows / groups : rows, groups, (int)D, dt, wdt, residual_scale};
-    hipLaunchKernelGGL(norm_grad_rows, dim3((unsigned)(rows < 65536 ? rows : 65536)), dim3(kBlock), 0, stream, n);
-    int rc = launch_status();
-    if (rc != SDGP_OK) return rc;
-    hipLaunchKernelGGL(norm_grad_columns, dim3((unsigned)((D + kBlock - 1) / kBlock)), dim3(kBlock), 0, stream, n);
+    const Slabs slabs = make_slabs(rows, D, groups, dt);
+    float* sums = static_cast<float*>(workspace);
+    const int64_t each = slabs.count * D;
+    const bool post = w_post != nullptr || (gate != nullptr && slabs.kind == kInGroup);
+    const NormGrad n = {dy, dh, y, u, gate, w_post, w_pre, stats, dx, du, dgate, dw_post, dw_pre, w_pre ? sums : nullptr,
+                        post ? sums + each : nullptr, rows, groups, groups > 0 ? rows / groups : rows, slabs, (int)D, dt, wdt, residual_scale};
+    const RowShape shape = row_shape(D, dt);
+    int rc;
+    if (shape.threads > 0) {
+        rc = dt == SDGP_BF16 ? norm_grad_launch<SDGP_BF16>(n, shape, stream) : norm_grad_launch<SDGP_F32>(n, shape, stream);
+    } else {
+        float* means = sums + 2 * each;
+        hipLaunchKernelGGL(norm_grad_long_rows, dim3((unsigned)(rows < 65536 ? rows : 65536)), dim3(kBlock), 0, stream, n, means);
+        rc = launch_status();
+        if (rc != SDGP_OK) return rc;
+        if (n.part_pre || n.part_post || gate) {
+            hipLaunchKernelGGL(norm_grad_columns, dim3((unsigned)((D + kBlock - 1) / kBlock), (unsigned)slabs.count), dim3(kBlock), 0, stream, n, means);
+            rc = launch_status();
+        }
+    }
+    if (rc != SDGP_OK || (!n.part_pre && !n.part_post)) return rc;
+    hipLaunchKernelGGL(norm_grad_finish, dim3((unsigned)((D + kCols - 1) / kCols)), dim3(kCols * kDown), 0, stream, n);
     return launch_status();
 }
 

@@ -1,0 +1,313 @@
+// Block norms of rows that fit the registers, forward and backward (the formulas stand in block_norm.hip).
+//
+// Bound by memory: 8 bytes an element forward (x, u in; y, h out), 12 backward (y, u, dy, dh in; dx, du out) in bf16, with
+// 15 and 30 vector instructions beside them.  Every value is loaded once and stays in registers, packed as stored,
+// until its row's sums are known.  Backward, the second norm's sum depends on the first's result (dY holds the
+// mean of dn t), but linearly: with v = dy + r_y dn,
+//     sum dY k a = sum v k a - r_y mean(dn t) sum t k a,        k = gate w_post,
+// so all three sums go over the lanes together and a row costs one exchange, not two.
+#pragma once
+
+#include "block_norm.h"
+
+namespace sdgp {
+
+namespace {
+
+template <int T>
+constexpr int norm_block() { return T < 256 ? 256 : T; }
+
+template <int DT, int T, int NV, bool BLOCK>
+__global__ void __launch_bounds__(norm_block<T>()) norm_fwd(const Norm n, int64_t rows_per_wg) {
+    using V = RowVec<DT>;
+    constexpr int N = V::kN, R = norm_block<T>() / T;
+    constexpr int64_t kSize = sizeof(typename V::Elem);
+    __shared__ float lds[T > 64 ? 2 * (T / 64) : 1];
+    int turn = 0;
+    const int t = threadIdx.x % T, sub = threadIdx.x / T;
+    const int64_t first = (int64_t)blockIdx.x * rows_per_wg;
+    const int64_t end = first + rows_per_wg < n.rows ? first + rows_per_wg : n.rows;
+    const float inv_d = 1.0f / (float)n.D;
+
+    float post[NV][N], pre[NV][N];
+    const bool one_gate = BLOCK && n.gate != nullptr && n.per_gate == n.rows;
+    const bool many_gates = BLOCK && n.gate != nullptr && n.per_gate != n.rows;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        const int e = (v * T + t) * N;
+        load_weights<N>(n.w_pre, n.wdt, e, n.D, pre[v]);
+        if constexpr (BLOCK) {
+            load_weights<N>(n.w_post, n.wdt, e, n.D, post[v]);
+            if (one_gate) {
+                const V g = load_row<DT>(n.gate, e, n.D);
+#pragma unroll
+                for (int i = 0; i < N; ++i) post[v][i] *= g.get(i);
+            }
+        }
+    }
+
+    for (int64_t r0 = first; r0 < end; r0 += R) {
+        const int64_t r = r0 + sub;
+        const bool live = r < end;
+        const int D = live ? n.D : 0;
+        const int64_t at = (live ? r : first) * n.D * kSize;
+        V x[NV], u[NV];
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int e = (v * T + t) * N;
+            x[v] = load_row<DT>(static_cast<const char*>(n.x) + at, e, D);
+            if constexpr (BLOCK) u[v] = load_row<DT>(static_cast<const char*>(n.u) + at, e, D);
+        }
+        float sum[1];
+        if constexpr (BLOCK) {
+            V g[NV];
+            if (many_gates) {
+                const int64_t gat = (live ? r : first) / n.per_gate * n.D * kSize;
+#pragma unroll
+                for (int v = 0; v < NV; ++v) g[v] = load_row<DT>(static_cast<const char*>(n.gate) + gat, (v * T + t) * N, D);
+            }
+            sum[0] = 0.0f;
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int i = 0; i < N; ++i) sum[0] += u[v].get(i) * u[v].get(i);
+            row_sums<T, 1>(sum, lds, turn);
+            const float ru = 1.0f / sqrtf(sum[0] * inv_d + n.eps);
+            if (t == 0 && live) n.stats[r] = ru;
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                float y[N];
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    float a = u[v].get(i) * ru * post[v][i];
+                    if (many_gates) a *= g[v].get(i);
+                    y[i] = n.residual_scale * x[v].get(i) + a;
+                }
+                x[v].set(y);   // y from here on, rounded as it is stored
+                store_row<DT>(static_cast<char*>(n.y) + at, (v * T + t) * N, D, x[v]);
+            }
+            if (n.h == nullptr) continue;
+        }
+        sum[0] = 0.0f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int i = 0; i < N; ++i) sum[0] += x[v].get(i) * x[v].get(i);
+        row_sums<T, 1>(sum, lds, turn);
+        const float ry = 1.0f / sqrtf(sum[0] * inv_d + n.eps);
+        if (t == 0 && live) n.stats[n.rows + r] = ry;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            float h[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) h[i] = x[v].get(i) * ry * pre[v][i];
+            V q;
+            q.set(h);
+            store_row<DT>(static_cast<char*>(n.h) + at, (v * T + t) * N, D, q);
+        }
+    }
+}
+
+// MODE: kNoBlock, or how the slab is cut.
+constexpr int kNoBlock = 2;
+
+template <int DT, int T, int NV, int MODE>
+__global__ void __launch_bounds__(norm_block<T>()) norm_bwd(const NormGrad n) {
+    using V = RowVec<DT>;
+    constexpr int N = V::kN, R = norm_block<T>() / T, kColumns = T * NV * N;
+    constexpr bool BLOCK = MODE != kNoBlock;
+    constexpr int64_t kSize = sizeof(typename V::Elem);
+    __shared__ float lds[R > 1 ? R * kColumns : T > 64 ? 2 * 3 * (T / 64) : 1];
+    int turn = 0;
+    const int t = threadIdx.x % T, sub = threadIdx.x / T;
+    const float inv_d = 1.0f / (float)n.D;
+
+    float w_pre[NV][N], k[NV][N];           // k: gate * w_post, or w_post while the gate changes
+    float sum_pre[NV][N], sum_post[NV][N];  // dh t, and dY a (kInGroup) or dY gate a (kWholeGroups)
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        load_weights<N>(n.w_pre, n.wdt, (v * T + t) * N, n.D, w_pre[v]);
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum_pre[v][i] = 0.0f, sum_post[v][i] = 0.0f, k[v][i] = 0.0f;
+    }
+
+    // the gates of this slab: one (kInGroup), or `len` of them, each sub-group of threads taking its own
+    const int64_t gate0 = MODE == kWholeGroups ? (int64_t)blockIdx.x * n.slabs.len : (int64_t)blockIdx.x / n.slabs.parts;
+    const int64_t gate1 = MODE != kWholeGroups ? gate0 + 1 : gate0 + n.slabs.len < n.groups ? gate0 + n.slabs.len : n.groups;
+    const int64_t step = MODE == kWholeGroups ? R : 1;
+    for (int64_t q0 = gate0; q0 < gate1; q0 += step) {
+        const int64_t q = MODE == kWholeGroups ? q0 + sub : q0;
+        const bool mine = q < gate1;
+        V gate[NV];
+        float sum_gate[NV][N];
+        if constexpr (BLOCK) {
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                const int e = (v * T + t) * N;
+                load_weights<N>(n.w_post, n.wdt, e, n.D, k[v]);
+                if (n.gate != nullptr) {
+                    gate[v] = load_row<DT>(static_cast<const char*>(n.gate) + (mine ? q : gate0) * n.D * kSize, e, n.D);
+#pragma unroll
+                    for (int i = 0; i < N; ++i) k[v][i] *= gate[v].get(i);
+                }
+#pragma unroll
+                for (int i = 0; i < N; ++i) sum_gate[v][i] = 0.0f;
+            }
+        }
+        int64_t first = q * n.per_gate, end = first + n.per_gate;
+        if constexpr (MODE != kWholeGroups) {
+            first += (int64_t)(blockIdx.x - gate0 * n.slabs.parts) * n.slabs.len;
+            if (first + n.slabs.len < end) end = first + n.slabs.len;
+        }
+        const int64_t rows = MODE == kWholeGroups ? n.per_gate : end - first;   // the same for all threads
+        for (int64_t i0 = 0; i0 < rows; i0 += MODE == kWholeGroups ? 1 : R) {
+            const int64_t r = first + i0 + (MODE == kWholeGroups ? 0 : sub);
+            const bool live = mine && r < end;
+            const int D = live ? n.D : 0;
+            const int64_t at = live ? r * n.D * kSize : 0;
+            V y[NV], u[NV], dy[NV], dh[NV];
+            const float ry = live && n.dh != nullptr ? n.stats[n.rows + r] : 0.0f;
+            const float ru = BLOCK && live ? n.stats[r] : 0.0f;
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                const int e = (v * T + t) * N;
+                y[v] = load_row<DT>(static_cast<const char*>(n.y) + at, e, n.dh != nullptr ? D : 0);
+                dh[v] = load_row<DT>(static_cast<const char*>(n.dh) + at, e, n.dh != nullptr ? D : 0);
+                dy[v] = load_row<DT>(static_cast<const char*>(n.dy) + at, e, n.dy != nullptr ? D : 0);
+                if constexpr (BLOCK) u[v] = load_row<DT>(static_cast<const char*>(n.u) + at, e, D);
+            }
+            float s[3] = {0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const float dn = dh[v].get(i) * w_pre[v][i], tt = y[v].get(i) * ry;
+                    s[0] += dn * tt;
+                    if constexpr (BLOCK) {
+                        const float ka = k[v][i] * (u[v].get(i) * ru);
+                        s[1] += ka * (dy[v].get(i) + ry * dn);
+                        s[2] += ka * tt;
+                    }
+                }
+            if constexpr (BLOCK) {
+                row_sums<T, 3>(s, lds, turn);
+            } else {
+                float one[1] = {s[0]};
+                row_sums<T, 1>(one, lds, turn);
+                s[0] = one[0];
+            }
+            const float c = ry * (s[0] * inv_d);              // r_y mean(dn t)
+            const float mean_a = (s[1] - c * s[2]) * inv_d;   // mean(dY k a)
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                const int e = (v * T + t) * N;
+                float dx[N], du[N];
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const float g = dh[v].get(i), tt = y[v].get(i) * ry;
+                    const float dY = dy[v].get(i) + ry * (g * w_pre[v][i]) - c * tt;
+                    sum_pre[v][i] += g * tt;
+                    dx[i] = dY;
+                    if constexpr (BLOCK) {
+                        const float a = u[v].get(i) * ru, da = dY * a;
+                        dx[i] = n.residual_scale * dY;
+                        du[i] = ru * (dY * k[v][i] - a * mean_a);
+                        if constexpr (MODE == kWholeGroups) sum_gate[v][i] += da;
+                        else sum_post[v][i] += da;
+                    }
+                }
+                V o;
+                o.set(dx);
+                store_row<DT>(static_cast<char*>(n.dx) + at, e, D, o);
+                if constexpr (BLOCK) {
+                    o.set(du);
+                    store_row<DT>(static_cast<char*>(n.du) + at, e, D, o);
+                }
+            }
+        }
+        if constexpr (MODE == kWholeGroups) {
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                const int e = (v * T + t) * N;
+                float w[N], d[N];
+                load_weights<N>(n.w_post, n.wdt, e, n.D, w);
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    d[i] = sum_gate[v][i] * w[i];
+                    sum_post[v][i] += sum_gate[v][i] * gate[v].get(i);
+                }
+                V o;
+                o.set(d);
+                store_row<DT>(static_cast<char*>(n.dgate) + (mine ? q : gate0) * n.D * kSize, e, mine ? n.D : 0, o);
+            }
+        }
+    }
+
+    // the slab's sums, those of its sub-groups of threads added up in their order
+    const auto leave = [&](float* part, const float (&sum)[NV][N]) {
+        if (part == nullptr) return;
+        part += (int64_t)blockIdx.x * n.D;
+        if constexpr (R > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int i = 0; i < N; ++i) lds[sub * kColumns + (v * T + t) * N + i] = sum[v][i];
+            __syncthreads();
+            for (int d = threadIdx.x; d < n.D; d += norm_block<T>()) {
+                float s = 0.0f;
+                for (int g = 0; g < R; ++g) s += lds[g * kColumns + d];
+                part[d] = s;
+            }
+        } else {
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int i = 0; i < N; i += 4) {
+                    RowVec<SDGP_F32> o;
+                    const float f[4] = {sum[v][i], sum[v][i + 1], sum[v][i + 2], sum[v][i + 3]};
+                    o.set(f);
+                    store_row<SDGP_F32>(part, (v * T + t) * N + i, n.D, o);
+                }
+        }
+    };
+    leave(n.part_pre, sum_pre);
+    if constexpr (BLOCK) leave(n.part_post, sum_post);
+}
+
+}  // namespace
+
+template <int DT>
+int norm_rows_launch(const Norm& n, RowShape shape, hipStream_t stream) {
+    const int R = shape.threads < 256 ? 256 / shape.threads : 1;
+    // workgroups that are there at once, about; each keeps the weights in registers over its rows
+    const int64_t most = shape.threads <= 256 ? 2048 : shape.threads == 512 ? 1024 : 512;
+    const int64_t groups = (n.rows + R - 1) / R, per = (groups + most - 1) / most * R;
+    const dim3 grid((unsigned)((n.rows + per - 1) / per)), block(shape.threads < 256 ? 256 : shape.threads);
+#define SDGP_CASE(T, NV)                                                                                              \
+    if (shape.threads == T && shape.vecs == NV) {                                                                     \
+        if (n.u != nullptr) hipLaunchKernelGGL((norm_fwd<DT, T, NV, true>), grid, block, 0, stream, n, per);          \
+        else hipLaunchKernelGGL((norm_fwd<DT, T, NV, false>), grid, block, 0, stream, n, per);                        \
+        return launch_status();                                                                                       \
+    }
+    SDGP_CASE(16, 1) SDGP_CASE(16, 2) SDGP_CASE(64, 1) SDGP_CASE(64, 2) SDGP_CASE(256, 1) SDGP_CASE(256, 2) SDGP_CASE(512, 2) SDGP_CASE(1024, 2)
+#undef SDGP_CASE
+    return SDGP_ERR_SHAPE;
+}
+
+template <int DT>
+int norm_grad_launch(const NormGrad& n, RowShape shape, hipStream_t stream) {
+    const dim3 grid((unsigned)n.slabs.count), block(shape.threads < 256 ? 256 : shape.threads);
+#define SDGP_CASE(T, NV)                                                                                              \
+    if (shape.threads == T && shape.vecs == NV) {                                                                     \
+        if (n.u == nullptr) hipLaunchKernelGGL((norm_bwd<DT, T, NV, kNoBlock>), grid, block, 0, stream, n);           \
+        else if (n.slabs.kind == kInGroup) hipLaunchKernelGGL((norm_bwd<DT, T, NV, kInGroup>), grid, block, 0, stream, n); \
+        else hipLaunchKernelGGL((norm_bwd<DT, T, NV, kWholeGroups>), grid, block, 0, stream, n);                      \
+        return launch_status();                                                                                       \
+    }
+    SDGP_CASE(16, 1) SDGP_CASE(16, 2) SDGP_CASE(64, 1) SDGP_CASE(64, 2) SDGP_CASE(256, 1) SDGP_CASE(256, 2) SDGP_CASE(512, 2) SDGP_CASE(1024, 2)
+#undef SDGP_CASE
+    return SDGP_ERR_SHAPE;
+}
+
+}  // namespace sdgp
