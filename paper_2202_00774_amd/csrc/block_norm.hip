@@ -58,15 +58,15 @@ __global__ void __launch_bounds__(kBlock) norm_long_rows(const Norm n) {
             const float u = load1(n.u, n.dt, base + d);
             sq += u * u;
         }
-        const float ru = 1.0f / sqrtf(block_sum(sq, lds) / n.D + n.eps);
+        const float ru = rsqrtf(block_sum(sq, lds) / n.D + n.eps);
         if (tid == 0) n.stats[r] = ru;
         const int64_t gbase = n.gate ? r / n.per_gate * n.D : 0;
         sq = 0.0f;
         for (int d = tid; d < n.D; d += kBlock) {
-            float v = load1(n.u, n.dt, base + d) * ru;
-            if (n.w_post) v *= load1(n.w_post, n.wdt, d);
-            if (n.gate) v *= load1(n.gate, n.dt, gbase + d);
-            v = store1(n.y, n.dt, base + d, n.residual_scale * load1(n.x, n.dt, base + d) + v);
+            float v = mul_rn(load1(n.u, n.dt, base + d), ru);
+            if (n.w_post) v = mul_rn(v, load1(n.w_post, n.wdt, d));
+            if (n.gate) v = mul_rn(v, load1(n.gate, n.dt, gbase + d));
+            v = store1(n.y, n.dt, base + d, add_rn(mul_rn(n.residual_scale, load1(n.x, n.dt, base + d)), v));
             sq += v * v;
         }
     } else {
@@ -76,7 +76,7 @@ __global__ void __launch_bounds__(kBlock) norm_long_rows(const Norm n) {
         }
     }
     if (!n.h) continue;
-    const float ry = 1.0f / sqrtf(block_sum(sq, lds) / n.D + n.eps);
+    const float ry = rsqrtf(block_sum(sq, lds) / n.D + n.eps);
     if (tid == 0) n.stats[n.rows + r] = ry;
     for (int d = tid; d < n.D; d += kBlock) {
         float v = load1(y, n.dt, base + d) * ry;      // what this thread stored itself
@@ -171,61 +171,57 @@ __global__ void __launch_bounds__(kBlock) norm_grad_columns(const NormGrad n, co
 // dgate, and the gates' sums times the gate to dw_post.  Fixed order throughout.
 constexpr int kCols = 32, kDown = 32;
 
-__device__ __forceinline__ float add_down(float v, float (*lds)[kCols + 1]) {
+// Sum of v over `over` threads down a column (a power of two; threads k * over .. k * over + over - 1), in the first of them.
+__device__ __forceinline__ float add_down(float v, int over, float (*lds)[kCols + 1]) {
     const int col = threadIdx.x % kCols, down = threadIdx.x / kCols;
     __syncthreads();
     lds[down][col] = v;
-    __syncthreads();
-    for (int o = kDown / 2; o > 0; o /= 2) {
-        if (down < o) lds[down][col] += lds[down + o][col];
+    for (int o = over / 2; o > 0; o /= 2) {
         __syncthreads();
+        if ((down & (over - 1)) < o) lds[down][col] += lds[down + o][col];
     }
-    return lds[0][col];
+    __syncthreads();
+    return lds[down][col];
 }
 
 __device__ __forceinline__ float add_slabs(const float* part, int D, int64_t first, int64_t end, int64_t step, int d) {
-    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    float s[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
     int64_t i = first;
-    for (; i + 3 * step < end; i += 4 * step)
+    for (; i + 7 * step < end; i += 8 * step)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) s[k] += part[(i + k * step) * D + d];
+        for (int k = 0; k < 8; ++k) s[k] += part[(i + k * step) * D + d];
     for (; i < end; i += step) s[0] += part[i * D + d];
-    return (s[0] + s[1]) + (s[2] + s[3]);
+    return ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
 }
 
+// blockIdx.y: 0 for dw_pre, 1 for dw_post and dgate.
 __global__ void __launch_bounds__(kCols* kDown) norm_grad_finish(const NormGrad n) {
     __shared__ float lds[kDown][kCols + 1];
     const int d = blockIdx.x * kCols + threadIdx.x % kCols, down = threadIdx.x / kCols;
     const bool in = d < n.D;
-    if (n.part_pre) {
-        const float s = add_down(in ? add_slabs(n.part_pre, n.D, down, n.slabs.count, kDown, d) : 0.0f, lds);
-        if (in && down == 0) n.dw_pre[d] = s;
-    }
-    if (!n.part_post) return;
-    float post = 0.0f;
-    if (n.slabs.kind == kWholeGroups || !n.gate) {
-        post = add_down(in ? add_slabs(n.part_post, n.D, down, n.slabs.count, kDown, d) : 0.0f, lds);
+    const float* part = blockIdx.y == 0 ? n.part_pre : n.part_post;
+    float* dw = blockIdx.y == 0 ? n.dw_pre : n.dw_post;
+    if (part == nullptr) return;
+    float sum = 0.0f;
+    if (blockIdx.y == 0 || n.slabs.kind == kWholeGroups || n.gate == nullptr) {
+        if (in) sum = add_slabs(part, n.D, down, n.slabs.count, kDown, d);
     } else {
+        // each gate's slabs by as many threads as there are for each (at least one), then the gates
+        int over = kDown;
+        while (over > 1 && over * n.groups > kDown) over /= 2;
+        const int64_t at_once = kDown / over, parts = n.slabs.parts;
         const float w = in ? weight(n.w_post, n.wdt, d) : 0.0f;
-        const int64_t parts = n.slabs.parts;
-        if (parts >= kDown) {          // many slabs a gate: all threads of a column on one gate
-            for (int64_t g = 0; g < n.groups; ++g) {
-                const float s = add_down(in ? add_slabs(n.part_post, n.D, g * parts + down, (g + 1) * parts, kDown, d) : 0.0f, lds);
-                if (!in || down != 0) continue;
-                store1(n.dgate, n.dt, g * n.D + d, s * w);
-                post += s * load1(n.gate, n.dt, g * n.D + d);
-            }
-        } else {                       // few: a gate a thread
-            if (in)
-                for (int64_t g = down; g < n.groups; g += kDown) {
-                    const float s = add_slabs(n.part_post, n.D, g * parts, (g + 1) * parts, 1, d);
-                    store1(n.dgate, n.dt, g * n.D + d, s * w);
-                    post += s * load1(n.gate, n.dt, g * n.D + d);
-                }
-            post = add_down(post, lds);
+        for (int64_t g0 = 0; g0 < n.groups; g0 += at_once) {
+            const int64_t g = g0 + down / over;
+            const bool mine = in && g < n.groups;
+            const float s = add_down(mine ? add_slabs(part, n.D, g * parts + (down & (over - 1)), (g + 1) * parts, over, d) : 0.0f, over, lds);
+            if (!mine || (down & (over - 1)) != 0) continue;
+            store1(n.dgate, n.dt, g * n.D + d, s * w);
+            sum += s * load1(n.gate, n.dt, g * n.D + d);
         }
     }
-    if (in && down == 0 && n.dw_post) n.dw_post[d] = post;
+    sum = add_down(sum, kDown, lds);
+    if (in && down == 0 && dw != nullptr) dw[d] = sum;
 }
 
 __global__ void __launch_bounds__(kBlock) clear_words(uint16_t* __restrict__ p, int64_t n) {
@@ -250,15 +246,16 @@ int block_norm_bwd_no_rows(void* dgate, int64_t gate_elements, int dt, float* dw
     return SDGP_OK;
 }
 
-// A slab costs its columns' sums written and read again, so it holds eight rows for each that a workgroup has in hand,
-// unless that leaves fewer than 256 workgroups, one a CU; more than 1024 hide no more latency.  Gates of up to 32 rows
+// A slab costs its columns' sums written and read again, so it holds four rows for each that a workgroup has in hand,
+// unless that leaves fewer than 256 workgroups, one a CU; more than 1024 hide no more latency (4099 x 1001 fp32: 76 us
+// with eight rows each, 63 with four).  Gates of up to 32 rows
 // that are many (2048) are finished by the slab that holds them.
 static Slabs make_slabs(int64_t rows, int64_t D, int64_t groups, int dt) {
     const RowShape shape = row_shape(D, dt);
     const int64_t at_once = shape.threads == 0 || shape.threads >= 256 ? 1 : 256 / shape.threads;
     const int64_t g = groups > 0 ? groups : 1, per_gate = rows / g;
     Slabs s;
-    int64_t want = rows / (8 * at_once);
+    int64_t want = rows / (4 * at_once);
     want = want < 256 ? 256 : want > 1024 ? 1024 : want;
     if (groups > 0 && (per_gate == 1 || (per_gate <= 32 && groups >= 2048))) {
         s.kind = kWholeGroups;
@@ -285,7 +282,8 @@ size_t block_norm_bwd_workspace(int64_t rows, int64_t D, int64_t groups, int dt)
 int block_norm_launch(const void* x, const void* u, const void* gate, const void* w_post, const void* w_pre, void* y, void* h,
                       float* stats, int64_t rows, int64_t D, int64_t groups, int dt, int wdt, float residual_scale, float eps,
                       hipStream_t stream) {
-    const Norm n = {x, u, gate, w_post, w_pre, y, h, stats, rows, groups > 0 ? rows / groups : rows, (int)D, dt, wdt, residual_scale, eps};
+    const Norm n = {x, u, gate, w_post, w_pre, y, h, stats, rows, groups > 0 ? rows / groups : rows, (int)D, dt, wdt, residual_scale, eps,
+                    rows_aligned(D, dt, {x, u, gate}), rows_large(rows, D, dt)};
     const RowShape shape = row_shape(D, dt);
     if (shape.threads > 0)
         return dt == SDGP_BF16 ? norm_rows_launch<SDGP_BF16>(n, shape, stream) : norm_rows_launch<SDGP_F32>(n, shape, stream);
@@ -302,7 +300,8 @@ int block_norm_bwd_launch(const void* dy, const void* dh, const void* y, const v
     const int64_t each = slabs.count * D;
     const bool post = w_post != nullptr || (gate != nullptr && slabs.kind == kInGroup);
     const NormGrad n = {dy, dh, y, u, gate, w_post, w_pre, stats, dx, du, dgate, dw_post, dw_pre, w_pre ? sums : nullptr,
-                        post ? sums + each : nullptr, rows, groups, groups > 0 ? rows / groups : rows, slabs, (int)D, dt, wdt, residual_scale};
+                        post ? sums + each : nullptr, rows, groups, groups > 0 ? rows / groups : rows, slabs, (int)D, dt, wdt, residual_scale,
+                        rows_aligned(D, dt, {dy, dh, y, u}), rows_large(rows, D, dt)};
     const RowShape shape = row_shape(D, dt);
     int rc;
     if (shape.threads > 0) {
@@ -318,7 +317,7 @@ int block_norm_bwd_launch(const void* dy, const void* dh, const void* y, const v
         }
     }
     if (rc != SDGP_OK || (!n.part_pre && !n.part_post)) return rc;
-    hipLaunchKernelGGL(norm_grad_finish, dim3((unsigned)((D + kCols - 1) / kCols)), dim3(kCols * kDown), 0, stream, n);
+    hipLaunchKernelGGL(norm_grad_finish, dim3((unsigned)((D + kCols - 1) / kCols), 2), dim3(kCols * kDown), 0, stream, n);
     return launch_status();
 }
 

@@ -22,15 +22,16 @@ __global__ void __launch_bounds__(norm_block<T>()) norm_fwd(const Norm n, int64_
     using V = RowVec<DT>;
     constexpr int N = V::kN, R = norm_block<T>() / T;
     constexpr int64_t kSize = sizeof(typename V::Elem);
-    __shared__ float lds[T > 64 ? 2 * (T / 64) : 1];
+    __shared__ float lds[row_lds<T, 1>()];
     int turn = 0;
     const int t = threadIdx.x % T, sub = threadIdx.x / T;
-    const int64_t first = (int64_t)blockIdx.x * rows_per_wg;
-    const int64_t end = first + rows_per_wg < n.rows ? first + rows_per_wg : n.rows;
+    // rows in turn, or a run of them
+    const int64_t first = (int64_t)blockIdx.x * (n.large ? R : rows_per_wg), step = n.large ? (int64_t)gridDim.x * R : R;
+    const int64_t end = n.large || first + rows_per_wg > n.rows ? n.rows : first + rows_per_wg;
     const float inv_d = 1.0f / (float)n.D;
 
     float post[NV][N], pre[NV][N];
-    const bool one_gate = BLOCK && n.gate != nullptr && n.per_gate == n.rows;
+    V gate[NV];
     const bool many_gates = BLOCK && n.gate != nullptr && n.per_gate != n.rows;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
@@ -38,33 +39,32 @@ __global__ void __launch_bounds__(norm_block<T>()) norm_fwd(const Norm n, int64_
         load_weights<N>(n.w_pre, n.wdt, e, n.D, pre[v]);
         if constexpr (BLOCK) {
             load_weights<N>(n.w_post, n.wdt, e, n.D, post[v]);
-            if (one_gate) {
-                const V g = load_row<DT>(n.gate, e, n.D);
-#pragma unroll
-                for (int i = 0; i < N; ++i) post[v][i] *= g.get(i);
-            }
+            if (n.gate != nullptr) gate[v] = load_row<DT>(n.gate, e, n.D);
         }
     }
 
-    for (int64_t r0 = first; r0 < end; r0 += R) {
+    for (int64_t r0 = first; r0 < end; r0 += step) {
         const int64_t r = r0 + sub;
         const bool live = r < end;
         const int D = live ? n.D : 0;
         const int64_t at = (live ? r : first) * n.D * kSize;
         V x[NV], u[NV];
+        const auto load = [&](auto caching) {
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int e = (v * T + t) * N;
-            x[v] = load_row<DT>(static_cast<const char*>(n.x) + at, e, D);
-            if constexpr (BLOCK) u[v] = load_row<DT>(static_cast<const char*>(n.u) + at, e, D);
-        }
+            for (int v = 0; v < NV; ++v) {
+                const int e = (v * T + t) * N;
+                x[v] = load_row<DT, decltype(caching)::value>(static_cast<const char*>(n.x) + at, e, D);
+                if constexpr (BLOCK) u[v] = load_row<DT, decltype(caching)::value>(static_cast<const char*>(n.u) + at, e, D);
+            }
+        };
+        if (n.aligned) load(Cached<kStream>{});
+        else load(Cached<kKeep>{});
         float sum[1];
         if constexpr (BLOCK) {
-            V g[NV];
             if (many_gates) {
                 const int64_t gat = (live ? r : first) / n.per_gate * n.D * kSize;
 #pragma unroll
-                for (int v = 0; v < NV; ++v) g[v] = load_row<DT>(static_cast<const char*>(n.gate) + gat, (v * T + t) * N, D);
+                for (int v = 0; v < NV; ++v) gate[v] = load_row<DT>(static_cast<const char*>(n.gate) + gat, (v * T + t) * N, D);
             }
             sum[0] = 0.0f;
 #pragma unroll
@@ -72,19 +72,21 @@ __global__ void __launch_bounds__(norm_block<T>()) norm_fwd(const Norm n, int64_
 #pragma unroll
                 for (int i = 0; i < N; ++i) sum[0] += u[v].get(i) * u[v].get(i);
             row_sums<T, 1>(sum, lds, turn);
-            const float ru = 1.0f / sqrtf(sum[0] * inv_d + n.eps);
+            const float ru = rsqrtf(sum[0] * inv_d + n.eps);
             if (t == 0 && live) n.stats[r] = ru;
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
                 float y[N];
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    float a = u[v].get(i) * ru * post[v][i];
-                    if (many_gates) a *= g[v].get(i);
-                    y[i] = n.residual_scale * x[v].get(i) + a;
+                    // in the formula's order, one rounding each: y is rounded again as it is stored, and all that follows
+                    // is computed from that
+                    float a = mul_rn(mul_rn(u[v].get(i), ru), post[v][i]);
+                    if (n.gate != nullptr) a = mul_rn(gate[v].get(i), a);
+                    y[i] = add_rn(mul_rn(n.residual_scale, x[v].get(i)), a);
                 }
                 x[v].set(y);   // y from here on, rounded as it is stored
-                store_row<DT>(static_cast<char*>(n.y) + at, (v * T + t) * N, D, x[v]);
+                store_row<DT>(static_cast<char*>(n.y) + at, (v * T + t) * N, D, x[v], n.large);
             }
             if (n.h == nullptr) continue;
         }
@@ -94,7 +96,7 @@ __global__ void __launch_bounds__(norm_block<T>()) norm_fwd(const Norm n, int64_
 #pragma unroll
             for (int i = 0; i < N; ++i) sum[0] += x[v].get(i) * x[v].get(i);
         row_sums<T, 1>(sum, lds, turn);
-        const float ry = 1.0f / sqrtf(sum[0] * inv_d + n.eps);
+        const float ry = rsqrtf(sum[0] * inv_d + n.eps);
         if (t == 0 && live) n.stats[n.rows + r] = ry;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
@@ -103,9 +105,40 @@ __global__ void __launch_bounds__(norm_block<T>()) norm_fwd(const Norm n, int64_
             for (int i = 0; i < N; ++i) h[i] = x[v].get(i) * ry * pre[v][i];
             V q;
             q.set(h);
-            store_row<DT>(static_cast<char*>(n.h) + at, (v * T + t) * N, D, q);
+            store_row<DT>(static_cast<char*>(n.h) + at, (v * T + t) * N, D, q, n.large);
         }
     }
+}
+
+// What the gradient of one row reads.
+template <int DT, int NV>
+struct Row {
+    RowVec<DT> y[NV], u[NV], dy[NV], dh[NV];
+    float ry, ru;
+};
+
+template <Caching CACHING, int T, bool BLOCK, int DT, int NV>
+__device__ __forceinline__ void load_as(Row<DT, NV>& row, const NormGrad& n, int64_t r, int64_t end, int t) {
+    constexpr int N = RowVec<DT>::kN;
+    const bool live = r < end;
+    const int D = live ? n.D : 0, Dh = n.dh != nullptr ? D : 0;
+    const int64_t at = live ? r * n.D * (int64_t)sizeof(typename RowVec<DT>::Elem) : 0;
+    row.ry = Dh > 0 ? n.stats[n.rows + r] : 0.0f;
+    row.ru = BLOCK && live ? n.stats[r] : 0.0f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        const int e = (v * T + t) * N;
+        row.y[v] = load_row<DT, CACHING>(static_cast<const char*>(n.y) + at, e, Dh);
+        row.dh[v] = load_row<DT, CACHING>(static_cast<const char*>(n.dh) + at, e, Dh);
+        row.dy[v] = load_row<DT, CACHING>(static_cast<const char*>(n.dy) + at, e, n.dy != nullptr ? D : 0);
+        if constexpr (BLOCK) row.u[v] = load_row<DT, CACHING>(static_cast<const char*>(n.u) + at, e, D);
+    }
+}
+
+template <int T, bool BLOCK, int DT, int NV>
+__device__ __forceinline__ void load(Row<DT, NV>& row, const NormGrad& n, int64_t r, int64_t end, int t) {
+    if (n.aligned) load_as<kStream, T, BLOCK>(row, n, r, end, t);
+    else load_as<kKeep, T, BLOCK>(row, n, r, end, t);
 }
 
 // MODE: kNoBlock, or how the slab is cut.
@@ -117,78 +150,89 @@ __global__ void __launch_bounds__(norm_block<T>()) norm_bwd(const NormGrad n) {
     constexpr int N = V::kN, R = norm_block<T>() / T, kColumns = T * NV * N;
     constexpr bool BLOCK = MODE != kNoBlock;
     constexpr int64_t kSize = sizeof(typename V::Elem);
-    __shared__ float lds[R > 1 ? R * kColumns : T > 64 ? 2 * 3 * (T / 64) : 1];
+    __shared__ float lds[R > 1 ? R * kColumns : row_lds<T, 3>()];
     int turn = 0;
     const int t = threadIdx.x % T, sub = threadIdx.x / T;
     const float inv_d = 1.0f / (float)n.D;
 
-    float w_pre[NV][N], k[NV][N];           // k: gate * w_post, or w_post while the gate changes
+    // Weights stay in registers, k = gate * w_post with them; but with two vectors a thread, of 1024 with 128 registers
+    // each, they are read again for every row (in registers they spilled 300).  The next row is not asked for ahead of its
+    // turn: that takes 25 registers, and a third or fourth wavefront a SIMD hides more (16384 x 2048: 134 us, without 124).
+    constexpr bool kHeld = NV == 1;
+    float w_pre[NV][N], k[NV][N];
     float sum_pre[NV][N], sum_post[NV][N];  // dh t, and dY a (kInGroup) or dY gate a (kWholeGroups)
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-        load_weights<N>(n.w_pre, n.wdt, (v * T + t) * N, n.D, w_pre[v]);
+        if constexpr (kHeld) load_weights<N>(n.w_pre, n.wdt, (v * T + t) * N, n.D, w_pre[v]);
 #pragma unroll
-        for (int i = 0; i < N; ++i) sum_pre[v][i] = 0.0f, sum_post[v][i] = 0.0f, k[v][i] = 0.0f;
+        for (int i = 0; i < N; ++i) sum_pre[v][i] = 0.0f, sum_post[v][i] = 0.0f;
     }
 
     // the gates of this slab: one (kInGroup), or `len` of them, each sub-group of threads taking its own
     const int64_t gate0 = MODE == kWholeGroups ? (int64_t)blockIdx.x * n.slabs.len : (int64_t)blockIdx.x / n.slabs.parts;
     const int64_t gate1 = MODE != kWholeGroups ? gate0 + 1 : gate0 + n.slabs.len < n.groups ? gate0 + n.slabs.len : n.groups;
-    const int64_t step = MODE == kWholeGroups ? R : 1;
-    for (int64_t q0 = gate0; q0 < gate1; q0 += step) {
+    for (int64_t q0 = gate0; q0 < gate1; q0 += MODE == kWholeGroups ? R : 1) {
         const int64_t q = MODE == kWholeGroups ? q0 + sub : q0;
         const bool mine = q < gate1;
-        V gate[NV];
+        const char* gate_row = static_cast<const char*>(n.gate) + (mine ? q : gate0) * n.D * kSize;
+        const auto gated = [&](int e, float (&kv)[N]) {
+            load_weights<N>(n.w_post, n.wdt, e, n.D, kv);
+            if (n.gate == nullptr) return;
+            const V g = load_row<DT>(gate_row, e, n.D);
+#pragma unroll
+            for (int i = 0; i < N; ++i) kv[i] *= g.get(i);
+        };
         float sum_gate[NV][N];
         if constexpr (BLOCK) {
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
-                const int e = (v * T + t) * N;
-                load_weights<N>(n.w_post, n.wdt, e, n.D, k[v]);
-                if (n.gate != nullptr) {
-                    gate[v] = load_row<DT>(static_cast<const char*>(n.gate) + (mine ? q : gate0) * n.D * kSize, e, n.D);
-#pragma unroll
-                    for (int i = 0; i < N; ++i) k[v][i] *= gate[v].get(i);
-                }
+                if constexpr (kHeld) gated((v * T + t) * N, k[v]);
 #pragma unroll
                 for (int i = 0; i < N; ++i) sum_gate[v][i] = 0.0f;
             }
         }
+        const auto weights = [&](int v, float (&wv)[N], float (&kv)[N]) {
+            if constexpr (kHeld) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) wv[i] = w_pre[v][i], kv[i] = BLOCK ? k[v][i] : 0.0f;
+            } else {
+                int e = (v * T + t) * N;
+                asm volatile("" : "+v"(e));   // in every row anew, not once in front of them
+                load_weights<N>(n.w_pre, n.wdt, e, n.D, wv);
+                if constexpr (BLOCK) gated(e, kv);
+            }
+        };
         int64_t first = q * n.per_gate, end = first + n.per_gate;
         if constexpr (MODE != kWholeGroups) {
-            first += (int64_t)(blockIdx.x - gate0 * n.slabs.parts) * n.slabs.len;
-            if (first + n.slabs.len < end) end = first + n.slabs.len;
+            first += (int64_t)(blockIdx.x - gate0 * n.slabs.parts) * (n.large ? R : n.slabs.len);
+            if (!n.large && first + n.slabs.len < end) end = first + n.slabs.len;
         }
         const int64_t rows = MODE == kWholeGroups ? n.per_gate : end - first;   // the same for all threads
-        for (int64_t i0 = 0; i0 < rows; i0 += MODE == kWholeGroups ? 1 : R) {
+        const int64_t step = MODE == kWholeGroups ? 1 : n.large ? R * n.slabs.parts : R;
+        for (int64_t i0 = 0; i0 < rows; i0 += step) {
             const int64_t r = first + i0 + (MODE == kWholeGroups ? 0 : sub);
-            const bool live = mine && r < end;
-            const int D = live ? n.D : 0;
-            const int64_t at = live ? r * n.D * kSize : 0;
-            V y[NV], u[NV], dy[NV], dh[NV];
-            const float ry = live && n.dh != nullptr ? n.stats[n.rows + r] : 0.0f;
-            const float ru = BLOCK && live ? n.stats[r] : 0.0f;
-#pragma unroll
-            for (int v = 0; v < NV; ++v) {
-                const int e = (v * T + t) * N;
-                y[v] = load_row<DT>(static_cast<const char*>(n.y) + at, e, n.dh != nullptr ? D : 0);
-                dh[v] = load_row<DT>(static_cast<const char*>(n.dh) + at, e, n.dh != nullptr ? D : 0);
-                dy[v] = load_row<DT>(static_cast<const char*>(n.dy) + at, e, n.dy != nullptr ? D : 0);
-                if constexpr (BLOCK) u[v] = load_row<DT>(static_cast<const char*>(n.u) + at, e, D);
-            }
+            const int D = mine && r < end ? n.D : 0;
+            const int64_t at = D > 0 ? r * n.D * kSize : 0;
+            Row<DT, NV> row;
+            load<T, BLOCK>(row, n, r, mine ? end : 0, t);
+            const auto &y = row.y, &u = row.u, &dy = row.dy, &dh = row.dh;
+            const float ry = row.ry, ru = row.ru;
             float s[3] = {0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int v = 0; v < NV; ++v)
+            for (int v = 0; v < NV; ++v) {
+                float wv[N], kv[N];
+                weights(v, wv, kv);
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    const float dn = dh[v].get(i) * w_pre[v][i], tt = y[v].get(i) * ry;
+                    const float dn = dh[v].get(i) * wv[i], tt = y[v].get(i) * ry;
                     s[0] += dn * tt;
                     if constexpr (BLOCK) {
-                        const float ka = k[v][i] * (u[v].get(i) * ru);
+                        const float ka = kv[i] * (u[v].get(i) * ru);
                         s[1] += ka * (dy[v].get(i) + ry * dn);
                         s[2] += ka * tt;
                     }
                 }
+            }
             if constexpr (BLOCK) {
                 row_sums<T, 3>(s, lds, turn);
             } else {
@@ -201,27 +245,28 @@ __global__ void __launch_bounds__(norm_block<T>()) norm_bwd(const NormGrad n) {
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
                 const int e = (v * T + t) * N;
-                float dx[N], du[N];
+                float dx[N], du[N], wv[N], kv[N];
+                weights(v, wv, kv);
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
                     const float g = dh[v].get(i), tt = y[v].get(i) * ry;
-                    const float dY = dy[v].get(i) + ry * (g * w_pre[v][i]) - c * tt;
+                    const float dY = dy[v].get(i) + ry * (g * wv[i]) - c * tt;
                     sum_pre[v][i] += g * tt;
                     dx[i] = dY;
                     if constexpr (BLOCK) {
                         const float a = u[v].get(i) * ru, da = dY * a;
                         dx[i] = n.residual_scale * dY;
-                        du[i] = ru * (dY * k[v][i] - a * mean_a);
+                        du[i] = ru * (dY * kv[i] - a * mean_a);
                         if constexpr (MODE == kWholeGroups) sum_gate[v][i] += da;
                         else sum_post[v][i] += da;
                     }
                 }
                 V o;
                 o.set(dx);
-                store_row<DT>(static_cast<char*>(n.dx) + at, e, D, o);
+                store_row<DT>(static_cast<char*>(n.dx) + at, e, D, o, n.large);
                 if constexpr (BLOCK) {
                     o.set(du);
-                    store_row<DT>(static_cast<char*>(n.du) + at, e, D, o);
+                    store_row<DT>(static_cast<char*>(n.du) + at, e, D, o, n.large);
                 }
             }
         }
@@ -231,10 +276,11 @@ __global__ void __launch_bounds__(norm_block<T>()) norm_bwd(const NormGrad n) {
                 const int e = (v * T + t) * N;
                 float w[N], d[N];
                 load_weights<N>(n.w_post, n.wdt, e, n.D, w);
+                const V g = load_row<DT>(gate_row, e, n.D);
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
                     d[i] = sum_gate[v][i] * w[i];
-                    sum_post[v][i] += sum_gate[v][i] * gate[v].get(i);
+                    sum_post[v][i] += sum_gate[v][i] * g.get(i);
                 }
                 V o;
                 o.set(d);
@@ -290,7 +336,7 @@ int norm_rows_launch(const Norm& n, RowShape shape, hipStream_t stream) {
         else hipLaunchKernelGGL((norm_fwd<DT, T, NV, false>), grid, block, 0, stream, n, per);                        \
         return launch_status();                                                                                       \
     }
-    SDGP_CASE(16, 1) SDGP_CASE(16, 2) SDGP_CASE(64, 1) SDGP_CASE(64, 2) SDGP_CASE(256, 1) SDGP_CASE(256, 2) SDGP_CASE(512, 2) SDGP_CASE(1024, 2)
+    SDGP_CASE(16, 1) SDGP_CASE(32, 1) SDGP_CASE(64, 1) SDGP_CASE(128, 1) SDGP_CASE(256, 1) SDGP_CASE(512, 1) SDGP_CASE(1024, 1) SDGP_CASE(1024, 2)
 #undef SDGP_CASE
     return SDGP_ERR_SHAPE;
 }
@@ -305,7 +351,7 @@ int norm_grad_launch(const NormGrad& n, RowShape shape, hipStream_t stream) {
         else hipLaunchKernelGGL((norm_bwd<DT, T, NV, kWholeGroups>), grid, block, 0, stream, n);                      \
         return launch_status();                                                                                       \
     }
-    SDGP_CASE(16, 1) SDGP_CASE(16, 2) SDGP_CASE(64, 1) SDGP_CASE(64, 2) SDGP_CASE(256, 1) SDGP_CASE(256, 2) SDGP_CASE(512, 2) SDGP_CASE(1024, 2)
+    SDGP_CASE(16, 1) SDGP_CASE(32, 1) SDGP_CASE(64, 1) SDGP_CASE(128, 1) SDGP_CASE(256, 1) SDGP_CASE(512, 1) SDGP_CASE(1024, 1) SDGP_CASE(1024, 2)
 #undef SDGP_CASE
     return SDGP_ERR_SHAPE;
 }

@@ -2,6 +2,8 @@
 // share a row.
 #pragma once
 
+#include <type_traits>
+
 #include "common.h"
 
 namespace sdgp {
@@ -35,13 +37,19 @@ struct RowVec<SDGP_BF16> {
     }
 };
 
+typedef uint32_t u32x4_half_aligned __attribute__((ext_vector_type(4), aligned(2), may_alias));
+typedef uint32_t u32x4_word_aligned __attribute__((ext_vector_type(4), aligned(4), may_alias));
+
 template <int DT>
-struct __attribute__((packed, aligned(DT == SDGP_BF16 ? 2 : 4), may_alias)) Unaligned16 {
-    uint32_t w[4];
-};
+using Unaligned16 = typename std::conditional<DT == SDGP_BF16, u32x4_half_aligned, u32x4_word_aligned>::type;
+
+// kStream: the line is not needed again soon (a hint to the caches).
+enum Caching { kKeep, kStream };
+template <Caching C>
+using Cached = std::integral_constant<Caching, C>;
 
 // Elements [e, e + kN) of a row of `n`; what lies outside is 0 and is not read.
-template <int DT>
+template <int DT, Caching CACHING = kKeep>
 __device__ __forceinline__ RowVec<DT> load_row(const void* row, int e, int n, uint32_t fill = 0u) {
     constexpr int N = RowVec<DT>::kN;
     union {
@@ -51,9 +59,10 @@ __device__ __forceinline__ RowVec<DT> load_row(const void* row, int e, int n, ui
     } u;
     const auto* p = static_cast<const typename RowVec<DT>::Elem*>(row) + e;
     if (e + N <= n) {
-        const auto q = *reinterpret_cast<const Unaligned16<DT>*>(p);
+        const auto* at = reinterpret_cast<const Unaligned16<DT>*>(p);
+        const auto q = CACHING == kStream ? __builtin_nontemporal_load(at) : *at;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) u.w[i] = q.w[i];
+        for (int i = 0; i < 4; ++i) u.w[i] = q[i];
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) u.w[i] = fill;
@@ -65,7 +74,7 @@ __device__ __forceinline__ RowVec<DT> load_row(const void* row, int e, int n, ui
 }
 
 template <int DT>
-__device__ __forceinline__ void store_row(void* row, int e, int n, const RowVec<DT>& r) {
+__device__ __forceinline__ void store_row(void* row, int e, int n, const RowVec<DT>& r, bool stream = false) {
     constexpr int N = RowVec<DT>::kN;
     union {
         RowVec<DT> r;
@@ -77,8 +86,10 @@ __device__ __forceinline__ void store_row(void* row, int e, int n, const RowVec<
     if (e + N <= n) {
         Unaligned16<DT> q;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) q.w[i] = u.w[i];
-        *reinterpret_cast<Unaligned16<DT>*>(p) = q;
+        for (int i = 0; i < 4; ++i) q[i] = u.w[i];
+        auto* at = reinterpret_cast<Unaligned16<DT>*>(p);
+        if (stream) __builtin_nontemporal_store(q, at);
+        else *at = q;
     } else {
 #pragma unroll
         for (int i = 0; i < N - 1; ++i)
@@ -109,6 +120,17 @@ __device__ __forceinline__ void load_weights(const void* w, int dt, int e, int n
     }
 }
 
+// Product and sum with a rounding each, never fused into one operation: where a result's last bit decides a later
+// rounding, it should not depend on what the compiler fused.
+__device__ __forceinline__ float mul_rn(float a, float b) {
+#pragma clang fp contract(off)
+    return a * b;
+}
+__device__ __forceinline__ float add_rn(float a, float b) {
+#pragma clang fp contract(off)
+    return a + b;
+}
+
 template <int CTRL>
 __device__ __forceinline__ float lane_swap(float v) {
     return bits_to_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)float_to_bits(v), CTRL, 0xF, 0xF, true));
@@ -132,30 +154,41 @@ __device__ __forceinline__ float sum64(float v) {
     return (lane_value(v, 0) + lane_value(v, 16)) + (lane_value(v, 32) + lane_value(v, 48));
 }
 
-// Sums of K values over the T threads that share a row, the same for all of them.  T = 16 and 64 stay inside a
-// wavefront; above that the wavefronts meet in `lds`, [2][K][T / 64], which the calls take in turn (`turn` flips), so one
-// barrier a call is enough: a wavefront can be at most one call ahead of another.
+__device__ __forceinline__ float sum32(float v) {
+    v = sum16(v);
+    return v + bits_to_float((uint32_t)__builtin_amdgcn_ds_swizzle((int)float_to_bits(v), 0x401F));   // the lane 16 away
+}
+
+// Sums of K values over the T threads that share a row, the same for all of them.  Up to 64 stay inside a wavefront;
+// above that the wavefronts meet in `lds` (row_lds floats), which the calls take in turn (`turn` flips), so one
+// barrier a call is enough: a wavefront can be at most one call ahead of another.  All threads of the workgroup call it.
+template <int T, int K>
+constexpr int row_lds() { return T > 64 ? 2 * K * (T < 256 ? 4 : T / 64) : 1; }
+
 template <int T, int K>
 __device__ __forceinline__ void row_sums(float (&v)[K], float* lds, int& turn) {
     if constexpr (T == 16) {
 #pragma unroll
         for (int k = 0; k < K; ++k) v[k] = sum16(v[k]);
+    } else if constexpr (T == 32) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) v[k] = sum32(v[k]);
     } else {
 #pragma unroll
         for (int k = 0; k < K; ++k) v[k] = sum64(v[k]);
         if constexpr (T > 64) {
-            constexpr int W = T / 64;
-            float* at = lds + turn * (K * W);
+            constexpr int W = T / 64, kAll = row_lds<T, K>() / (2 * K);   // wavefronts a row, a workgroup
+            float* at = lds + turn * (K * kAll);
             if ((threadIdx.x & 63) == 0) {
 #pragma unroll
-                for (int k = 0; k < K; ++k) at[k * W + threadIdx.x / 64] = v[k];
+                for (int k = 0; k < K; ++k) at[k * kAll + threadIdx.x / 64] = v[k];
             }
             __syncthreads();
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 float s = 0.0f;
 #pragma unroll
-                for (int w = 0; w < W; ++w) s += at[k * W + w];
+                for (int w = 0; w < W; ++w) s += at[k * kAll + threadIdx.x / T * W + w];
                 v[k] = s;
             }
             turn ^= 1;

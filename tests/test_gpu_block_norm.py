@@ -267,3 +267,31 @@ def test_another_stream():
     side.synchronize()
     for p, q in zip((*want, *grads), (*got, *more)):
         assert torch.equal(p, q)
+
+
+@pytest.mark.parametrize("dtype,rows,D,gate", [(torch.bfloat16, 36000, 2048, 1), (torch.float32, 9001, 4097, 1), (torch.bfloat16, 18000, 4096, 4)])
+def test_tensors_larger_than_the_caches(dtype, rows, D, gate):
+    """More than 128 MB a tensor: written and cut differently.  Every row is its own problem, so a part of the rows gives
+    the same bits; the sums over rows are the parts' sums, to (rows) e of the sum of sizes each side."""
+    t = make(rows, D, dtype, gate, D)
+    assert rows * D * t["x"].element_size() > 128 << 20
+    y, h, stats = sdgp.sdgp_block_norm(t["x"], t["u"], t["gate"], t["w_post"], t["w_pre"])
+    dx, du, dgate, dw_post, dw_pre = sdgp.sdgp_block_norm_bwd(t["dy"], t["dh"], y, stats, t["u"], t["gate"], t["w_post"], t["w_pre"])
+    per = rows // gate
+    post, pre, sizes = 0.0, 0.0, 0.0
+    for g in range(gate):
+        gates = []
+        for cut in (slice(g * per, g * per + per // 2), slice(g * per + per // 2, (g + 1) * per)):
+            p = {k: v[cut] for k, v in t.items() if k in ("x", "u", "dy", "dh")}
+            one = t["gate"][g].contiguous()
+            py, ph, ps = sdgp.sdgp_block_norm(p["x"], p["u"], one, t["w_post"], t["w_pre"])
+            assert torch.equal(py, y[cut]) and torch.equal(ph, h[cut]) and torch.equal(ps, stats[:, cut])
+            pdx, pdu, pg, p_post, p_pre = sdgp.sdgp_block_norm_bwd(p["dy"], p["dh"], py, ps, p["u"], one, t["w_post"], t["w_pre"])
+            assert torch.equal(pdx, dx[cut]) and torch.equal(pdu, du[cut])
+            gates.append(f64(pg))
+            post, pre = post + f64(p_post), pre + f64(p_pre)
+            sizes = sizes + f64((p["dh"].float().abs() * 6 + p["dy"].float().abs()).sum(0)) * 12
+        store = 2.0 ** -7 if dtype == torch.bfloat16 else 2 * E
+        near(dgate.view(gate, D)[g], gates[0] + gates[1], 2 * E * per * sizes + store * (np.abs(gates[0]) + np.abs(gates[1])), "dgate")
+    near(dw_post, post, 2 * E * rows * sizes, "dw_post")
+    near(dw_pre, pre, 2 * E * rows * sizes, "dw_pre")
