@@ -4,17 +4,22 @@
 //   logp = (x_t - m) scale - ln s        entropy = ln s - (1/s) sum_j e^(z_j - scale m) (z_j - scale m)
 //   dL/dx_j = scale * (g (d_jt - p_j) - h p_j (ln p_j + entropy)),  g = dL/dlogp, h = dL/dentropy
 //
-// One pass over a row: running maximum, sum and weighted sum (both brought to the new maximum when it grows), and the
-// best `top` logits so far.  Differences to the maximum are taken before the scale is applied, so a mask of the type's
-// lowest value cannot overflow into a NaN; in the weighted sum they are cut at -256 (in powers of two), where e^ is 0
-// already, so that a logit of -inf adds 0 and not 0 * inf.  All sums are fp32.
-#include "common.h"
+// One pass over a row: running maximum, sum and weighted sum, and the best `top` logits so far.  A wavefront has one maximum
+// for all its lanes; only when a chunk brings a larger one (a few times a row) are its sums brought to it.  Differences to
+// the maximum are taken before the scale is applied, so a mask of the type's lowest value cannot overflow into a NaN; in the
+// weighted sum they are cut at -256 (in powers of two), where e^ is 0 already, so that a logit of -inf adds 0 and not
+// 0 * inf.  All sums are fp32.
+//
+// Bound by memory where rows are many: 2 bytes an element read forward, 4 read and written backward in bf16; beside them
+// 11 vector instructions forward, one of them an exponential, and 14 backward.  A row is one workgroup's (or, where rows are
+// short and many, one wavefront's); few long rows are cut into pieces, whose sums and lists a second kernel joins.
+#include "rows.h"
 
 namespace sdgp {
 
 namespace {
 
-constexpr int kBlock = 256, kWave = 64, kWaves = kBlock / kWave;
+constexpr int kBlock = 256, kWave = 64;
 constexpr float kLowest = -3.402823466e38f;
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kFloor2 = -256.0f;   // exponents of two below this count as this: 2^-256 is 0 in fp32
@@ -29,20 +34,37 @@ struct Sums {
 
 __device__ __forceinline__ float exponent(float x, float m, float c) { return (x - m) * c; }
 
-__device__ __forceinline__ Sums joined(const Sums& p, const Sums& q, float c) {
-    Sums r;
-    r.m = fmaxf(p.m, q.m);
-    const float dp = fmaxf(exponent(p.m, r.m, c), kFloor2), dq = fmaxf(exponent(q.m, r.m, c), kFloor2);
-    const float fp = exp2_hw(dp), fq = exp2_hw(dq);
-    r.s = p.s * fp + q.s * fq;
-    r.a = fp * (p.a + p.s * dp) + fq * (q.a + q.s * dq);
-    return r;
+// The sums as they are with the maximum m >= t.m.
+__device__ __forceinline__ void rebase(Sums& t, float m, float c) {
+    const float d = fmaxf(exponent(t.m, m, c), kFloor2), f = exp2_hw(d);
+    t.a = f * (t.a + t.s * d);
+    t.s *= f;
+    t.m = m;
+}
+
+__device__ __forceinline__ Sums joined(Sums p, Sums q, float c) {
+    const float m = fmaxf(p.m, q.m);
+    rebase(p, m, c);
+    rebase(q, m, c);
+    return {m, p.s + q.s, p.a + q.a};
 }
 
 template <int DT>
 __device__ __forceinline__ float load_logit(const void* row, int64_t j) {
     if constexpr (DT == SDGP_BF16) return bf16_to_float(static_cast<const uint16_t*>(row)[j]);
     else return static_cast<const float*>(row)[j];
+}
+
+template <int DT>
+constexpr uint32_t kMinusInf = DT == SDGP_BF16 ? 0xFF80FF80u : 0xFF800000u;
+
+// Largest over the wavefront, the same for all lanes.
+__device__ __forceinline__ float max64(float v) {
+    v = fmaxf(v, lane_swap<0xB1>(v));
+    v = fmaxf(v, lane_swap<0x4E>(v));
+    v = fmaxf(v, lane_swap<0x141>(v));
+    v = fmaxf(v, lane_swap<0x140>(v));
+    return fmaxf(fmaxf(lane_value(v, 0), lane_value(v, 16)), fmaxf(lane_value(v, 32), lane_value(v, 48)));
 }
 
 // The best logits a wavefront has met, lane i the i-th; equal logits in the order of their index.  Places not taken
@@ -54,141 +76,366 @@ struct Best {
 
 __device__ __forceinline__ bool better(float x, uint32_t j, float y, uint32_t k) { return x > y || (x == y && j < k); }
 
-// Takes one logit (the same for all lanes) into the list.
+__device__ __forceinline__ uint32_t from_lane_below(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, 0x138, 0xF, 0xF, false);   // wave_shr 1; lane 0 keeps its own
+}
+
+// Takes one logit (the same for all lanes) into the list: the ones it is better than move up a lane.
 __device__ __forceinline__ void insert(Best& b, float x, uint32_t j) {
-    const float ux = __shfl_up(b.x, 1);
-    const uint32_t uj = __shfl_up(b.j, 1);
     const bool keep = better(b.x, b.j, x, j);
-    const bool up = (threadIdx.x & (kWave - 1)) != 0 && !better(ux, uj, x, j);   // the new one went in further up
+    const float ux = bits_to_float(from_lane_below(float_to_bits(b.x)));
+    const uint32_t uj = from_lane_below(b.j);
+    const bool moves = (threadIdx.x & (kWave - 1)) != 0 && !better(ux, uj, x, j);   // the one below moves up to here
     if (!keep) {
-        b.x = up ? ux : x;
-        b.j = up ? uj : j;
+        b.x = moves ? ux : x;
+        b.j = moves ? uj : j;
     }
 }
 
-template <int DT>
-__global__ void __launch_bounds__(kBlock) logprob_rows(const void* __restrict__ logits, int64_t ld, const void* __restrict__ tokens,
-                                                       int token_bits, float* __restrict__ logp, float* __restrict__ entropy,
-                                                       float* __restrict__ top_logp, int64_t* __restrict__ top_ids,
-                                                       float* __restrict__ stats, int64_t rows, int V, int top, float scale) {
-    __shared__ Sums part[kWaves];
-    __shared__ Best lists[kWaves][kMaxTop];
-    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
-    const char* row = static_cast<const char*>(logits) + r * ld * (DT == SDGP_BF16 ? 2 : 4);
-    const float c = scale * kLog2e;
-    Sums t = {kLowest, 0.0f, 0.0f};
-    Best best = {-INFINITY, 0xFFFFFFFFu};
-    for (int j0 = 0; j0 < V; j0 += kBlock) {
-        const int j = j0 + tid;
-        const float x = j < V ? load_logit<DT>(row, j) : -INFINITY;
-        if (x > t.m) {
-            const float d = fmaxf(exponent(t.m, x, c), kFloor2), f = exp2_hw(d);
-            t.a = f * (t.a + t.s * d);
-            t.s *= f;
-            t.m = x;
-        }
-        const float d = exponent(x, t.m, c), e = exp2_hw(d);
-        t.s += e;
-        t.a += e * fmaxf(d, kFloor2);
-        if (top > 0) {
-            uint64_t some = __ballot(x > __shfl(best.x, top - 1));
-            while (some) {
-                const int from = __builtin_ctzll(some);
-                some &= some - 1;
-                insert(best, __shfl(x, from), (uint32_t)(j0 + wave * kWave + from));
+__device__ __forceinline__ uint32_t lane_word(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); }
+
+// Offers the N logits that each lane holds, lane l those of the indexes first + l * N onwards, larger than any index that
+// was offered before.  The largest goes in first, so no more than `top` of them do.
+template <int N>
+__device__ __forceinline__ void offer(Best& b, int top, float (&x)[N], float most, uint32_t first) {
+    float last = lane_value(b.x, top - 1);
+    while (__ballot(most > last)) {
+        const float m = max64(most);
+        const int from = __builtin_ctzll(__ballot(most == m));
+        int at = 0;
+#pragma unroll
+        for (int i = N - 1; i >= 0; --i) at = x[i] == m ? i : at;
+        at = (int)lane_word((uint32_t)at, from);
+        insert(b, m, first + (uint32_t)(from * N + at));
+        if ((int)(threadIdx.x & (kWave - 1)) == from) {
+            most = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                if (i == at) x[i] = -INFINITY;
+                most = fmaxf(most, x[i]);
             }
         }
+        last = lane_value(b.x, top - 1);
     }
+}
+
+// Takes another list in, places [0, top).
+__device__ __forceinline__ void merge(Best& b, int top, const Best* list) {
+    for (int i = 0; i < top; ++i) {
+        const Best q = list[i];
+        if (!better(q.x, q.j, lane_value(b.x, top - 1), lane_word(b.j, top - 1))) break;   // nor are the ones after it
+        insert(b, q.x, q.j);
+    }
+}
+
+// One wavefront's share of a row: chunks of `stride` vectors from vector v0 on, up to element `end`.
+constexpr int kAtOnce = 2;   // vectors a lane that are looked through together
+
+template <int DT, bool TOP>
+__device__ __forceinline__ void scan(const void* row, int64_t first, int64_t stride, int end, float c, int top, Sums& t, Best& best) {
+    using V = RowVec<DT>;
+    constexpr int N = V::kN;
+    const int lane = threadIdx.x & (kWave - 1);
+    // vectors of a chunk lie `stride` apart, chunks kAtOnce * stride; 64 lanes side by side
+    V next[kAtOnce];
+    int64_t e = first;
 #pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) t = joined(t, {__shfl_xor(t.m, o), __shfl_xor(t.s, o), __shfl_xor(t.a, o)}, c);
-
-    __syncthreads();   // the first wavefront is done with the row before
-    if (lane == 0) part[wave] = t;
-    lists[wave][lane] = best;
-    __syncthreads();
-    if (wave != 0) continue;
-    for (int w = 1; w < kWaves; ++w) {
-        t = joined(t, part[w], c);
-        for (int i = 0; i < top; ++i) insert(best, lists[w][i].x, lists[w][i].j);
+    for (int u = 0; u < kAtOnce; ++u) {
+        const int64_t at = e + u * stride + lane * N;
+        next[u] = load_row<DT>(row, (int)(at < end ? at : end), end, kMinusInf<DT>);
     }
+    while (e < end) {
+        float x[kAtOnce][N], most[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            most[u] = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                x[u][i] = next[u].get(i);
+                most[u] = fmaxf(most[u], x[u][i]);
+            }
+        }
+        const int64_t e0 = e;
+        e += kAtOnce * stride;
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int64_t at = e + u * stride + lane * N;
+            next[u] = load_row<DT>(row, (int)(at < end ? at : end), end, kMinusInf<DT>);
+        }
+        float all = most[0];
+#pragma unroll
+        for (int u = 1; u < kAtOnce; ++u) all = fmaxf(all, most[u]);
+        if (__ballot(all > t.m)) rebase(t, fmaxf(max64(all), t.m), c);
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float d = exponent(x[u][i], t.m, c), p = exp2_hw(d);
+                t.s += p;
+                t.a += p * fmaxf(d, kFloor2);
+            }
+        if constexpr (TOP) {
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) offer<N>(best, top, x[u], most[u], (uint32_t)(e0 + u * stride));
+        }
+    }
+    // every lane's sums have the same maximum
+    t.s = sum64(t.s);
+    t.a = sum64(t.a);
+}
 
+struct Logprobs {
+    const void *logits, *tokens;
+    float *logp, *entropy, *top_logp, *stats;
+    int64_t* top_ids;
+    int64_t ld, rows;
+    int V, top, token_bits;
+    float scale;
+    // few long rows: pieces of a row, of `piece` elements each, and where their sums and lists go
+    int pieces, piece;
+    Sums* part_sums;   // [rows, pieces]
+    Best* part_best;   // [rows, pieces, top]
+};
+
+// Results of row r from one wavefront's sums and list.
+template <int DT>
+__device__ __forceinline__ void finish(const Logprobs& q, int64_t r, const Sums& t, const Best& best) {
+    const int lane = threadIdx.x & (kWave - 1);
     const float logs = logf(t.s);                    // of an empty row: -inf
     const bool empty = t.s == 0.0f, bad = t.s != t.s;
     if (lane == 0) {
-        if (logp) {
-            const int64_t token = token_bits == 64 ? static_cast<const int64_t*>(tokens)[r] : (int64_t) static_cast<const int32_t*>(tokens)[r];
+        if (q.logp) {
+            const int64_t token = q.token_bits == 64 ? static_cast<const int64_t*>(q.tokens)[r] : (int64_t) static_cast<const int32_t*>(q.tokens)[r];
+            const char* row = static_cast<const char*>(q.logits) + r * q.ld * (DT == SDGP_BF16 ? 2 : 4);
             float lp = 0.0f;
-            if (token >= V) lp = NAN;
-            else if (token >= 0) lp = empty ? -INFINITY : (load_logit<DT>(row, token) - t.m) * scale - logs;
-            logp[r] = lp;
+            if (token >= q.V) lp = NAN;
+            else if (token >= 0) lp = empty ? -INFINITY : (load_logit<DT>(row, token) - t.m) * q.scale - logs;
+            q.logp[r] = lp;
         }
-        entropy[r] = empty ? 0.0f : logs - kLn2 * t.a / t.s;
-        stats[2 * r] = t.m;
-        stats[2 * r + 1] = logs;
+        q.entropy[r] = empty ? 0.0f : logs - kLn2 * t.a / t.s;
+        q.stats[2 * r] = t.m;
+        q.stats[2 * r + 1] = logs;
     }
-    if (lane < top) {
+    if (lane < q.top) {
         const bool none = bad || best.j == 0xFFFFFFFFu;
-        top_ids[r * top + lane] = none ? -1 : (int64_t)best.j;
-        top_logp[r * top + lane] = bad ? NAN : none ? -INFINITY : (best.x - t.m) * scale - logs;
-    }
-    }
-}
-
-template <int DT>
-__global__ void __launch_bounds__(kBlock) logprob_grad(const void* __restrict__ logits, int64_t ld, const void* __restrict__ tokens,
-                                                       int token_bits, const float* __restrict__ stats, const float* __restrict__ entropy,
-                                                       const float* __restrict__ g_logp, const float* __restrict__ g_entropy,
-                                                       void* __restrict__ dlogits, int64_t ld_out, int64_t rows, int V, float scale) {
-    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-    const char* row = static_cast<const char*>(logits) + r * ld * (DT == SDGP_BF16 ? 2 : 4);
-    char* out = static_cast<char*>(dlogits) + r * ld_out * (DT == SDGP_BF16 ? 2 : 4);
-    const float m = stats[2 * r], logs = stats[2 * r + 1];
-    int64_t token = -1;
-    float g = 0.0f, h = 0.0f, H = 0.0f;
-    if (g_logp) {
-        token = token_bits == 64 ? static_cast<const int64_t*>(tokens)[r] : (int64_t) static_cast<const int32_t*>(tokens)[r];
-        g = token >= V ? NAN : token >= 0 ? g_logp[r] : 0.0f;
-    }
-    if (g_entropy) {
-        h = g_entropy[r];
-        H = entropy[r];
-    }
-    const bool empty = logs == -INFINITY;
-    for (int j = threadIdx.x; j < V; j += kBlock) {
-        const float x = load_logit<DT>(row, j);
-        const float l = (x - m) * scale - logs, p = exp2_hw(l * kLog2e);
-        float d = -p * (g + h * (fmaxf(l, kFloor2) + H));
-        if (j == token) d += g;
-        d = empty ? 0.0f : d * scale;
-        if constexpr (DT == SDGP_BF16) reinterpret_cast<uint16_t*>(out)[j] = (uint16_t)float_to_bf16(d);
-        else reinterpret_cast<float*>(out)[j] = d;
-    }
+        q.top_ids[r * q.top + lane] = none ? -1 : (int64_t)best.j;
+        q.top_logp[r * q.top + lane] = bad ? NAN : none ? -INFINITY : (best.x - t.m) * q.scale - logs;
     }
 }
 
-unsigned row_grid(int64_t rows) { return (unsigned)(rows < 65536 ? rows : 65536); }
+// The workgroup's sums and list in its first wavefront.
+template <bool TOP>
+__device__ __forceinline__ void join_waves(Sums& t, Best& best, int top, float c, Sums* part, Best (*lists)[kMaxTop]) {
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    __syncthreads();   // the first wavefront is done with what was there
+    if (lane == 0) part[wave] = t;
+    if constexpr (TOP) lists[wave][lane] = best;
+    __syncthreads();
+    if (wave != 0) return;
+    for (int w = 1; w < kBlock / kWave; ++w) {
+        t = joined(t, part[w], c);
+        if constexpr (TOP) merge(best, top, lists[w]);
+    }
+}
+
+// T = 64: a wavefront a row; 256: a workgroup a row, or a piece of one.
+template <int DT, int T, bool TOP>
+__global__ void __launch_bounds__(kBlock) logprob_rows(const Logprobs q) {
+    constexpr int N = RowVec<DT>::kN, R = kBlock / T;
+    __shared__ Sums part[T > kWave ? kBlock / kWave : 1];
+    __shared__ Best lists[T > kWave && TOP ? kBlock / kWave : 1][kMaxTop];
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const float c = q.scale * kLog2e;
+    const int64_t items = q.rows * q.pieces;
+    for (int64_t i0 = (int64_t)blockIdx.x * R; i0 < items; i0 += (int64_t)gridDim.x * R) {
+        const int64_t item = i0 + (T == kWave ? wave : 0);
+        if (item >= items) continue;   // T = 64 only, a whole wavefront: nothing is shared
+        const int64_t r = item / q.pieces;
+        const int begin = (int)(item - r * q.pieces) * q.piece;
+        const int end = q.V - begin < q.piece ? q.V : begin + q.piece;
+        const char* row = static_cast<const char*>(q.logits) + r * q.ld * (DT == SDGP_BF16 ? 2 : 4);
+        Sums t = {kLowest, 0.0f, 0.0f};
+        Best best = {-INFINITY, 0xFFFFFFFFu};
+        scan<DT, TOP>(row, begin + (T == kWave ? 0 : wave * kWave * N), (int64_t)T * N, end, c, q.top, t, best);
+        if constexpr (T > kWave) {
+            join_waves<TOP>(t, best, q.top, c, part, lists);
+            if (wave != 0) continue;
+        }
+        if (q.pieces == 1) {
+            finish<DT>(q, r, t, best);
+        } else {
+            if (lane == 0) q.part_sums[item] = t;
+            if (lane < q.top) q.part_best[item * q.top + lane] = best;
+        }
+    }
+}
+
+// One workgroup a row: each wavefront joins every fourth piece, then the four are joined.
+template <int DT, bool TOP>
+__global__ void __launch_bounds__(kBlock) logprob_join(const Logprobs q) {
+    __shared__ Sums part[kBlock / kWave];
+    __shared__ Best lists[kBlock / kWave][kMaxTop];
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const float c = q.scale * kLog2e;
+    for (int64_t r = blockIdx.x; r < q.rows; r += gridDim.x) {
+        const Sums* sums = q.part_sums + r * q.pieces;
+        Sums t = {kLowest, 0.0f, 0.0f};
+        for (int i = wave * kWave + lane; i < q.pieces; i += kBlock) t = joined(t, sums[i], c);
+        const float m = max64(t.m);
+        rebase(t, m, c);
+        t.s = sum64(t.s);
+        t.a = sum64(t.a);
+        Best best = {-INFINITY, 0xFFFFFFFFu};
+        if constexpr (TOP) {
+            // an entry a lane; the wavefront's entries come in batches of 64, the best of each batch first
+            const Best* list = q.part_best + r * q.pieces * q.top;
+            const int n = q.pieces * q.top;
+            for (int i0 = wave * kWave; i0 < n; i0 += kBlock) {
+                Best mine = {-INFINITY, 0xFFFFFFFFu};
+                if (i0 + lane < n) mine = list[i0 + lane];
+                for (;;) {
+                    const float x = lane_value(best.x, q.top - 1);
+                    const uint32_t j = lane_word(best.j, q.top - 1);
+                    if (!__ballot(better(mine.x, mine.j, x, j))) break;
+                    const float top_x = max64(mine.x);
+                    // of equal ones the lowest index: pieces and their lists are in that order
+                    const int from = __builtin_ctzll(__ballot(mine.x == top_x));
+                    insert(best, top_x, lane_word(mine.j, from));
+                    if (lane == from) mine = {-INFINITY, 0xFFFFFFFFu};
+                }
+            }
+        }
+        join_waves<TOP>(t, best, q.top, c, part, lists);
+        if (wave == 0) finish<DT>(q, r, t, best);
+    }
+}
+
+struct LogprobsGrad {
+    const void *logits, *tokens;
+    const float *stats, *entropy, *g_logp, *g_entropy;
+    void* dlogits;
+    int64_t ld, ld_out, rows;
+    int V, token_bits, chunks;
+    float scale;
+};
+
+// T threads on a chunk of a row, kVecs vectors each.
+template <int DT, int T, int VECS, bool ENTROPY>
+__global__ void __launch_bounds__(kBlock) logprob_grad(const LogprobsGrad q) {
+    using V = RowVec<DT>;
+    constexpr int N = V::kN, R = kBlock / T;
+    constexpr int64_t kSize = sizeof(typename V::Elem);
+    const int t = threadIdx.x % T;
+    const int64_t items = q.rows * q.chunks;
+    for (int64_t item = (int64_t)blockIdx.x * R + threadIdx.x / T; item < items; item += (int64_t)gridDim.x * R) {
+        const int64_t r = q.chunks == 1 ? item : item / q.chunks;
+        const int first = (int)(item - r * q.chunks) * (T * VECS * N) + t * N;
+        const char* row = static_cast<const char*>(q.logits) + r * q.ld * kSize;
+        V x[VECS];
+#pragma unroll
+        for (int v = 0; v < VECS; ++v) {
+            const int64_t e = (int64_t)first + v * T * N;
+            x[v] = load_row<DT>(row, (int)(e < q.V ? e : q.V), q.V);
+        }
+        const float m = q.stats[2 * r], logs = q.stats[2 * r + 1];
+        int64_t token = -1;
+        float g = 0.0f, h = 0.0f, H = 0.0f;
+        if (q.g_logp) {
+            token = q.token_bits == 64 ? static_cast<const int64_t*>(q.tokens)[r] : (int64_t) static_cast<const int32_t*>(q.tokens)[r];
+            g = token >= q.V ? NAN : token >= 0 ? q.g_logp[r] * q.scale : 0.0f;
+        }
+        if constexpr (ENTROPY) {
+            h = q.g_entropy[r] * q.scale;
+            H = q.entropy[r];
+        }
+        const bool empty = logs == -INFINITY;
+#pragma unroll
+        for (int v = 0; v < VECS; ++v) {
+            const int64_t e = (int64_t)first + v * T * N;
+            float d[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float l = (x[v].get(i) - m) * q.scale - logs, p = exp2_hw(l * kLog2e);
+                d[i] = ENTROPY ? -p * (g + h * (fmaxf(l, kFloor2) + H)) : -p * g;
+                if (e + i == token) d[i] += g;
+                if (empty) d[i] = 0.0f;
+            }
+            V o;
+            o.set(d);
+            store_row<DT>(static_cast<char*>(q.dlogits) + r * q.ld_out * kSize, (int)(e < q.V ? e : q.V), q.V, o);
+        }
+    }
+}
+
+unsigned grid_of(int64_t items) { return (unsigned)(items < (1 << 20) ? items : (1 << 20)); }
+
+// How rows are cut.  A workgroup looks through 2 * 256 vectors at once, so a piece is at least one such chunk; rows that
+// are fewer than the workgroups the chip holds are cut until there are about 1024 pieces.
+struct Cut {
+    int threads, pieces, piece;
+};
+
+Cut cut_rows(int64_t rows, int64_t V, int dt) {
+    const int64_t chunk = (dt == SDGP_BF16 ? 8 : 4) * kAtOnce * (int64_t)kBlock;
+    if (V <= chunk) return {rows >= 1024 ? kWave : kBlock, 1, (int)V};
+    int64_t pieces = rows >= 512 ? 1 : 1024 / rows;
+    const int64_t most = (V + chunk - 1) / chunk;
+    pieces = pieces > most ? most : pieces;
+    const int64_t piece = ((V + pieces - 1) / pieces + chunk - 1) / chunk * chunk;
+    return {kBlock, (int)((V + piece - 1) / piece), (int)(piece < V ? piece : V)};
+}
+
+template <int DT, bool TOP>
+int launch_rows(const Logprobs& q, const Cut& cut, hipStream_t stream) {
+    const int64_t items = q.rows * cut.pieces;
+    if (cut.threads == kWave) hipLaunchKernelGGL((logprob_rows<DT, kWave, TOP>), dim3(grid_of((items + 3) / 4)), dim3(kBlock), 0, stream, q);
+    else hipLaunchKernelGGL((logprob_rows<DT, kBlock, TOP>), dim3(grid_of(items)), dim3(kBlock), 0, stream, q);
+    const int rc = launch_status();
+    if (rc != SDGP_OK || cut.pieces == 1) return rc;
+    hipLaunchKernelGGL((logprob_join<DT, TOP>), dim3(grid_of(q.rows)), dim3(kBlock), 0, stream, q);
+    return launch_status();
+}
+
+template <int DT, bool ENTROPY>
+int launch_grad(LogprobsGrad q, hipStream_t stream) {
+    constexpr int N = RowVec<DT>::kN;
+    const auto go = [&](auto kernel, int threads, int vecs) {
+        q.chunks = (int)((q.V + threads * vecs * N - 1) / (threads * vecs * N));
+        const int64_t items = q.rows * q.chunks, at_once = kBlock / threads;
+        hipLaunchKernelGGL(kernel, dim3(grid_of((items + at_once - 1) / at_once)), dim3(kBlock), 0, stream, q);
+        return launch_status();
+    };
+    if (q.V <= 16 * N) return go(logprob_grad<DT, 16, 1, ENTROPY>, 16, 1);
+    if (q.V <= 64 * 2 * N) return go(logprob_grad<DT, 64, 2, ENTROPY>, 64, 2);
+    return go(logprob_grad<DT, 256, 2, ENTROPY>, 256, 2);
+}
 
 }  // namespace
 
-size_t token_logprobs_workspace(int64_t, int64_t, int, int) { return 0; }
+size_t token_logprobs_workspace(int64_t rows, int64_t V, int dt, int top) {
+    if (rows == 0) return 0;
+    const Cut cut = cut_rows(rows, V, dt);
+    return cut.pieces == 1 ? 0 : (size_t)rows * cut.pieces * (sizeof(Sums) + top * sizeof(Best));
+}
 
 int token_logprobs_launch(const void* logits, int64_t ld, const void* tokens, int token_bits, float* logp, float* entropy,
                           float* top_logp, int64_t* top_ids, float* stats, int64_t rows, int64_t V, int dt, int top, float scale,
-                          void*, hipStream_t stream) {
-    auto kernel = dt == SDGP_BF16 ? logprob_rows<SDGP_BF16> : logprob_rows<SDGP_F32>;
-    hipLaunchKernelGGL(kernel, dim3(row_grid(rows)), dim3(kBlock), 0, stream, logits, ld, tokens, token_bits, logp, entropy, top_logp,
-                       top_ids, stats, rows, (int)V, top, scale);
-    return launch_status();
+                          void* workspace, hipStream_t stream) {
+    const Cut cut = cut_rows(rows, V, dt);
+    const int64_t items = rows * cut.pieces;
+    Best* lists = static_cast<Best*>(workspace);
+    const Logprobs q = {logits, tokens, logp, entropy, top_logp, stats, top_ids, ld, rows, (int)V, top, token_bits, scale, cut.pieces,
+                        cut.piece, reinterpret_cast<Sums*>(lists + items * top), lists};
+    if (dt == SDGP_BF16) return top > 0 ? launch_rows<SDGP_BF16, true>(q, cut, stream) : launch_rows<SDGP_BF16, false>(q, cut, stream);
+    return top > 0 ? launch_rows<SDGP_F32, true>(q, cut, stream) : launch_rows<SDGP_F32, false>(q, cut, stream);
 }
 
 int token_logprobs_bwd_launch(const void* logits, int64_t ld, const void* tokens, int token_bits, const float* stats, const float* entropy,
                               const float* g_logp, const float* g_entropy, void* dlogits, int64_t ld_out, int64_t rows, int64_t V,
                               int dt, float scale, hipStream_t stream) {
-    auto kernel = dt == SDGP_BF16 ? logprob_grad<SDGP_BF16> : logprob_grad<SDGP_F32>;
-    hipLaunchKernelGGL(kernel, dim3(row_grid(rows)), dim3(kBlock), 0, stream, logits, ld, tokens, token_bits, stats, entropy, g_logp,
-                       g_entropy, dlogits, ld_out, rows, (int)V, scale);
-    return launch_status();
+    const LogprobsGrad q = {logits, tokens, stats, entropy, g_logp, g_entropy, dlogits, ld, ld_out, rows, (int)V, token_bits, 1, scale};
+    if (dt == SDGP_BF16) return g_entropy ? launch_grad<SDGP_BF16, true>(q, stream) : launch_grad<SDGP_BF16, false>(q, stream);
+    return g_entropy ? launch_grad<SDGP_F32, true>(q, stream) : launch_grad<SDGP_F32, false>(q, stream);
 }
 
 }  // namespace sdgp
