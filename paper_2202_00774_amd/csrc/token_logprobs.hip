@@ -94,90 +94,185 @@ __device__ __forceinline__ void insert(Best& b, float x, uint32_t j) {
 
 __device__ __forceinline__ uint32_t lane_word(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); }
 
+// The value of lane (own ^ X).
+template <int X>
+__device__ __forceinline__ uint32_t lane_xor(uint32_t v) {
+    constexpr int kDpp = X == 1 ? 0xB1 : X == 2 ? 0x4E : X == 3 ? 0x1B : X == 7 ? 0x141 : X == 15 ? 0x140 : X == 8 ? 0x128 : 0;
+    if constexpr (kDpp != 0) return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, kDpp, 0xF, 0xF, true);
+    else if constexpr (X < 32) return (uint32_t)__builtin_amdgcn_ds_swizzle((int)v, 0x1F | (X << 10));
+    else return (uint32_t)__shfl_xor((int)v, X);
+}
+
+// Of each pair of lanes l, l ^ X the lower one keeps the better logit.
+template <int X>
+__device__ __forceinline__ void exchange(Best& b) {
+    constexpr int kTop = X >= 32 ? 32 : X >= 16 ? 16 : X >= 8 ? 8 : X >= 4 ? 4 : X >= 2 ? 2 : 1;   // set in the upper of a pair
+    const Best o = {bits_to_float(lane_xor<X>(float_to_bits(b.x))), lane_xor<X>(b.j)};
+    const bool lower = (threadIdx.x & kTop) == 0;
+    if (better(o.x, o.j, b.x, b.j) == lower) b = o;   // equal pairs (two empty places) may swap: they are alike
+}
+
+// Sorts one logit a lane, the best first.
+__device__ __forceinline__ void sort(Best& b) {
+    exchange<1>(b);
+    exchange<3>(b), exchange<1>(b);
+    exchange<7>(b), exchange<2>(b), exchange<1>(b);
+    exchange<15>(b), exchange<4>(b), exchange<2>(b), exchange<1>(b);
+    exchange<31>(b), exchange<8>(b), exchange<4>(b), exchange<2>(b), exchange<1>(b);
+    exchange<63>(b), exchange<16>(b), exchange<8>(b), exchange<4>(b), exchange<2>(b), exchange<1>(b);
+}
+
+// The 64 best of two sorted lists, the second one given from its end: of each pair the better one, then put in order.
+__device__ __forceinline__ void merge_reversed(Best& b, const Best& end_first) {
+    if (better(end_first.x, end_first.j, b.x, b.j)) b = end_first;
+    exchange<32>(b), exchange<16>(b), exchange<8>(b), exchange<4>(b), exchange<2>(b), exchange<1>(b);
+}
+
+// Takes in one logit a lane, in any order.
+__device__ __forceinline__ void merge_unsorted(Best& b, Best o) {
+    sort(o);
+    merge_reversed(b, {bits_to_float(lane_xor<63>(float_to_bits(o.x))), lane_xor<63>(o.j)});
+}
+
+// What the wavefronts of a row tell each other: how good a logit must at least be.  A row's `top` best are no worse than
+// any one wavefront's last, and no worse than the worst of the wavefronts' (top / 4)-th, since these are `top` logits
+// together.  Written and read without a barrier: whatever a reader meets was a lower bound when it was written, and is one.
+struct Bounds {
+    volatile float least, share[kBlock / kWave];
+
+    __device__ __forceinline__ void tell(int wave, float last, float own_share) {
+        share[wave] = own_share;
+        const float all = fminf(fminf(share[0], share[1]), fminf(share[2], share[3]));
+        least = fmaxf(least, fmaxf(last, all));
+    }
+};
+
+constexpr int kOneByOne = 4;   // up to so many lanes with new ones, they go in one by one (25 instructions each); else a
+                               // lane's best each together (190)
+
 // Offers the N logits that each lane holds, lane l those of the indexes first + l * N onwards, larger than any index that
-// was offered before.  The largest goes in first, so no more than `top` of them do.
+// was offered before; `bound`: what is less is not among the best.  A logit like the last in the list is no better than
+// it, its index being larger; but among those offered here it may be, so the list's end is compared with its index.
 template <int N>
-__device__ __forceinline__ void offer(Best& b, int top, float (&x)[N], float most, uint32_t first) {
-    float last = lane_value(b.x, top - 1);
-    while (__ballot(most > last)) {
-        const float m = max64(most);
-        const int from = __builtin_ctzll(__ballot(most == m));
-        int at = 0;
+__device__ __forceinline__ void offer(Best& b, int top, float bound, float (&x)[N], float most, uint32_t first) {
+    if (!__ballot(most > lane_value(b.x, top - 1) && most >= bound)) return;
+    const int lane = threadIdx.x & (kWave - 1);
+    const uint32_t j0 = first + (uint32_t)(lane * N);
+    for (;;) {
+        uint32_t j = 0xFFFFFFFFu;   // a lane's best: the first of equal ones
 #pragma unroll
-        for (int i = N - 1; i >= 0; --i) at = x[i] == m ? i : at;
-        at = (int)lane_word((uint32_t)at, from);
-        insert(b, m, first + (uint32_t)(from * N + at));
-        if ((int)(threadIdx.x & (kWave - 1)) == from) {
+        for (int i = N - 1; i >= 0; --i) j = x[i] == most ? j0 + i : j;
+        const bool mine = most > -INFINITY && most >= bound && better(most, j, lane_value(b.x, top - 1), lane_word(b.j, top - 1));
+        const uint64_t who = __ballot(mine);
+        if (!who) return;
+        if (__builtin_popcountll(who) <= kOneByOne) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                uint64_t some = __ballot(mine && x[i] >= lane_value(b.x, top - 1) && x[i] >= bound && x[i] > -INFINITY);
+                while (some) {
+                    const int from = __builtin_ctzll(some);
+                    some &= some - 1;
+                    insert(b, lane_value(x[i], from), first + (uint32_t)(from * N + i));
+                }
+            }
+            return;
+        }
+        merge_unsorted(b, {mine ? most : -INFINITY, mine ? j : 0xFFFFFFFFu});
+        if (mine) {
             most = -INFINITY;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                if (i == at) x[i] = -INFINITY;
+                if (j0 + i == j) x[i] = -INFINITY;
                 most = fmaxf(most, x[i]);
             }
         }
-        last = lane_value(b.x, top - 1);
     }
 }
 
-// Takes another list in, places [0, top).
-__device__ __forceinline__ void merge(Best& b, int top, const Best* list) {
-    for (int i = 0; i < top; ++i) {
-        const Best q = list[i];
-        if (!better(q.x, q.j, lane_value(b.x, top - 1), lane_word(b.j, top - 1))) break;   // nor are the ones after it
-        insert(b, q.x, q.j);
-    }
-}
+// One wavefront's share of a row, up to element `end`: 64 vectors side by side from element `first` on, kAtOnce of them
+// `stride` elements apart in a chunk.  Whole chunks come first, the next one always on its way, then the row's end.
+constexpr int kAtOnce = 2;
 
-// One wavefront's share of a row: chunks of `stride` vectors from vector v0 on, up to element `end`.
-constexpr int kAtOnce = 2;   // vectors a lane that are looked through together
-
-template <int DT, bool TOP>
-__device__ __forceinline__ void scan(const void* row, int64_t first, int64_t stride, int end, float c, int top, Sums& t, Best& best) {
-    using V = RowVec<DT>;
-    constexpr int N = V::kN;
-    const int lane = threadIdx.x & (kWave - 1);
-    // vectors of a chunk lie `stride` apart, chunks kAtOnce * stride; 64 lanes side by side
-    V next[kAtOnce];
-    int64_t e = first;
-#pragma unroll
-    for (int u = 0; u < kAtOnce; ++u) {
-        const int64_t at = e + u * stride + lane * N;
-        next[u] = load_row<DT>(row, (int)(at < end ? at : end), end, kMinusInf<DT>);
-    }
-    while (e < end) {
-        float x[kAtOnce][N], most[kAtOnce];
-#pragma unroll
-        for (int u = 0; u < kAtOnce; ++u) {
-            most[u] = -INFINITY;
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                x[u][i] = next[u].get(i);
-                most[u] = fmaxf(most[u], x[u][i]);
-            }
-        }
-        const int64_t e0 = e;
-        e += kAtOnce * stride;
-#pragma unroll
-        for (int u = 0; u < kAtOnce; ++u) {
-            const int64_t at = e + u * stride + lane * N;
-            next[u] = load_row<DT>(row, (int)(at < end ? at : end), end, kMinusInf<DT>);
-        }
-        float all = most[0];
-#pragma unroll
-        for (int u = 1; u < kAtOnce; ++u) all = fmaxf(all, most[u]);
-        if (__ballot(all > t.m)) rebase(t, fmaxf(max64(all), t.m), c);
+// Adds a chunk to the sums.  Without a floor under the exponents a masked logit makes the weighted sum a NaN (0 * inf): then
+// the chunk is added again with the floor, and so are the row's later chunks (`careful`).
+template <int N>
+__device__ __forceinline__ void add_chunk(Sums& t, const float (&x)[kAtOnce][N], float c, bool& careful) {
+    float s[2] = {0.0f, 0.0f}, a[2] = {0.0f, 0.0f};   // two chains each
+    const auto add = [&](auto floor) {
 #pragma unroll
         for (int u = 0; u < kAtOnce; ++u)
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const float d = exponent(x[u][i], t.m, c), p = exp2_hw(d);
-                t.s += p;
-                t.a += p * fmaxf(d, kFloor2);
+                s[i & 1] += p;
+                a[i & 1] = fmaf(p, decltype(floor)::value ? fmaxf(d, kFloor2) : d, a[i & 1]);
             }
-        if constexpr (TOP) {
+    };
+    if (!careful) {
+        add(std::false_type{});
+        careful = __ballot(a[0] + a[1] != a[0] + a[1]) != 0;
+        if (careful) s[0] = s[1] = a[0] = a[1] = 0.0f;
+        else return (void)(t.s += s[0] + s[1], t.a += a[0] + a[1]);
+    }
+    add(std::true_type{});
+    t.s += s[0] + s[1];
+    t.a += a[0] + a[1];
+}
+
+template <int DT, bool TOP>
+__device__ __forceinline__ void scan(const void* row, int64_t first, int64_t stride, int end, float c, int top, Sums& t, Best& best,
+                                     Bounds* bounds, int wave) {
+    using V = RowVec<DT>;
+    constexpr int N = V::kN;
+    const int lane = threadIdx.x & (kWave - 1);
+    const int64_t step = kAtOnce * stride, span = (kAtOnce - 1) * stride + kWave * N;
+    bool careful = false;
+    const auto take = [&](const V (&v)[kAtOnce], int64_t e, auto&& then) {
+        float x[kAtOnce][N], most[kAtOnce], all = -INFINITY;
 #pragma unroll
-            for (int u = 0; u < kAtOnce; ++u) offer<N>(best, top, x[u], most[u], (uint32_t)(e0 + u * stride));
+        for (int u = 0; u < kAtOnce; ++u) {
+            most[u] = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                x[u][i] = v[u].get(i);
+                most[u] = fmaxf(most[u], x[u][i]);
+            }
+            all = fmaxf(all, most[u]);
         }
+        then();   // the vectors' registers are free
+        if (__ballot(all > t.m)) rebase(t, fmaxf(max64(all), t.m), c);
+        add_chunk<N>(t, x, c, careful);
+        if constexpr (TOP) {
+            const float bound = bounds != nullptr ? bounds->least : -INFINITY;
+            if (__ballot(all > lane_value(best.x, top - 1) && all >= bound)) {
+#pragma unroll
+                for (int u = 0; u < kAtOnce; ++u) offer<N>(best, top, bound, x[u], most[u], (uint32_t)(e + u * stride));
+                if (bounds != nullptr) bounds->tell(wave, lane_value(best.x, top - 1), lane_value(best.x, (top + 3) / 4 - 1));
+            }
+        }
+    };
+
+    int64_t e = first;
+    V v[kAtOnce];
+    if (first + span <= end) {
+        const int64_t last = first + (end - first - span) / step * step;   // where the last whole chunk begins
+        const auto load = [&](int64_t at) {
+            const char* from = static_cast<const char*>(row) + at * (int64_t)sizeof(typename V::Elem);   // the same for all lanes
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u)
+                v[u] = load_row<DT>(from + u * stride * (int64_t)sizeof(typename V::Elem), lane * N, INT32_MAX);
+        };
+        load(e);
+        for (; e <= last; e += step)
+            take(v, e, [&] { load(e < last ? e + step : last); });
+    }
+    for (; e < end; e += step) {
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int64_t at = e + u * stride + lane * N;
+            v[u] = load_row<DT>(row, (int)(at < end ? at : end), end, kMinusInf<DT>);
+        }
+        take(v, e, [] {});
     }
     // every lane's sums have the same maximum
     t.s = sum64(t.s);
@@ -225,7 +320,7 @@ __device__ __forceinline__ void finish(const Logprobs& q, int64_t r, const Sums&
 
 // The workgroup's sums and list in its first wavefront.
 template <bool TOP>
-__device__ __forceinline__ void join_waves(Sums& t, Best& best, int top, float c, Sums* part, Best (*lists)[kMaxTop]) {
+__device__ __forceinline__ void join_waves(Sums& t, Best& best, float c, Sums* part, Best (*lists)[kMaxTop]) {
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
     __syncthreads();   // the first wavefront is done with what was there
     if (lane == 0) part[wave] = t;
@@ -234,7 +329,7 @@ __device__ __forceinline__ void join_waves(Sums& t, Best& best, int top, float c
     if (wave != 0) return;
     for (int w = 1; w < kBlock / kWave; ++w) {
         t = joined(t, part[w], c);
-        if constexpr (TOP) merge(best, top, lists[w]);
+        if constexpr (TOP) merge_reversed(best, lists[w][kWave - 1 - lane]);
     }
 }
 
@@ -244,7 +339,8 @@ __global__ void __launch_bounds__(kBlock) logprob_rows(const Logprobs q) {
     constexpr int N = RowVec<DT>::kN, R = kBlock / T;
     __shared__ Sums part[T > kWave ? kBlock / kWave : 1];
     __shared__ Best lists[T > kWave && TOP ? kBlock / kWave : 1][kMaxTop];
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    __shared__ Bounds bounds;
+    const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
     const float c = q.scale * kLog2e;
     const int64_t items = q.rows * q.pieces;
     for (int64_t i0 = (int64_t)blockIdx.x * R; i0 < items; i0 += (int64_t)gridDim.x * R) {
@@ -256,9 +352,14 @@ __global__ void __launch_bounds__(kBlock) logprob_rows(const Logprobs q) {
         const char* row = static_cast<const char*>(q.logits) + r * q.ld * (DT == SDGP_BF16 ? 2 : 4);
         Sums t = {kLowest, 0.0f, 0.0f};
         Best best = {-INFINITY, 0xFFFFFFFFu};
-        scan<DT, TOP>(row, begin + (T == kWave ? 0 : wave * kWave * N), (int64_t)T * N, end, c, q.top, t, best);
+        if constexpr (T > kWave && TOP) {
+            if (lane == 0) bounds.share[wave] = -INFINITY;
+            if (threadIdx.x == 0) bounds.least = -INFINITY;
+            __syncthreads();
+        }
+        scan<DT, TOP>(row, begin + (T == kWave ? 0 : wave * kWave * N), (int64_t)T * N, end, c, q.top, t, best, T > kWave ? &bounds : nullptr, wave);
         if constexpr (T > kWave) {
-            join_waves<TOP>(t, best, q.top, c, part, lists);
+            join_waves<TOP>(t, best, c, part, lists);
             if (wave != 0) continue;
         }
         if (q.pieces == 1) {
@@ -287,25 +388,15 @@ __global__ void __launch_bounds__(kBlock) logprob_join(const Logprobs q) {
         t.a = sum64(t.a);
         Best best = {-INFINITY, 0xFFFFFFFFu};
         if constexpr (TOP) {
-            // an entry a lane; the wavefront's entries come in batches of 64, the best of each batch first
             const Best* list = q.part_best + r * q.pieces * q.top;
             const int n = q.pieces * q.top;
             for (int i0 = wave * kWave; i0 < n; i0 += kBlock) {
                 Best mine = {-INFINITY, 0xFFFFFFFFu};
                 if (i0 + lane < n) mine = list[i0 + lane];
-                for (;;) {
-                    const float x = lane_value(best.x, q.top - 1);
-                    const uint32_t j = lane_word(best.j, q.top - 1);
-                    if (!__ballot(better(mine.x, mine.j, x, j))) break;
-                    const float top_x = max64(mine.x);
-                    // of equal ones the lowest index: pieces and their lists are in that order
-                    const int from = __builtin_ctzll(__ballot(mine.x == top_x));
-                    insert(best, top_x, lane_word(mine.j, from));
-                    if (lane == from) mine = {-INFINITY, 0xFFFFFFFFu};
-                }
+                if (__ballot(better(mine.x, mine.j, lane_value(best.x, q.top - 1), lane_word(best.j, q.top - 1)))) merge_unsorted(best, mine);
             }
         }
-        join_waves<TOP>(t, best, q.top, c, part, lists);
+        join_waves<TOP>(t, best, c, part, lists);
         if (wave == 0) finish<DT>(q, r, t, best);
     }
 }
@@ -319,24 +410,26 @@ struct LogprobsGrad {
     float scale;
 };
 
-// T threads on a chunk of a row, kVecs vectors each.
+// T threads on a chunk of a row, VECS vectors each.  The gradient is p (A + B log2 p) with A and B the row's, and
+// log2 p = c (x - m) - log2(sum) a difference and a fused operation; what rounding log2(sum) cut off is in A and B.  Seven
+// instructions an element and the exponential.
 template <int DT, int T, int VECS, bool ENTROPY>
 __global__ void __launch_bounds__(kBlock) logprob_grad(const LogprobsGrad q) {
     using V = RowVec<DT>;
     constexpr int N = V::kN, R = kBlock / T;
     constexpr int64_t kSize = sizeof(typename V::Elem);
     const int t = threadIdx.x % T;
+    const float c = q.scale * kLog2e;
     const int64_t items = q.rows * q.chunks;
-    for (int64_t item = (int64_t)blockIdx.x * R + threadIdx.x / T; item < items; item += (int64_t)gridDim.x * R) {
+    for (int64_t item = (int64_t)blockIdx.x * R + (R > 1 ? threadIdx.x / T : 0); item < items; item += (int64_t)gridDim.x * R) {
         const int64_t r = q.chunks == 1 ? item : item / q.chunks;
-        const int first = (int)(item - r * q.chunks) * (T * VECS * N) + t * N;
-        const char* row = static_cast<const char*>(q.logits) + r * q.ld * kSize;
+        const int64_t first = (item - r * q.chunks) * (T * VECS * N);
+        const char* row = static_cast<const char*>(q.logits) + (r * q.ld + first) * kSize;
+        char* out = static_cast<char*>(q.dlogits) + (r * q.ld_out + first) * kSize;
+        const int left = (int)(q.V - first);
         V x[VECS];
 #pragma unroll
-        for (int v = 0; v < VECS; ++v) {
-            const int64_t e = (int64_t)first + v * T * N;
-            x[v] = load_row<DT>(row, (int)(e < q.V ? e : q.V), q.V);
-        }
+        for (int v = 0; v < VECS; ++v) x[v] = load_row<DT>(row, (v * T + t) * N, left);
         const float m = q.stats[2 * r], logs = q.stats[2 * r + 1];
         int64_t token = -1;
         float g = 0.0f, h = 0.0f, H = 0.0f;
@@ -349,20 +442,27 @@ __global__ void __launch_bounds__(kBlock) logprob_grad(const LogprobsGrad q) {
             H = q.entropy[r];
         }
         const bool empty = logs == -INFINITY;
+        const float l2 = mul_rn(empty ? 0.0f : logs, kLog2e), off = empty ? 0.0f : fmaf(logs, kLog2e, -l2), back = exp2_hw(-off);
+        if (empty) g = h = 0.0f;
+        const float B = -h * kLn2 * back, A = -(g + h * (H - kLn2 * off)) * back;
+        const int64_t at = token - first;   // the token's place in this chunk
 #pragma unroll
         for (int v = 0; v < VECS; ++v) {
-            const int64_t e = (int64_t)first + v * T * N;
+            const int e = (v * T + t) * N;
             float d[N];
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const float l = (x[v].get(i) - m) * q.scale - logs, p = exp2_hw(l * kLog2e);
-                d[i] = ENTROPY ? -p * (g + h * (fmaxf(l, kFloor2) + H)) : -p * g;
-                if (e + i == token) d[i] += g;
-                if (empty) d[i] = 0.0f;
+                const float l = fmaf(x[v].get(i) - m, c, -l2), p = exp2_hw(l);
+                d[i] = ENTROPY ? p * fmaf(B, fmaxf(l, kFloor2), A) : p * A;
+            }
+            if (at >= e && at < e + N && token >= 0) {
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if (e + i == at) d[i] += g;
             }
             V o;
             o.set(d);
-            store_row<DT>(static_cast<char*>(q.dlogits) + r * q.ld_out * kSize, (int)(e < q.V ? e : q.V), q.V, o);
+            store_row<DT>(out, e, left, o);
         }
     }
 }
@@ -407,7 +507,8 @@ int launch_grad(LogprobsGrad q, hipStream_t stream) {
     };
     if (q.V <= 16 * N) return go(logprob_grad<DT, 16, 1, ENTROPY>, 16, 1);
     if (q.V <= 64 * 2 * N) return go(logprob_grad<DT, 64, 2, ENTROPY>, 64, 2);
-    return go(logprob_grad<DT, 256, 2, ENTROPY>, 256, 2);
+    if (q.V <= 256 * 8 * N) return go(logprob_grad<DT, 256, 2, ENTROPY>, 256, 2);
+    return go(logprob_grad<DT, 256, 4, ENTROPY>, 256, 4);
 }
 
 }  // namespace
