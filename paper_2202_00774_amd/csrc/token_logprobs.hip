@@ -155,20 +155,16 @@ constexpr int kOneByOne = 4;   // up to so many lanes with new ones, they go in 
 // it, its index being larger; but among those offered here it may be, so the list's end is compared with its index.
 template <int N>
 __device__ __forceinline__ void offer(Best& b, int top, float bound, float (&x)[N], float most, uint32_t first) {
-    if (!__ballot(most > lane_value(b.x, top - 1) && most >= bound)) return;
     const int lane = threadIdx.x & (kWave - 1);
     const uint32_t j0 = first + (uint32_t)(lane * N);
-    for (;;) {
-        uint32_t j = 0xFFFFFFFFu;   // a lane's best: the first of equal ones
-#pragma unroll
-        for (int i = N - 1; i >= 0; --i) j = x[i] == most ? j0 + i : j;
-        const bool mine = most > -INFINITY && most >= bound && better(most, j, lane_value(b.x, top - 1), lane_word(b.j, top - 1));
-        const uint64_t who = __ballot(mine);
-        if (!who) return;
+    uint64_t who = __ballot(most > lane_value(b.x, top - 1) && most >= bound);
+    while (who) {
         if (__builtin_popcountll(who) <= kOneByOne) {
+            // at least as good as the list's end (one that is only as good may go in behind it), and not -inf
+            const float least = fmaxf(fmaxf(lane_value(b.x, top - 1), bound), kLowest);
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                uint64_t some = __ballot(mine && x[i] >= lane_value(b.x, top - 1) && x[i] >= bound && x[i] > -INFINITY);
+                uint64_t some = __ballot(x[i] >= least);
                 while (some) {
                     const int from = __builtin_ctzll(some);
                     some &= some - 1;
@@ -177,15 +173,20 @@ __device__ __forceinline__ void offer(Best& b, int top, float bound, float (&x)[
             }
             return;
         }
-        merge_unsorted(b, {mine ? most : -INFINITY, mine ? j : 0xFFFFFFFFu});
-        if (mine) {
-            most = -INFINITY;
+        uint32_t j = 0xFFFFFFFFu;   // a lane's best: the first of equal ones
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                if (j0 + i == j) x[i] = -INFINITY;
-                most = fmaxf(most, x[i]);
-            }
+        for (int i = N - 1; i >= 0; --i) j = x[i] == most ? j0 + i : j;
+        const bool mine = most >= fmaxf(bound, kLowest) && better(most, j, lane_value(b.x, top - 1), lane_word(b.j, top - 1));
+        if (!__ballot(mine)) return;   // each turn takes one away at least
+        merge_unsorted(b, {mine ? most : -INFINITY, mine ? j : 0xFFFFFFFFu});
+        most = mine ? -INFINITY : most;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (mine && j0 + i == j) x[i] = -INFINITY;
+            most = fmaxf(most, x[i]);
         }
+        // what is left over may be as good as the list's end, with a lower index
+        who = __ballot(most >= fmaxf(fmaxf(lane_value(b.x, top - 1), bound), kLowest));
     }
 }
 
@@ -194,29 +195,31 @@ __device__ __forceinline__ void offer(Best& b, int top, float bound, float (&x)[
 constexpr int kAtOnce = 2;
 
 // Adds a chunk to the sums.  Without a floor under the exponents a masked logit makes the weighted sum a NaN (0 * inf): then
-// the chunk is added again with the floor, and so are the row's later chunks (`careful`).
+// it is summed again with the floor, and in the row's later chunks at once (`careful`).
 template <int N>
 __device__ __forceinline__ void add_chunk(Sums& t, const float (&x)[kAtOnce][N], float c, bool& careful) {
-    float s[2] = {0.0f, 0.0f}, a[2] = {0.0f, 0.0f};   // two chains each
-    const auto add = [&](auto floor) {
+    constexpr int M = kAtOnce * N;
+    float d[M], p[M], s[2] = {0.0f, 0.0f}, a[2] = {0.0f, 0.0f};   // two chains each
 #pragma unroll
-        for (int u = 0; u < kAtOnce; ++u)
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const float d = exponent(x[u][i], t.m, c), p = exp2_hw(d);
-                s[i & 1] += p;
-                a[i & 1] = fmaf(p, decltype(floor)::value ? fmaxf(d, kFloor2) : d, a[i & 1]);
-            }
-    };
-    if (!careful) {
-        add(std::false_type{});
-        careful = __ballot(a[0] + a[1] != a[0] + a[1]) != 0;
-        if (careful) s[0] = s[1] = a[0] = a[1] = 0.0f;
-        else return (void)(t.s += s[0] + s[1], t.a += a[0] + a[1]);
+    for (int i = 0; i < M; ++i) {
+        d[i] = exponent(x[i / N][i % N], t.m, c);
+        p[i] = exp2_hw(d[i]);
+        s[i & 1] += p[i];
     }
-    add(std::true_type{});
     t.s += s[0] + s[1];
-    t.a += a[0] + a[1];
+    if (!careful) {
+#pragma unroll
+        for (int i = 0; i < M; ++i) a[i & 1] = fmaf(p[i], d[i], a[i & 1]);
+        a[0] += a[1];
+        careful = __ballot(a[0] != a[0]) != 0;
+    }
+    if (careful) {
+        a[0] = a[1] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < M; ++i) a[i & 1] = fmaf(p[i], fmaxf(d[i], kFloor2), a[i & 1]);
+        a[0] += a[1];
+    }
+    t.a += a[0];
 }
 
 template <int DT, bool TOP>
