@@ -546,12 +546,12 @@ def sdgp_token_logprobs(logits: torch.Tensor, tokens: torch.Tensor | None, *, to
     wbytes = 0
     if need:
         workspace, wbytes = _workspace(need, workspace, logits.device, "sdgp_token_logprobs_workspace")
-    new = functools.partial(torch.empty, dtype=torch.float32, device=logits.device)
-    logp = None if tokens is None else new(shape)
-    entropy, stats = new(shape), new((*shape, 2))
+    entropy = logits.new_empty(shape, dtype=torch.float32)
+    logp = None if tokens is None else torch.empty_like(entropy)
+    stats = entropy.new_empty((*shape, 2))
     top_logp = top_ids = None
     if top:
-        top_logp, top_ids = new((*shape, top)), torch.empty((*shape, top), dtype=torch.int64, device=logits.device)
+        top_logp, top_ids = entropy.new_empty((*shape, top)), entropy.new_empty((*shape, top), dtype=torch.int64)
     rc = lib.sdgp_token_logprobs(_ptr(logits), ld, _ptr(tokens), bits, _ptr(logp), _ptr(entropy), _ptr(top_logp), _ptr(top_ids),
                                  _ptr(stats), rows, V, dt, top, scale, _ptr(workspace) if need else None, wbytes, _stream(logits))
     if rc != 0:
@@ -582,7 +582,7 @@ def sdgp_token_logprobs_bwd(logits: torch.Tensor, tokens: torch.Tensor | None, s
         _per_row(g_entropy, shape, "g_entropy", _FLOAT)
         _per_row(entropy, shape, "entropy", _FLOAT)
     if out is None:
-        out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        out = logits.new_empty(logits.shape)
     if out.shape != logits.shape or out.dtype != logits.dtype:
         raise ValueError("out must have the shape and dtype of logits")
     rc = load().sdgp_token_logprobs_bwd(_ptr(logits), ld, _ptr(tokens), bits, _ptr(stats), _ptr(entropy), _ptr(g_logp),

@@ -94,13 +94,26 @@ __device__ __forceinline__ void insert(Best& b, float x, uint32_t j) {
 
 __device__ __forceinline__ uint32_t lane_word(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); }
 
-// The value of lane (own ^ X).
+// The value of lane (own ^ X), without the LDS: within 16 lanes by DPP (4 as 7 and 3), between rows and halves by the swaps.
 template <int X>
 __device__ __forceinline__ uint32_t lane_xor(uint32_t v) {
     constexpr int kDpp = X == 1 ? 0xB1 : X == 2 ? 0x4E : X == 3 ? 0x1B : X == 7 ? 0x141 : X == 15 ? 0x140 : X == 8 ? 0x128 : 0;
-    if constexpr (kDpp != 0) return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, kDpp, 0xF, 0xF, true);
-    else if constexpr (X < 32) return (uint32_t)__builtin_amdgcn_ds_swizzle((int)v, 0x1F | (X << 10));
-    else return (uint32_t)__shfl_xor((int)v, X);
+    if constexpr (kDpp != 0) {
+        return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, kDpp, 0xF, 0xF, true);
+    } else if constexpr (X == 4) {
+        return lane_xor<3>(lane_xor<7>(v));
+    } else if constexpr (X == 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);   // rows 0 0 2 2 and 1 1 3 3
+        return (threadIdx.x & 16) ? r[0] : r[1];
+    } else if constexpr (X == 32) {
+        const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);   // the lower half twice, the upper half twice
+        return (threadIdx.x & 32) ? r[0] : r[1];
+    } else if constexpr (X == 31) {
+        return lane_xor<15>(lane_xor<16>(v));
+    } else {
+        static_assert(X == 63, "");
+        return lane_xor<31>(lane_xor<32>(v));
+    }
 }
 
 // Of each pair of lanes l, l ^ X the lower one keeps the better logit.
