@@ -10,17 +10,26 @@
 // the library's counter hash of (seed, element), so a step can be repeated bit for bit.  A root that is not zero is not
 // stored as zero, since the step divides by it.  A gradient that is infinite or NaN spoils its own element only: the
 // scale is taken over the block's finite values.
+//
+// Bound by memory: 28 bytes an element with fp32 states (parameter and both states in and out, gradient in), 16 with 8-bit
+// ones.  A wavefront takes a block of 256 elements, four a lane, so a block's scale is a maximum over one wavefront; four
+// blocks' loads are in flight together.  A workgroup's tile of 16 blocks lies in one tensor, which it looks up in the
+// arguments.  In 8 bits an element costs 75 vector instructions, as many as fit beside its 16 bytes: codes are cut from the
+// float's bits, and what only infinities and NaN need is done where a block has them.
 #include "adamw.h"
+
+#include "rows.h"
 
 namespace sdgp {
 
 namespace {
 
-constexpr float kMaxFinite = 3.402823466e38f;
+constexpr int kThreads = 256, kWave = 64, kAtOnce = kAdamTile / (kThreads / kWave);   // blocks of a wavefront
+constexpr uint32_t kInf = 0x7F800000u;
 
 // One mixed word of (seed, element): the finalizer of common.h's hash, one word an element.
-__device__ __forceinline__ uint32_t random_word(uint32_t mix, uint64_t e) {
-    uint32_t v = hash_row(mix, (uint32_t)(e >> 32)) ^ (uint32_t)e;
+__device__ __forceinline__ uint32_t random_word(uint32_t row, uint32_t e) {
+    uint32_t v = row ^ e;
     v ^= v >> 16;
     v *= 0x6A09E667u;
     v ^= v >> 15;
@@ -28,102 +37,206 @@ __device__ __forceinline__ uint32_t random_word(uint32_t mix, uint64_t e) {
     return v ^ (v >> 16);
 }
 
-// Largest over the 256 threads of the workgroup.
-__device__ __forceinline__ float block_max(float v, float* lds) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) v = fmaxf(v, __shfl_xor(v, o));
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x / 64] = v;
-    __syncthreads();
-    return fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3]));
+// Largest over the wavefront: of the bits of floats that are not negative, which are in the floats' order.
+__device__ __forceinline__ uint32_t max_bits(uint32_t v) {
+    const auto dpp = [](uint32_t x, auto ctrl) {
+        return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, decltype(ctrl)::value, 0xF, 0xF, true);
+    };
+    v = max(v, dpp(v, std::integral_constant<int, 0xB1>{}));
+    v = max(v, dpp(v, std::integral_constant<int, 0x4E>{}));
+    v = max(v, dpp(v, std::integral_constant<int, 0x141>{}));
+    v = max(v, dpp(v, std::integral_constant<int, 0x140>{}));
+    const auto lane = [&](int l) { return (uint32_t)__builtin_amdgcn_readlane((int)v, l); };
+    return max(max(lane(0), lane(16)), max(lane(32), lane(48)));
 }
 
-// The exponent k of a block's scale 2^k: the smallest with top <= 448 * 2^k, -126 at least; 0 for a block of zeros.
-__device__ __forceinline__ int scale_exponent(float top) {
-    if (!(top > 0.0f)) return 0;
-    int e;
-    const float f = frexpf(top, &e);
-    const int k = e - 9 + (f > 0.875f ? 1 : 0);
+// The exponent k of a block's scale 2^k, from the bits of its largest value: the smallest with top <= 448 * 2^k, -126 at
+// least; 0 for a block of zeros.  448 is 1.75 * 2^8, so k is the exponent less 8, one more above 1.75 (subnormal tops end up
+// at -126 either way).
+__device__ __forceinline__ int scale_exponent(uint32_t top) {
+    if (top == 0) return 0;
+    const int k = (int)(top >> 23) - 127 - 8 + ((top & 0x7FFFFFu) > 0x600000u ? 1 : 0);
     return k < -126 ? -126 : k;
 }
 
 __device__ __forceinline__ float power_of_two(int k) { return bits_to_float((uint32_t)(k + 127) << 23); }
 
-// x / 2^k on the grid of e4m3 (8 steps a power of two, evenly spaced below 2^-6), rounded up where u exceeds what is
-// cut off; the code's eight bits.
-__device__ __forceinline__ uint32_t to_code(float x, int k, float u, bool keep) {
-    if (!(fabsf(x) <= kMaxFinite)) return 0x7Fu;
-    const float y = ldexpf(fabsf(x), -k);
-    int e = (int)(float_to_bits(y) >> 23) - 127;
-    e = e < -6 ? -6 : e;
-    float c = floorf(ldexpf(y, 3 - e) + u);
-    if (keep && y > 0.0f && c == 0.0f) c = 1.0f;
-    const uint32_t sign = (float_to_bits(x) >> 24) & 0x80u;
-    // c in 0 .. 16 steps of 2^(e-3): a step past 15 is the next power of two's first code
-    return sign | ((uint32_t)((e + 6) << 3) + (uint32_t)c);
+// |x| / 2^k (`y`, at most 448) on the grid of e4m3, rounded up where u / 2^16 exceeds what is cut off.  From 2^-6 on the
+// code is the float's exponent and upper three mantissa bits, u added below them; the codes below are evenly spaced.
+__device__ __forceinline__ uint32_t to_code(float y, uint32_t u) {
+    const uint32_t upper = ((float_to_bits(y) + (u << 4)) >> 20) - 960u;                      // exponent bias 127 -> 7
+    const uint32_t lower = (uint32_t)fmaf(y, 512.0f, (float)u * 0x1p-16f);
+    return y < 0x1p-6f ? lower : upper;
 }
 
-__device__ __forceinline__ float from_code(uint32_t code) {
-    const uint32_t e = (code >> 3) & 15u, f = code & 7u;
-    const float v = e ? ldexpf((float)(8u + f), (int)e - 10) : ldexpf((float)f, -9);
-    return (code & 0x7Fu) == 0x7Fu ? NAN : (code & 0x80u) ? -v : v;
+typedef uint32_t u32x2_half_aligned __attribute__((ext_vector_type(2), aligned(2), may_alias));
+typedef uint32_t u32_any __attribute__((aligned(1), may_alias));
+
+// Four values of a lane: elements e .. e + 3 of a tensor of n.  What lies outside is 0 and is neither read nor written.
+template <int DT>
+__device__ __forceinline__ void load4(const void* p, int64_t e, int64_t n, float (&f)[4]) {
+    if (e + 4 <= n) {
+        if constexpr (DT == SDGP_BF16) {
+            const auto v = *reinterpret_cast<const u32x2_half_aligned*>(static_cast<const uint16_t*>(p) + e);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) f[2 * i] = bits_to_float(v[i] << 16), f[2 * i + 1] = bits_to_float(v[i] & 0xFFFF0000u);
+        } else {
+            const auto v = *reinterpret_cast<const u32x4_word_aligned*>(static_cast<const float*>(p) + e);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[i] = bits_to_float(v[i]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f[i] = 0.0f;
+            if (e + i < n) f[i] = DT == SDGP_BF16 ? bf16_to_float(static_cast<const uint16_t*>(p)[e + i]) : static_cast<const float*>(p)[e + i];
+        }
+    }
+}
+
+template <int DT>
+__device__ __forceinline__ void store4(void* p, int64_t e, int64_t n, const float (&f)[4]) {
+    if (e + 4 <= n) {
+        if constexpr (DT == SDGP_BF16) {
+            const u32x2_half_aligned v = {float2_to_bf16x2(f[0], f[1]), float2_to_bf16x2(f[2], f[3])};
+            *reinterpret_cast<u32x2_half_aligned*>(static_cast<uint16_t*>(p) + e) = v;
+        } else {
+            const u32x4_word_aligned v = {float_to_bits(f[0]), float_to_bits(f[1]), float_to_bits(f[2]), float_to_bits(f[3])};
+            *reinterpret_cast<u32x4_word_aligned*>(static_cast<float*>(p) + e) = v;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (e + i < n) {
+                if constexpr (DT == SDGP_BF16) static_cast<uint16_t*>(p)[e + i] = (uint16_t)float2_to_bf16x2(f[i], 0.0f);
+                else static_cast<float*>(p)[e + i] = f[i];
+            }
+    }
+}
+
+__device__ __forceinline__ uint32_t load4_codes(const void* p, int64_t e, int64_t n) {
+    const uint8_t* at = static_cast<const uint8_t*>(p) + e;
+    if (e + 4 <= n) return *reinterpret_cast<const u32_any*>(at);
+    uint32_t v = 0;
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+        if (e + i < n) v |= (uint32_t)at[i] << (8 * i);
+    return v;
+}
+
+__device__ __forceinline__ void store4_codes(void* p, int64_t e, int64_t n, uint32_t v) {
+    uint8_t* at = static_cast<uint8_t*>(p) + e;
+    if (e + 4 <= n) {
+        *reinterpret_cast<u32_any*>(at) = v;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+        if (e + i < n) at[i] = (uint8_t)(v >> (8 * i));
+}
+
+__device__ __forceinline__ void from_codes(uint32_t v, float scale, float (&f)[4]) {
+    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)v, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)v, true);
+    f[0] = lo[0] * scale, f[1] = lo[1] * scale, f[2] = hi[0] * scale, f[3] = hi[1] * scale;
+}
+
+// The codes of a block's four values a lane; KEEP: not negative, and what is not zero is not stored as zero.
+template <bool KEEP>
+__device__ __forceinline__ uint32_t to_codes(const float (&x)[4], const uint32_t (&u)[4], float* scale_at) {
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) most = max(most, float_to_bits(x[i]) & 0x7FFFFFFFu);
+    uint32_t top = max_bits(most);
+    const bool odd = top >= kInf;       // something infinite or NaN: the scale is that of the others
+    if (odd) {
+        most = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t b = float_to_bits(x[i]) & 0x7FFFFFFFu;
+            most = b < kInf ? max(most, b) : most;
+        }
+        top = max_bits(most);
+    }
+    const int k = scale_exponent(top);
+    if ((threadIdx.x & (kWave - 1)) == 0) *scale_at = power_of_two(k);
+    const float inv = power_of_two(-k);
+    uint32_t codes = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t b = float_to_bits(x[i]);
+        const float y = fabsf(x[i]) * inv;
+        uint32_t code = to_code(y, u[i]);
+        if constexpr (KEEP) code = max(code, min(float_to_bits(y), 1u));
+        else code |= (b >> 24) & 0x80u;
+        if (odd && (b & 0x7FFFFFFFu) >= kInf) code = 0x7Fu;
+        codes |= code << (8 * i);
+    }
+    return codes;
 }
 
 template <int PDT, int GDT, int BITS>
-__global__ void __launch_bounds__(kAdamBlock) adamw_blocks(const AdamArgs a) {
-    __shared__ float lds[4];
-    int lo = 0, hi = a.count;                       // the tensor that holds this block
+__global__ void __launch_bounds__(kThreads) adamw_tiles(const AdamArgs a) {
+    int lo = 0, hi = a.count;                       // the tensor that holds this tile
     while (hi - lo > 1) {
         const int mid = (lo + hi) / 2;
         if (a.first[mid] <= blockIdx.x) lo = mid;
         else hi = mid;
     }
     const AdamTensor& t = a.t[lo];
-    const int64_t block = blockIdx.x - a.first[lo], i = block * kAdamBlock + threadIdx.x;
-    const bool in = i < t.n;
+    const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+    const int64_t block0 = (int64_t)(blockIdx.x - a.first[lo]) * kAdamTile + wave * kAtOnce, n = t.n;
+    if (block0 * kAdamBlock >= n) return;
     const float gs = a.grad_scale ? *a.grad_scale : 1.0f;
 
-    float p = 0.0f, g = 0.0f, m = 0.0f, v = 0.0f;
-    if (in) {
-        p = PDT == SDGP_BF16 ? bf16_to_float(static_cast<uint16_t*>(t.p)[i]) : static_cast<float*>(t.p)[i];
-        g = GDT == SDGP_BF16 ? bf16_to_float(static_cast<const uint16_t*>(t.g)[i]) : static_cast<const float*>(t.g)[i];
+    float p[kAtOnce][4], g[kAtOnce][4], m[kAtOnce][4], v[kAtOnce][4];
+    uint32_t mc[kAtOnce], vc[kAtOnce];
+#pragma unroll
+    for (int b = 0; b < kAtOnce; ++b) {
+        const int64_t e = (block0 + b) * kAdamBlock + lane * 4;
+        load4<PDT>(t.p, e, n, p[b]);
+        load4<GDT>(t.g, e, n, g[b]);
         if constexpr (BITS == 32) {
-            m = static_cast<float*>(t.m)[i];
-            v = static_cast<float*>(t.v)[i];
+            load4<SDGP_F32>(t.m, e, n, m[b]);
+            load4<SDGP_F32>(t.v, e, n, v[b]);
         } else {
-            m = from_code(static_cast<uint8_t*>(t.m)[i]) * t.m_scale[block];
-            const float r = from_code(static_cast<uint8_t*>(t.v)[i]) * t.v_scale[block];
-            v = __fmul_rn(r, r);
+            mc[b] = load4_codes(t.m, e, n);
+            vc[b] = load4_codes(t.v, e, n);
         }
     }
-    // one rounding an operation, so that a code does not depend on which products were fused
-    g = __fmul_rn(g, gs);
-    m = __fadd_rn(__fmul_rn(m, a.b1), __fmul_rn(g, a.one_b1));
-    v = __fadd_rn(__fmul_rn(v, a.b2), __fmul_rn(__fmul_rn(g, g), a.one_b2));
-    const float r = sqrtf(v);
-    p = p * a.decay - a.rate * (m / (r / a.root_bc2 + a.eps));
-    if (in) {
-        if constexpr (PDT == SDGP_BF16) static_cast<uint16_t*>(t.p)[i] = (uint16_t)float_to_bf16(p);
-        else static_cast<float*>(t.p)[i] = p;
-        if (t.copy) t.copy[i] = (uint16_t)float_to_bf16(p);
-    }
-    if constexpr (BITS == 32) {
-        if (in) {
-            static_cast<float*>(t.m)[i] = m;
-            static_cast<float*>(t.v)[i] = v;
+#pragma unroll
+    for (int b = 0; b < kAtOnce; ++b) {
+        const int64_t block = block0 + b, e = block * kAdamBlock + lane * 4;
+        if (block * kAdamBlock >= n) break;
+        if constexpr (BITS == 8) {
+            from_codes(mc[b], t.m_scale[block], m[b]);
+            from_codes(vc[b], t.v_scale[block], v[b]);
         }
-    } else {
-        const float am = fabsf(m);
-        const int km = scale_exponent(block_max(am <= kMaxFinite ? am : 0.0f, lds));
-        const int kv = scale_exponent(block_max(r <= kMaxFinite ? r : 0.0f, lds));
-        if (in) {
-            const uint32_t w = random_word(a.mix, ((uint64_t)a.base + blockIdx.x) * kAdamBlock + threadIdx.x);
-            static_cast<uint8_t*>(t.m)[i] = (uint8_t)to_code(m, km, (float)(w & 0xFFFFu) * 0x1p-16f, false);
-            static_cast<uint8_t*>(t.v)[i] = (uint8_t)to_code(r, kv, (float)(w >> 16) * 0x1p-16f, true);
+        float r[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            // one rounding an operation, so that a code does not depend on which products were fused
+            const float gi = mul_rn(g[b][i], gs), v0 = BITS == 8 ? mul_rn(v[b][i], v[b][i]) : v[b][i];
+            m[b][i] = add_rn(mul_rn(m[b][i], a.b1), mul_rn(gi, a.one_b1));
+            v[b][i] = add_rn(mul_rn(v0, a.b2), mul_rn(mul_rn(gi, gi), a.one_b2));
+            r[i] = sqrtf(v[b][i]);
+            p[b][i] = fmaf(p[b][i], a.decay, -a.rate * (m[b][i] / fmaf(r[i], a.inv_root_bc2, a.eps)));
         }
-        if (threadIdx.x == 0) {
-            t.m_scale[block] = power_of_two(km);
-            t.v_scale[block] = power_of_two(kv);
+        store4<PDT>(t.p, e, n, p[b]);
+        if (PDT == SDGP_F32 && t.copy != nullptr) store4<SDGP_BF16>(t.copy, e, n, p[b]);
+        if constexpr (BITS == 32) {
+            store4<SDGP_F32>(t.m, e, n, m[b]);
+            store4<SDGP_F32>(t.v, e, n, v[b]);
+        } else {
+            const uint64_t at = (uint64_t)(t.block + block) * kAdamBlock;
+            const uint32_t row = hash_row(a.mix, (uint32_t)(at >> 32)), e32 = (uint32_t)at + lane * 4;
+            uint32_t um[4], uv[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t w = random_word(row, e32 + i);
+                um[i] = w & 0xFFFFu, uv[i] = w >> 16;
+            }
+            store4_codes(t.m, e, n, to_codes<false>(m[b], um, t.m_scale + block));
+            store4_codes(t.v, e, n, to_codes<true>(r, uv, t.v_scale + block));
         }
     }
 }
@@ -131,17 +244,13 @@ __global__ void __launch_bounds__(kAdamBlock) adamw_blocks(const AdamArgs a) {
 }  // namespace
 
 int adamw_launch(const AdamArgs& a, int param_dt, int grad_dt, int state_bits, hipStream_t stream) {
-    const dim3 grid(a.first[a.count]), block(kAdamBlock);
+    const dim3 grid(a.first[a.count]), block(kThreads);
     const bool pb = param_dt == SDGP_BF16, gb = grad_dt == SDGP_BF16;
-    if (state_bits == 32) {
-        auto k = pb ? (gb ? adamw_blocks<SDGP_BF16, SDGP_BF16, 32> : adamw_blocks<SDGP_BF16, SDGP_F32, 32>)
-                    : (gb ? adamw_blocks<SDGP_F32, SDGP_BF16, 32> : adamw_blocks<SDGP_F32, SDGP_F32, 32>);
-        hipLaunchKernelGGL(k, grid, block, 0, stream, a);
-    } else {
-        auto k = pb ? (gb ? adamw_blocks<SDGP_BF16, SDGP_BF16, 8> : adamw_blocks<SDGP_BF16, SDGP_F32, 8>)
-                    : (gb ? adamw_blocks<SDGP_F32, SDGP_BF16, 8> : adamw_blocks<SDGP_F32, SDGP_F32, 8>);
-        hipLaunchKernelGGL(k, grid, block, 0, stream, a);
-    }
+    auto k = state_bits == 32 ? (pb ? (gb ? adamw_tiles<SDGP_BF16, SDGP_BF16, 32> : adamw_tiles<SDGP_BF16, SDGP_F32, 32>)
+                                    : (gb ? adamw_tiles<SDGP_F32, SDGP_BF16, 32> : adamw_tiles<SDGP_F32, SDGP_F32, 32>))
+                              : (pb ? (gb ? adamw_tiles<SDGP_BF16, SDGP_BF16, 8> : adamw_tiles<SDGP_BF16, SDGP_F32, 8>)
+                                    : (gb ? adamw_tiles<SDGP_F32, SDGP_BF16, 8> : adamw_tiles<SDGP_F32, SDGP_F32, 8>));
+    hipLaunchKernelGGL(k, grid, block, 0, stream, a);
     return launch_status();
 }
 

@@ -178,36 +178,39 @@ int sdgp_adamw_step(int count, void* const* params, const void* const* grads, vo
     a.b1 = (float)beta1, a.one_b1 = (float)(1.0 - beta1), a.b2 = (float)beta2, a.one_b2 = (float)(1.0 - beta2);
     a.decay = (float)(1.0 - lr * weight_decay);
     a.rate = (float)(lr / (1.0 - std::pow(beta1, (double)step)));
-    a.root_bc2 = (float)std::sqrt(1.0 - std::pow(beta2, (double)step));
+    a.inv_root_bc2 = (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, (double)step)));
     a.eps = (float)eps;
     a.mix = sdgp::seed_mix(seed);
-    a.base = 0, a.count = 0, a.first[0] = 0;
+    a.count = 0, a.first[0] = 0;
+    constexpr int64_t kTileElements = (int64_t)sdgp::kAdamTile * sdgp::kAdamBlock;
+    int64_t block = 0;   // first block of a tensor, counted in the call
     for (int i = 0; i < count; ++i) {
-        // a tensor longer than a launch holds goes in parts, whole blocks each
+        // a tensor longer than a launch holds goes in parts, whole tiles each
         for (int64_t from = 0; from < numel[i];) {
             const int64_t room = sdgp::kAdamLaunch - a.first[a.count];
             if (a.count == sdgp::kAdamTensors || room == 0) {
                 const int rc = sdgp::adamw_launch(a, param_dt, grad_dt, state_bits, static_cast<hipStream_t>(hip_stream));
                 if (rc != SDGP_OK) return rc;
-                a.base += a.first[a.count];
                 a.count = 0;
                 continue;
             }
-            const int64_t left = numel[i] - from, part = left < room * sdgp::kAdamBlock ? left : room * sdgp::kAdamBlock;
+            const int64_t left = numel[i] - from, part = left < room * kTileElements ? left : room * kTileElements;
             sdgp::AdamTensor& t = a.t[a.count];
-            const int64_t state = state_bits == 8 ? 1 : 4, block = from / sdgp::kAdamBlock;
+            const int64_t state = state_bits == 8 ? 1 : 4, at = from / sdgp::kAdamBlock;
             t.p = static_cast<char*>(params[i]) + from * element(param_dt);
             t.g = static_cast<const char*>(grads[i]) + from * element(grad_dt);
             t.m = static_cast<char*>(exp_avg[i]) + from * state;
             t.v = static_cast<char*>(exp_avg_sq[i]) + from * state;
-            t.m_scale = state_bits == 8 ? exp_avg_scale[i] + block : nullptr;
-            t.v_scale = state_bits == 8 ? exp_avg_sq_scale[i] + block : nullptr;
+            t.m_scale = state_bits == 8 ? exp_avg_scale[i] + at : nullptr;
+            t.v_scale = state_bits == 8 ? exp_avg_sq_scale[i] + at : nullptr;
             t.copy = copies ? static_cast<uint16_t*>(copies[i]) + from : nullptr;
             t.n = part;
-            a.first[a.count + 1] = a.first[a.count] + (uint32_t)((part + sdgp::kAdamBlock - 1) / sdgp::kAdamBlock);
+            t.block = block + at;
+            a.first[a.count + 1] = a.first[a.count] + (uint32_t)((part + kTileElements - 1) / kTileElements);
             ++a.count;
             from += part;
         }
+        block += (numel[i] + sdgp::kAdamBlock - 1) / sdgp::kAdamBlock;
     }
     return a.count == 0 ? SDGP_OK : sdgp::adamw_launch(a, param_dt, grad_dt, state_bits, static_cast<hipStream_t>(hip_stream));
 }
