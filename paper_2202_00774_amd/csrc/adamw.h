@@ -5,32 +5,51 @@
 
 namespace sdgp {
 
-constexpr int kAdamTensors = 48;                      // a launch's arguments stay below 4 KB
 constexpr int kAdamBlock = 256;                       // elements that share a scale in an 8-bit state
 constexpr int kAdamTile = 16;                         // blocks of a workgroup
 constexpr int64_t kAdamLaunch = (int64_t)1 << 22;     // tiles of a launch: its threads are counted in 32 bits
+constexpr int64_t kAdamPart = (int64_t)1 << 31;       // elements of a tensor in one launch: counted in 32 bits, whole tiles
 
-struct AdamTensor {
-    void* p;
-    const void* g;
-    void *m, *v;
-    float *m_scale, *v_scale;      // 8-bit states
-    uint16_t* copy;                // bf16 copy of an fp32 parameter, or null
-    int64_t n;
-    int64_t block;                 // its first block, counted in the call
+// The tensors of a launch, by value: as many as leave its arguments below 4 KB.
+template <int BITS>
+struct AdamTensors;
+
+template <>
+struct AdamTensors<32> {
+    static constexpr int kMost = 82;
+    void* p[kMost];
+    const void* g[kMost];
+    void *m[kMost], *v[kMost];
+    uint16_t* copy[kMost];         // bf16 copy of an fp32 parameter, or null
+    uint32_t n[kMost];
+    uint32_t first[kMost];         // first tile of a tensor, counted in the launch
 };
 
+template <>
+struct AdamTensors<8> {
+    static constexpr int kMost = 58;
+    void* p[kMost];
+    const void* g[kMost];
+    void *m[kMost], *v[kMost];
+    uint16_t* copy[kMost];
+    uint32_t n[kMost];
+    uint32_t first[kMost];
+    float *m_scale[kMost], *v_scale[kMost];
+    uint32_t block[kMost];         // its first block, counted in the call
+};
+
+template <int BITS>
 struct AdamArgs {
-    AdamTensor t[kAdamTensors];
-    uint32_t first[kAdamTensors + 1];   // first tile of each tensor, counted in the launch
+    AdamTensors<BITS> t;
     int count;
     uint32_t mix;
     const float* grad_scale;
     // what the formula takes, computed in 64 bits
     float b1, one_b1, b2, one_b2, decay, rate, inv_root_bc2, eps;
 };
-static_assert(sizeof(AdamArgs) <= 4096, "a launch's arguments");
+static_assert(sizeof(AdamArgs<32>) <= 4096 && sizeof(AdamArgs<8>) <= 4096, "a launch's arguments");
 
-int adamw_launch(const AdamArgs& a, int param_dt, int grad_dt, int state_bits, hipStream_t stream);
+template <int BITS>
+int adamw_launch(const AdamArgs<BITS>& a, uint32_t tiles, int param_dt, int grad_dt, hipStream_t stream);
 
 }  // namespace sdgp

@@ -61,12 +61,11 @@ __device__ __forceinline__ int scale_exponent(uint32_t top) {
 
 __device__ __forceinline__ float power_of_two(int k) { return bits_to_float((uint32_t)(k + 127) << 23); }
 
-// |x| / 2^k (`y`, at most 448) on the grid of e4m3, rounded up where u / 2^16 exceeds what is cut off.  From 2^-6 on the
-// code is the float's exponent and upper three mantissa bits, u added below them; the codes below are evenly spaced.
-__device__ __forceinline__ uint32_t to_code(float y, uint32_t u) {
-    const uint32_t upper = ((float_to_bits(y) + (u << 4)) >> 20) - 960u;                      // exponent bias 127 -> 7
-    const uint32_t lower = (uint32_t)fmaf(y, 512.0f, (float)u * 0x1p-16f);
-    return y < 0x1p-6f ? lower : upper;
+// |x| / 2^k, at most 448, on the grid of e4m3, rounded up where u / 2^16 exceeds what is cut off.  Another 120 off the
+// exponent, a float's exponent and upper three mantissa bits are the code, subnormal codes being where a float's subnormals
+// are; u is added below them.  (What lies under 2^-6 is rounded to 2^-20 of a code's step by that.)
+__device__ __forceinline__ uint32_t to_code(float x, int k, uint32_t u) {
+    return (float_to_bits(ldexpf(fabsf(x), -k - 120)) + (u << 4)) >> 20;
 }
 
 typedef uint32_t u32x2_half_aligned __attribute__((ext_vector_type(2), aligned(2), may_alias));
@@ -142,50 +141,58 @@ __device__ __forceinline__ void from_codes(uint32_t v, float scale, float (&f)[4
 
 // The codes of a block's four values a lane; KEEP: not negative, and what is not zero is not stored as zero.
 template <bool KEEP>
-__device__ __forceinline__ uint32_t to_codes(const float (&x)[4], const uint32_t (&u)[4], float* scale_at) {
+__device__ __forceinline__ uint32_t to_codes(float (&x)[4], const uint32_t (&u)[4], float* scale_at) {
     uint32_t most = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) most = max(most, float_to_bits(x[i]) & 0x7FFFFFFFu);
     uint32_t top = max_bits(most);
     const bool odd = top >= kInf;       // something infinite or NaN: the scale is that of the others
+    uint32_t spoilt = 0;                // the code of NaN in their places
     if (odd) {
         most = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const uint32_t b = float_to_bits(x[i]) & 0x7FFFFFFFu;
-            most = b < kInf ? max(most, b) : most;
+            if (b >= kInf) x[i] = 0.0f, spoilt |= 0x7Fu << (8 * i);
+            else most = max(most, b);
         }
         top = max_bits(most);
     }
     const int k = scale_exponent(top);
     if ((threadIdx.x & (kWave - 1)) == 0) *scale_at = power_of_two(k);
-    const float inv = power_of_two(-k);
     uint32_t codes = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const uint32_t b = float_to_bits(x[i]);
-        const float y = fabsf(x[i]) * inv;
-        uint32_t code = to_code(y, u[i]);
-        if constexpr (KEEP) code = max(code, min(float_to_bits(y), 1u));
+        uint32_t code = to_code(x[i], k, u[i]);
+        if constexpr (KEEP) code = max(code, min(b, 1u));
         else code |= (b >> 24) & 0x80u;
-        if (odd && (b & 0x7FFFFFFFu) >= kInf) code = 0x7Fu;
         codes |= code << (8 * i);
     }
-    return codes;
+    return codes | spoilt;   // a 0, whatever its random bits, is stored as 0
 }
 
 template <int PDT, int GDT, int BITS>
-__global__ void __launch_bounds__(kThreads) adamw_tiles(const AdamArgs a) {
-    int lo = 0, hi = a.count;                       // the tensor that holds this tile
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (a.first[mid] <= blockIdx.x) lo = mid;
-        else hi = mid;
-    }
-    const AdamTensor& t = a.t[lo];
+__global__ void __launch_bounds__(kThreads) adamw_tiles(const AdamArgs<BITS> a) {
+    using Tensors = AdamTensors<BITS>;
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
-    const int64_t block0 = (int64_t)(blockIdx.x - a.first[lo]) * kAdamTile + wave * kAtOnce, n = t.n;
+    // the last tensor that begins at this tile or before it; every lane compares one or two (a search would wait for each step)
+    int at = -1;
+#pragma unroll
+    for (int i = 0; i < Tensors::kMost; i += kWave) {
+        const int mine = i + lane < Tensors::kMost ? i + lane : Tensors::kMost - 1;
+        at += __builtin_popcountll(__ballot(i + lane < a.count && a.t.first[mine] <= blockIdx.x));
+    }
+    struct {
+        void* p;
+        const void* g;
+        void *m, *v;
+        uint16_t* copy;
+    } const t = {a.t.p[at], a.t.g[at], a.t.m[at], a.t.v[at], a.t.copy[at]};
+    const int64_t block0 = (int64_t)(blockIdx.x - a.t.first[at]) * kAdamTile + wave * kAtOnce, n = a.t.n[at];
     if (block0 * kAdamBlock >= n) return;
+    float *m_scale = nullptr, *v_scale = nullptr;
+    if constexpr (BITS == 8) m_scale = a.t.m_scale[at], v_scale = a.t.v_scale[at];
     const float gs = a.grad_scale ? *a.grad_scale : 1.0f;
 
     float p[kAtOnce][4], g[kAtOnce][4], m[kAtOnce][4], v[kAtOnce][4];
@@ -208,8 +215,8 @@ __global__ void __launch_bounds__(kThreads) adamw_tiles(const AdamArgs a) {
         const int64_t block = block0 + b, e = block * kAdamBlock + lane * 4;
         if (block * kAdamBlock >= n) break;
         if constexpr (BITS == 8) {
-            from_codes(mc[b], t.m_scale[block], m[b]);
-            from_codes(vc[b], t.v_scale[block], v[b]);
+            from_codes(mc[b], m_scale[block], m[b]);
+            from_codes(vc[b], v_scale[block], v[b]);
         }
         float r[4];
 #pragma unroll
@@ -219,7 +226,7 @@ __global__ void __launch_bounds__(kThreads) adamw_tiles(const AdamArgs a) {
             m[b][i] = add_rn(mul_rn(m[b][i], a.b1), mul_rn(gi, a.one_b1));
             v[b][i] = add_rn(mul_rn(v0, a.b2), mul_rn(mul_rn(gi, gi), a.one_b2));
             r[i] = sqrtf(v[b][i]);
-            p[b][i] = fmaf(p[b][i], a.decay, -a.rate * (m[b][i] / fmaf(r[i], a.inv_root_bc2, a.eps)));
+            p[b][i] = fmaf(p[b][i], a.decay, -a.rate * m[b][i] * __builtin_amdgcn_rcpf(fmaf(r[i], a.inv_root_bc2, a.eps)));
         }
         store4<PDT>(t.p, e, n, p[b]);
         if (PDT == SDGP_F32 && t.copy != nullptr) store4<SDGP_BF16>(t.copy, e, n, p[b]);
@@ -227,31 +234,32 @@ __global__ void __launch_bounds__(kThreads) adamw_tiles(const AdamArgs a) {
             store4<SDGP_F32>(t.m, e, n, m[b]);
             store4<SDGP_F32>(t.v, e, n, v[b]);
         } else {
-            const uint64_t at = (uint64_t)(t.block + block) * kAdamBlock;
-            const uint32_t row = hash_row(a.mix, (uint32_t)(at >> 32)), e32 = (uint32_t)at + lane * 4;
+            const uint64_t from = ((uint64_t)a.t.block[at] + block) * kAdamBlock;
+            const uint32_t row = hash_row(a.mix, (uint32_t)(from >> 32)), e32 = (uint32_t)from + lane * 4;
             uint32_t um[4], uv[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const uint32_t w = random_word(row, e32 + i);
                 um[i] = w & 0xFFFFu, uv[i] = w >> 16;
             }
-            store4_codes(t.m, e, n, to_codes<false>(m[b], um, t.m_scale + block));
-            store4_codes(t.v, e, n, to_codes<true>(r, uv, t.v_scale + block));
+            store4_codes(t.m, e, n, to_codes<false>(m[b], um, m_scale + block));
+            store4_codes(t.v, e, n, to_codes<true>(r, uv, v_scale + block));
         }
     }
 }
 
 }  // namespace
 
-int adamw_launch(const AdamArgs& a, int param_dt, int grad_dt, int state_bits, hipStream_t stream) {
-    const dim3 grid(a.first[a.count]), block(kThreads);
+template <int BITS>
+int adamw_launch(const AdamArgs<BITS>& a, uint32_t tiles, int param_dt, int grad_dt, hipStream_t stream) {
     const bool pb = param_dt == SDGP_BF16, gb = grad_dt == SDGP_BF16;
-    auto k = state_bits == 32 ? (pb ? (gb ? adamw_tiles<SDGP_BF16, SDGP_BF16, 32> : adamw_tiles<SDGP_BF16, SDGP_F32, 32>)
-                                    : (gb ? adamw_tiles<SDGP_F32, SDGP_BF16, 32> : adamw_tiles<SDGP_F32, SDGP_F32, 32>))
-                              : (pb ? (gb ? adamw_tiles<SDGP_BF16, SDGP_BF16, 8> : adamw_tiles<SDGP_BF16, SDGP_F32, 8>)
-                                    : (gb ? adamw_tiles<SDGP_F32, SDGP_BF16, 8> : adamw_tiles<SDGP_F32, SDGP_F32, 8>));
-    hipLaunchKernelGGL(k, grid, block, 0, stream, a);
+    auto k = pb ? (gb ? adamw_tiles<SDGP_BF16, SDGP_BF16, BITS> : adamw_tiles<SDGP_BF16, SDGP_F32, BITS>)
+                : (gb ? adamw_tiles<SDGP_F32, SDGP_BF16, BITS> : adamw_tiles<SDGP_F32, SDGP_F32, BITS>);
+    hipLaunchKernelGGL(k, dim3(tiles), dim3(kThreads), 0, stream, a);
     return launch_status();
 }
+
+template int adamw_launch<8>(const AdamArgs<8>& a, uint32_t tiles, int param_dt, int grad_dt, hipStream_t stream);
+template int adamw_launch<32>(const AdamArgs<32>& a, uint32_t tiles, int param_dt, int grad_dt, hipStream_t stream);
 
 }  // namespace sdgp

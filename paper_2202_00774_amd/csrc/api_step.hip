@@ -57,6 +57,64 @@ int check_norm(int64_t rows, int64_t D, int64_t groups, int dt, int wdt) {
     return groups < 0 || (groups > 0 && rows % groups != 0) ? SDGP_ERR_SHAPE : SDGP_OK;
 }
 
+struct AdamCall {
+    int count;
+    void* const* params;
+    const void* const* grads;
+    void* const* exp_avg;
+    void* const* exp_avg_sq;
+    float* const* exp_avg_scale;
+    float* const* exp_avg_sq_scale;
+    void* const* copies;
+    const int64_t* numel;
+    int param_dt, grad_dt;
+    hipStream_t stream;
+};
+
+// As many launches as the tensors fill.  A tensor longer than a launch counts goes in parts of whole tiles.
+template <int BITS>
+int adamw_launches(const AdamCall& c, sdgp::AdamArgs<BITS>& a) {
+    constexpr int64_t kTile = (int64_t)sdgp::kAdamTile * sdgp::kAdamBlock;
+    int64_t tiles = 0, block = 0;   // tiles of this launch; a tensor's first block, counted in the call
+    int k = 0;
+    const auto launch = [&] {
+        a.count = k;
+        const int rc = sdgp::adamw_launch<BITS>(a, (uint32_t)tiles, c.param_dt, c.grad_dt, c.stream);
+        tiles = 0, k = 0;
+        return rc;
+    };
+    for (int i = 0; i < c.count; ++i) {
+        for (int64_t from = 0; from < c.numel[i];) {
+            if (k == sdgp::AdamTensors<BITS>::kMost || tiles == sdgp::kAdamLaunch) {
+                const int rc = launch();
+                if (rc != SDGP_OK) return rc;
+            }
+            int64_t part = (sdgp::kAdamLaunch - tiles) * kTile;
+            part = part < sdgp::kAdamPart ? part : sdgp::kAdamPart;
+            part = part < c.numel[i] - from ? part : c.numel[i] - from;
+            auto& t = a.t;
+            t.p[k] = static_cast<char*>(c.params[i]) + from * element(c.param_dt);
+            t.g[k] = static_cast<const char*>(c.grads[i]) + from * element(c.grad_dt);
+            t.m[k] = static_cast<char*>(c.exp_avg[i]) + from * (BITS / 8);
+            t.v[k] = static_cast<char*>(c.exp_avg_sq[i]) + from * (BITS / 8);
+            t.copy[k] = c.copies ? static_cast<uint16_t*>(c.copies[i]) + from : nullptr;
+            t.n[k] = (uint32_t)part;
+            t.first[k] = (uint32_t)tiles;
+            if constexpr (BITS == 8) {
+                const int64_t at = from / sdgp::kAdamBlock;
+                t.m_scale[k] = c.exp_avg_scale[i] + at;
+                t.v_scale[k] = c.exp_avg_sq_scale[i] + at;
+                t.block[k] = (uint32_t)(block + at);
+            }
+            tiles += (part + kTile - 1) / kTile;
+            ++k;
+            from += part;
+        }
+        block += (c.numel[i] + sdgp::kAdamBlock - 1) / sdgp::kAdamBlock;
+    }
+    return k == 0 ? SDGP_OK : launch();
+}
+
 }  // namespace
 
 extern "C" {
@@ -173,46 +231,26 @@ int sdgp_adamw_step(int count, void* const* params, const void* const* grads, vo
         if (state_bits == 32 && (!aligned(exp_avg[i], 4) || !aligned(exp_avg_sq[i], 4))) return SDGP_ERR_SHAPE;
         if (state_bits == 8 && (!aligned(exp_avg_scale[i], 4) || !aligned(exp_avg_sq_scale[i], 4))) return SDGP_ERR_SHAPE;
     }
-    sdgp::AdamArgs a;
-    a.grad_scale = grad_scale;
-    a.b1 = (float)beta1, a.one_b1 = (float)(1.0 - beta1), a.b2 = (float)beta2, a.one_b2 = (float)(1.0 - beta2);
-    a.decay = (float)(1.0 - lr * weight_decay);
-    a.rate = (float)(lr / (1.0 - std::pow(beta1, (double)step)));
-    a.inv_root_bc2 = (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, (double)step)));
-    a.eps = (float)eps;
-    a.mix = sdgp::seed_mix(seed);
-    a.count = 0, a.first[0] = 0;
-    constexpr int64_t kTileElements = (int64_t)sdgp::kAdamTile * sdgp::kAdamBlock;
-    int64_t block = 0;   // first block of a tensor, counted in the call
-    for (int i = 0; i < count; ++i) {
-        // a tensor longer than a launch holds goes in parts, whole tiles each
-        for (int64_t from = 0; from < numel[i];) {
-            const int64_t room = sdgp::kAdamLaunch - a.first[a.count];
-            if (a.count == sdgp::kAdamTensors || room == 0) {
-                const int rc = sdgp::adamw_launch(a, param_dt, grad_dt, state_bits, static_cast<hipStream_t>(hip_stream));
-                if (rc != SDGP_OK) return rc;
-                a.count = 0;
-                continue;
-            }
-            const int64_t left = numel[i] - from, part = left < room * kTileElements ? left : room * kTileElements;
-            sdgp::AdamTensor& t = a.t[a.count];
-            const int64_t state = state_bits == 8 ? 1 : 4, at = from / sdgp::kAdamBlock;
-            t.p = static_cast<char*>(params[i]) + from * element(param_dt);
-            t.g = static_cast<const char*>(grads[i]) + from * element(grad_dt);
-            t.m = static_cast<char*>(exp_avg[i]) + from * state;
-            t.v = static_cast<char*>(exp_avg_sq[i]) + from * state;
-            t.m_scale = state_bits == 8 ? exp_avg_scale[i] + at : nullptr;
-            t.v_scale = state_bits == 8 ? exp_avg_sq_scale[i] + at : nullptr;
-            t.copy = copies ? static_cast<uint16_t*>(copies[i]) + from : nullptr;
-            t.n = part;
-            t.block = block + at;
-            a.first[a.count + 1] = a.first[a.count] + (uint32_t)((part + kTileElements - 1) / kTileElements);
-            ++a.count;
-            from += part;
-        }
-        block += (numel[i] + sdgp::kAdamBlock - 1) / sdgp::kAdamBlock;
+    const AdamCall c = {count, params, grads, exp_avg, exp_avg_sq, exp_avg_scale, exp_avg_sq_scale, copies, numel, param_dt, grad_dt,
+                        static_cast<hipStream_t>(hip_stream)};
+    const double bc1 = 1.0 - std::pow(beta1, (double)step), bc2 = 1.0 - std::pow(beta2, (double)step);
+    const auto rates = [&](auto& a) {
+        a.mix = sdgp::seed_mix(seed);
+        a.grad_scale = grad_scale;
+        a.b1 = (float)beta1, a.one_b1 = (float)(1.0 - beta1), a.b2 = (float)beta2, a.one_b2 = (float)(1.0 - beta2);
+        a.decay = (float)(1.0 - lr * weight_decay);
+        a.rate = (float)(lr / bc1);
+        a.inv_root_bc2 = (float)(1.0 / std::sqrt(bc2));
+        a.eps = (float)eps;
+    };
+    if (state_bits == 8) {
+        sdgp::AdamArgs<8> a;
+        rates(a);
+        return adamw_launches(c, a);
     }
-    return a.count == 0 ? SDGP_OK : sdgp::adamw_launch(a, param_dt, grad_dt, state_bits, static_cast<hipStream_t>(hip_stream));
+    sdgp::AdamArgs<32> a;
+    rates(a);
+    return adamw_launches(c, a);
 }
 
 }  // extern "C"
