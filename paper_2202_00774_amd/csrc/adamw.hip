@@ -72,15 +72,17 @@ typedef uint32_t u32x2_half_aligned __attribute__((ext_vector_type(2), aligned(2
 typedef uint32_t u32_any __attribute__((aligned(1), may_alias));
 
 // Four values of a lane: elements e .. e + 3 of a tensor of n.  What lies outside is 0 and is neither read nor written.
+// Everything passes by once a step, so loads and stores have the streaming hint (634 us without, 568 with it, for 24 x 8388608
+// elements in 8 bits; 157 and 137 for ResNet-50's tensors in fp32).
 template <int DT>
 __device__ __forceinline__ void load4(const void* p, int64_t e, int64_t n, float (&f)[4]) {
     if (e + 4 <= n) {
         if constexpr (DT == SDGP_BF16) {
-            const auto v = *reinterpret_cast<const u32x2_half_aligned*>(static_cast<const uint16_t*>(p) + e);
+            const auto v = __builtin_nontemporal_load(reinterpret_cast<const u32x2_half_aligned*>(static_cast<const uint16_t*>(p) + e));
 #pragma unroll
             for (int i = 0; i < 2; ++i) f[2 * i] = bits_to_float(v[i] << 16), f[2 * i + 1] = bits_to_float(v[i] & 0xFFFF0000u);
         } else {
-            const auto v = *reinterpret_cast<const u32x4_word_aligned*>(static_cast<const float*>(p) + e);
+            const auto v = __builtin_nontemporal_load(reinterpret_cast<const u32x4_word_aligned*>(static_cast<const float*>(p) + e));
 #pragma unroll
             for (int i = 0; i < 4; ++i) f[i] = bits_to_float(v[i]);
         }
@@ -98,10 +100,10 @@ __device__ __forceinline__ void store4(void* p, int64_t e, int64_t n, const floa
     if (e + 4 <= n) {
         if constexpr (DT == SDGP_BF16) {
             const u32x2_half_aligned v = {float2_to_bf16x2(f[0], f[1]), float2_to_bf16x2(f[2], f[3])};
-            *reinterpret_cast<u32x2_half_aligned*>(static_cast<uint16_t*>(p) + e) = v;
+            __builtin_nontemporal_store(v, reinterpret_cast<u32x2_half_aligned*>(static_cast<uint16_t*>(p) + e));
         } else {
             const u32x4_word_aligned v = {float_to_bits(f[0]), float_to_bits(f[1]), float_to_bits(f[2]), float_to_bits(f[3])};
-            *reinterpret_cast<u32x4_word_aligned*>(static_cast<float*>(p) + e) = v;
+            __builtin_nontemporal_store(v, reinterpret_cast<u32x4_word_aligned*>(static_cast<float*>(p) + e));
         }
     } else {
 #pragma unroll
@@ -115,7 +117,7 @@ __device__ __forceinline__ void store4(void* p, int64_t e, int64_t n, const floa
 
 __device__ __forceinline__ uint32_t load4_codes(const void* p, int64_t e, int64_t n) {
     const uint8_t* at = static_cast<const uint8_t*>(p) + e;
-    if (e + 4 <= n) return *reinterpret_cast<const u32_any*>(at);
+    if (e + 4 <= n) return __builtin_nontemporal_load(reinterpret_cast<const u32_any*>(at));
     uint32_t v = 0;
 #pragma unroll
     for (int i = 0; i < 3; ++i)
@@ -126,7 +128,7 @@ __device__ __forceinline__ uint32_t load4_codes(const void* p, int64_t e, int64_
 __device__ __forceinline__ void store4_codes(void* p, int64_t e, int64_t n, uint32_t v) {
     uint8_t* at = static_cast<uint8_t*>(p) + e;
     if (e + 4 <= n) {
-        *reinterpret_cast<u32_any*>(at) = v;
+        __builtin_nontemporal_store(v, reinterpret_cast<u32_any*>(at));
         return;
     }
 #pragma unroll

@@ -12,7 +12,6 @@ fp32 parameter and gradient.
 from __future__ import annotations
 
 import ctypes
-import operator
 
 import torch
 
@@ -21,17 +20,16 @@ from . import binding
 BLOCK = 256   # elements that share a scale
 
 
-def _pointers(tensors):
-    return (ctypes.c_void_p * len(tensors))(*map(torch.Tensor.data_ptr, tensors))
-
-
 def _check(tensors, name: str, dtype=None):
-    """One dtype, one GPU, contiguous; returns the dtype."""
-    for t in tensors:
-        binding._dev(t, name)
-        if t.dtype != (dtype or tensors[0].dtype) or t.device != tensors[0].device:
-            raise ValueError(f"{name} must have one dtype and one device")
-    return tensors[0].dtype if tensors else torch.float32
+    """One dtype (this one, where it is given), one GPU, contiguous; returns the dtype."""
+    if not all(map(torch.Tensor.is_contiguous, tensors)):
+        raise ValueError(f"{name} must be contiguous")
+    if tensors and min(map(torch.Tensor.get_device, tensors)) < 0:
+        raise ValueError(f"{name} must live on the GPU")
+    dtypes = {t.dtype for t in tensors}
+    if len(dtypes | ({dtype} if dtype else set())) > 1 or len(set(map(torch.Tensor.get_device, tensors))) > 1:
+        raise ValueError(f"{name} must have one dtype{f' ({dtype})' if dtype else ''} and one device")
+    return next(iter(dtypes), torch.float32)
 
 
 class AdamW:
@@ -49,40 +47,51 @@ class AdamW:
         self.copies = None if copies is None else list(copies)
         self.lr, self.betas, self.eps, self.weight_decay = lr, tuple(betas), eps, weight_decay
         self.state_bits, self.seed, self.steps = state_bits, int(seed), int(steps)
-        dtype = _check(self.params, "params")
+        self._dtype = _check(self.params, "params")
         self._param_dt = binding._dtype_code(self.params[0]) if self.params else binding.F32
-        if self.copies is not None:
-            if dtype != torch.float32:
-                raise ValueError("copies are for fp32 params")
-            self._same(self.copies, "copies", torch.bfloat16)
         self._numel, self._shapes = [p.numel() for p in self.params], [p.shape for p in self.params]
+        self._counts = (ctypes.c_int64 * len(self.params))(*self._numel)
+        if self.copies is not None and self._dtype != torch.float32:
+            raise ValueError("copies are for fp32 params")
         if state is None:
             state = self._zeros()
         names = ("exp_avg", "exp_avg_sq") + (("exp_avg_scale", "exp_avg_sq_scale") if state_bits == 8 else ())
         if set(state) != set(names):
             raise ValueError(f"state holds {', '.join(names)}")
         self._state = {k: list(state[k]) for k in names}
-        for k in names[:2]:
-            self._same(self._state[k], k, torch.float32 if state_bits == 32 else torch.float8_e4m3fn)
-        for k in names[2:]:
-            _check(self._state[k], k, torch.float32)
-            if [t.numel() for t in self._state[k]] != [-(-n // BLOCK) for n in self._numel]:
-                raise ValueError(f"{k} holds one value for each {BLOCK} elements of every param")
-        # the tensors are held here, so their addresses stay; the params' are looked at again in every step
-        self._counts = (ctypes.c_int64 * len(self.params))(*self._numel)
-        self._arrays = {k: _pointers(v) for k, v in self._state.items()}
-        self._copy_array = None if self.copies is None else _pointers(self.copies)
+        # the tensors' addresses, and the array made of them: looked at in every step, the tensors checked when one has moved
+        self._arrays = {}
+        for k in ("params", "copies", *names):
+            self._array(k)
 
-    def _same(self, tensors, name: str, dtype):
-        _check(tensors, name, dtype)
-        if [t.shape for t in tensors] != [p.shape for p in self.params] or any(map(operator.ne, map(torch.Tensor.get_device, tensors), map(torch.Tensor.get_device, self.params))):
-            raise ValueError(f"{name} must have the shapes and the device of params")
+    def _array(self, name: str):
+        tensors = self._state[name] if name in self._state else getattr(self, name)
+        if tensors is None:
+            return None
+        now = list(map(torch.Tensor.data_ptr, tensors))
+        seen = self._arrays.get(name)
+        if seen is None or seen[0] != now:
+            self._check_list(name, tensors)
+            seen = self._arrays[name] = (now, (ctypes.c_void_p * len(now))(*now))
+        return seen[1]
+
+    def _check_list(self, name: str, tensors) -> None:
+        scales = name.endswith("_scale")
+        _check(tensors, name, {"params": self._dtype, "copies": torch.bfloat16}.get(name) or
+               (torch.float32 if scales or self.state_bits == 32 else torch.float8_e4m3fn))
+        if scales and [t.numel() for t in tensors] != [-(-n // BLOCK) for n in self._numel]:
+            raise ValueError(f"{name} holds one value for each {BLOCK} elements of every param")
+        if not scales and [t.shape for t in tensors] != self._shapes:
+            raise ValueError(f"{name} must have the shapes of params")
+        if tensors and tensors[0].get_device() != self.params[0].get_device():
+            raise ValueError(f"{name} must live on the GPU of params")
 
     def _zeros(self):
-        of = torch.float32 if self.state_bits == 32 else torch.float8_e4m3fn
-        # (zeros of the code's bytes: e4m3 zero is the byte 0)
-        zeros = lambda: [torch.zeros(p.shape, dtype=torch.float32 if self.state_bits == 32 else torch.uint8, device=p.device).view(of)  # noqa: E731
-                         for p in self.params]
+        def zeros():
+            if self.state_bits == 32:
+                return [torch.zeros_like(p, dtype=torch.float32, memory_format=torch.contiguous_format) for p in self.params]
+            return [torch.zeros(p.shape, dtype=torch.uint8, device=p.device).view(torch.float8_e4m3fn) for p in self.params]   # e4m3's 0 is 0
+
         state = {"exp_avg": zeros(), "exp_avg_sq": zeros()}
         if self.state_bits == 8:
             for k in ("exp_avg_scale", "exp_avg_sq_scale"):
@@ -111,12 +120,13 @@ class AdamW:
         if grad_scale is not None and (grad_scale.get_device() != device or grad_scale.dtype != torch.float32 or grad_scale.numel() != 1):
             raise ValueError("grad_scale must be one float32 on the params' GPU")
         step = self.steps + 1
-        a = self._arrays
+        array = self._array
         rc = binding.load().sdgp_adamw_step(
-            len(grads), _pointers(self.params), _pointers(grads), a["exp_avg"], a["exp_avg_sq"], a.get("exp_avg_scale"),
-            a.get("exp_avg_sq_scale"), self._copy_array, self._counts, self._param_dt, binding._dtype_code(grads[0]),
-            self.state_bits, self.lr, *self.betas, self.eps, self.weight_decay, step, binding._ptr(grad_scale),
-            (self.seed + step) & (2**64 - 1), binding._stream(grads[0]))
+            len(grads), array("params"), (ctypes.c_void_p * len(grads))(*map(torch.Tensor.data_ptr, grads)), array("exp_avg"),
+            array("exp_avg_sq"), array("exp_avg_scale") if self.state_bits == 8 else None,
+            array("exp_avg_sq_scale") if self.state_bits == 8 else None, array("copies"), self._counts, self._param_dt,
+            binding._dtype_code(grads[0]), self.state_bits, self.lr, *self.betas, self.eps, self.weight_decay, step,
+            binding._ptr(grad_scale), (self.seed + step) & (2**64 - 1), binding._stream(grads[0]))
         if rc != 0:
             raise binding.SdgpError(rc, "sdgp_adamw_step")
         self.steps = step
