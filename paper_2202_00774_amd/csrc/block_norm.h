@@ -57,15 +57,20 @@ inline bool rows_aligned(int64_t D, int dt, std::initializer_list<const void*> t
 inline bool rows_large(int64_t rows, int64_t D, int dt) { return rows * D * (dt == SDGP_BF16 ? 2 : 4) > ((int64_t)128 << 20); }
 
 // Threads a row and 16-byte vectors a thread, for rows that fit the registers: one vector each, from 16 lanes to 1024
-// threads, two above that.  (Two vectors and half the threads: 331 us against 301 at 8192 x 8192 bf16, 92 against 77 at
-// 4096 x 4096, both directions.) 0 threads: the row is longer (above 16384 bf16 or 8192 fp32 values).
+// threads, two above that.  Loads in flight bound these kernels, so idle lanes count: with 192, 384 and 768 threads beside the
+// powers of two 30000 x 1104 bf16 takes 169 us instead of 190, 16384 x 2560 156 instead of 172, both directions.  (Two vectors
+// and half the threads: 331 us against 301 at 8192 x 8192, 92 against 77 at 4096 x 4096.)  0 threads: the row is longer (above
+// 16384 bf16 or 8192 fp32 values).
 struct RowShape {
     int threads, vecs;
 };
 
+// Rows that a workgroup (of 256 threads, or a row's) works on at a time.
+constexpr int rows_at_once(int threads) { return threads < 192 ? 256 / threads : 1; }
+
 inline RowShape row_shape(int64_t D, int dt) {
     const int64_t vecs = (D + (dt == SDGP_BF16 ? 7 : 3)) / (dt == SDGP_BF16 ? 8 : 4);
-    for (const RowShape s : {RowShape{16, 1}, {32, 1}, {64, 1}, {128, 1}, {256, 1}, {512, 1}, {1024, 1}, {1024, 2}})
+    for (const RowShape s : {RowShape{16, 1}, {32, 1}, {64, 1}, {128, 1}, {192, 1}, {256, 1}, {384, 1}, {512, 1}, {768, 1}, {1024, 1}, {1024, 2}})
         if (vecs <= s.threads * s.vecs) return s;
     return {0, 0};
 }

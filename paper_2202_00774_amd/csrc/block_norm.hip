@@ -246,17 +246,18 @@ int block_norm_bwd_no_rows(void* dgate, int64_t gate_elements, int dt, float* dw
     return SDGP_OK;
 }
 
-// A slab costs its columns' sums written and read again, so it holds four rows for each that a workgroup has in hand,
-// unless that leaves fewer than 256 workgroups, one a CU; more than 1024 hide no more latency (4099 x 1001 fp32: 76 us
-// with eight rows each, 63 with four).  Gates of up to 32 rows
-// that are many (2048) are finished by the slab that holds them.
+// A slab costs its columns' sums written and read again, so it holds four rows for each that a workgroup has in hand (4099
+// x 1001 fp32: 76 us with eight rows each, 63 with four), unless that leaves fewer than 256 workgroups, one a CU; nor are
+// there more than a CU holds at 16 wavefronts.  Gates of up to 32 rows that are many (2048) are finished by the slab that
+// holds them.
 static Slabs make_slabs(int64_t rows, int64_t D, int64_t groups, int dt) {
     const RowShape shape = row_shape(D, dt);
-    const int64_t at_once = shape.threads == 0 || shape.threads >= 256 ? 1 : 256 / shape.threads;
+    const int64_t at_once = shape.threads == 0 ? 1 : rows_at_once(shape.threads);
     const int64_t g = groups > 0 ? groups : 1, per_gate = rows / g;
     Slabs s;
     int64_t want = rows / (4 * at_once);
-    want = want < 256 ? 256 : want > 1024 ? 1024 : want;
+    const int64_t waves = shape.threads == 0 ? kBlock / kWave : shape.threads * at_once / kWave, most = 256 * (waves >= 16 ? 1 : 16 / waves);
+    want = want < 256 ? 256 : want > most ? most : want;
     if (groups > 0 && (per_gate == 1 || (per_gate <= 32 && groups >= 2048))) {
         s.kind = kWholeGroups;
         s.len = ((groups + want - 1) / want + at_once - 1) / at_once * at_once;
@@ -265,8 +266,8 @@ static Slabs make_slabs(int64_t rows, int64_t D, int64_t groups, int dt) {
     } else {
         s.kind = kInGroup;
         int64_t parts = want / g;
-        const int64_t most = (per_gate + at_once - 1) / at_once;
-        parts = parts < 1 ? 1 : parts > most ? most : parts;
+        const int64_t steps = (per_gate + at_once - 1) / at_once;
+        parts = parts < 1 ? 1 : parts > steps ? steps : parts;
         s.len = ((per_gate + parts - 1) / parts + at_once - 1) / at_once * at_once;
         s.parts = (per_gate + s.len - 1) / s.len;
         s.count = s.parts * g;

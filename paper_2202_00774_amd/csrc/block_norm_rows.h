@@ -15,7 +15,7 @@ namespace sdgp {
 namespace {
 
 template <int T>
-constexpr int norm_block() { return T < 256 ? 256 : T; }
+constexpr int norm_block() { return T * rows_at_once(T); }
 
 template <int DT, int T, int NV, bool BLOCK>
 __global__ void __launch_bounds__(norm_block<T>()) norm_fwd(const Norm n, int64_t rows_per_wg) {
@@ -325,25 +325,26 @@ __global__ void __launch_bounds__(norm_block<T>()) norm_bwd(const NormGrad n) {
 
 template <int DT>
 int norm_rows_launch(const Norm& n, RowShape shape, hipStream_t stream) {
-    const int R = shape.threads < 256 ? 256 / shape.threads : 1;
+    const int R = rows_at_once(shape.threads);
     // workgroups that are there at once, about; each keeps the weights in registers over its rows
-    const int64_t most = shape.threads <= 256 ? 2048 : shape.threads == 512 ? 1024 : 512;
+    const int64_t most = shape.threads <= 256 ? 2048 : shape.threads <= 512 ? 1024 : 512;
     const int64_t groups = (n.rows + R - 1) / R, per = (groups + most - 1) / most * R;
-    const dim3 grid((unsigned)((n.rows + per - 1) / per)), block(shape.threads < 256 ? 256 : shape.threads);
+    const dim3 grid((unsigned)((n.rows + per - 1) / per)), block(shape.threads * rows_at_once(shape.threads));
 #define SDGP_CASE(T, NV)                                                                                              \
     if (shape.threads == T && shape.vecs == NV) {                                                                     \
         if (n.u != nullptr) hipLaunchKernelGGL((norm_fwd<DT, T, NV, true>), grid, block, 0, stream, n, per);          \
         else hipLaunchKernelGGL((norm_fwd<DT, T, NV, false>), grid, block, 0, stream, n, per);                        \
         return launch_status();                                                                                       \
     }
-    SDGP_CASE(16, 1) SDGP_CASE(32, 1) SDGP_CASE(64, 1) SDGP_CASE(128, 1) SDGP_CASE(256, 1) SDGP_CASE(512, 1) SDGP_CASE(1024, 1) SDGP_CASE(1024, 2)
+    SDGP_CASE(16, 1) SDGP_CASE(32, 1) SDGP_CASE(64, 1) SDGP_CASE(128, 1) SDGP_CASE(192, 1) SDGP_CASE(256, 1) SDGP_CASE(384, 1)
+    SDGP_CASE(512, 1) SDGP_CASE(768, 1) SDGP_CASE(1024, 1) SDGP_CASE(1024, 2)
 #undef SDGP_CASE
     return SDGP_ERR_SHAPE;
 }
 
 template <int DT>
 int norm_grad_launch(const NormGrad& n, RowShape shape, hipStream_t stream) {
-    const dim3 grid((unsigned)n.slabs.count), block(shape.threads < 256 ? 256 : shape.threads);
+    const dim3 grid((unsigned)n.slabs.count), block(shape.threads * rows_at_once(shape.threads));
 #define SDGP_CASE(T, NV)                                                                                              \
     if (shape.threads == T && shape.vecs == NV) {                                                                     \
         if (n.u == nullptr) hipLaunchKernelGGL((norm_bwd<DT, T, NV, kNoBlock>), grid, block, 0, stream, n);           \
@@ -351,7 +352,8 @@ int norm_grad_launch(const NormGrad& n, RowShape shape, hipStream_t stream) {
         else hipLaunchKernelGGL((norm_bwd<DT, T, NV, kWholeGroups>), grid, block, 0, stream, n);                      \
         return launch_status();                                                                                       \
     }
-    SDGP_CASE(16, 1) SDGP_CASE(32, 1) SDGP_CASE(64, 1) SDGP_CASE(128, 1) SDGP_CASE(256, 1) SDGP_CASE(512, 1) SDGP_CASE(1024, 1) SDGP_CASE(1024, 2)
+    SDGP_CASE(16, 1) SDGP_CASE(32, 1) SDGP_CASE(64, 1) SDGP_CASE(128, 1) SDGP_CASE(192, 1) SDGP_CASE(256, 1) SDGP_CASE(384, 1)
+    SDGP_CASE(512, 1) SDGP_CASE(768, 1) SDGP_CASE(1024, 1) SDGP_CASE(1024, 2)
 #undef SDGP_CASE
     return SDGP_ERR_SHAPE;
 }

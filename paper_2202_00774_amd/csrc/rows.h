@@ -163,7 +163,7 @@ __device__ __forceinline__ float sum32(float v) {
 // above that the wavefronts meet in `lds` (row_lds floats), which the calls take in turn (`turn` flips), so one
 // barrier a call is enough: a wavefront can be at most one call ahead of another.  All threads of the workgroup call it.
 template <int T, int K>
-constexpr int row_lds() { return T > 64 ? 2 * K * (T < 256 ? 4 : T / 64) : 1; }
+constexpr int row_lds() { return T > 64 ? 2 * K * (T < 192 ? 4 : T / 64) : 1; }
 
 template <int T, int K>
 __device__ __forceinline__ void row_sums(float (&v)[K], float* lds, int& turn) {

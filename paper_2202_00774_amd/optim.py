@@ -20,6 +20,10 @@ from . import binding
 BLOCK = 256   # elements that share a scale
 
 
+def _array(addresses):
+    return (ctypes.c_void_p * len(addresses))(*addresses)
+
+
 def _check(tensors, name: str, dtype=None):
     """One dtype (this one, where it is given), one GPU, contiguous; returns the dtype."""
     if not all(map(torch.Tensor.is_contiguous, tensors)):
@@ -58,21 +62,25 @@ class AdamW:
         names = ("exp_avg", "exp_avg_sq") + (("exp_avg_scale", "exp_avg_sq_scale") if state_bits == 8 else ())
         if set(state) != set(names):
             raise ValueError(f"state holds {', '.join(names)}")
-        self._state = {k: list(state[k]) for k in names}
-        # the tensors' addresses, and the array made of them: looked at in every step, the tensors checked when one has moved
-        self._arrays = {}
-        for k in ("params", "copies", *names):
-            self._array(k)
+        # The states are aliases that nobody else holds, so they stay where they are.  Params and copies are the caller's, who may
+        # give them new storage: their addresses are looked at in every step, and the tensors checked when one has moved.
+        self._state = {k: [t.detach() for t in state[k]] for k in names}
+        for k in names:
+            self._check_list(k, self._state[k])
+        self._state_arrays = [_array([t.data_ptr() for t in self._state[k]]) for k in names] + [None] * (4 - len(names))
+        self._seen = {}
+        for k in ("params", "copies"):
+            self._addresses(k)
 
-    def _array(self, name: str):
-        tensors = self._state[name] if name in self._state else getattr(self, name)
+    def _addresses(self, name: str):
+        tensors = getattr(self, name)
         if tensors is None:
             return None
         now = list(map(torch.Tensor.data_ptr, tensors))
-        seen = self._arrays.get(name)
+        seen = self._seen.get(name)
         if seen is None or seen[0] != now:
             self._check_list(name, tensors)
-            seen = self._arrays[name] = (now, (ctypes.c_void_p * len(now))(*now))
+            seen = self._seen[name] = (now, _array(now))
         return seen[1]
 
     def _check_list(self, name: str, tensors) -> None:
@@ -99,8 +107,8 @@ class AdamW:
         return state
 
     def state(self) -> dict:
-        """The state's own tensors by name, a list each in the order of the params."""
-        return dict(self._state)
+        """The state by name, a list of tensors each in the order of the params; they share the optimizer's memory."""
+        return {k: [t.detach() for t in v] for k, v in self._state.items()}
 
     def step(self, grads=None, *, grad_scale: torch.Tensor | None = None) -> None:
         """One step from ``grads`` (one dtype, fp32 or bf16; default: every param's ``.grad``).  ``grad_scale``: an fp32
@@ -120,13 +128,12 @@ class AdamW:
         if grad_scale is not None and (grad_scale.get_device() != device or grad_scale.dtype != torch.float32 or grad_scale.numel() != 1):
             raise ValueError("grad_scale must be one float32 on the params' GPU")
         step = self.steps + 1
-        array = self._array
+        m, v, m_scale, v_scale = self._state_arrays
         rc = binding.load().sdgp_adamw_step(
-            len(grads), array("params"), (ctypes.c_void_p * len(grads))(*map(torch.Tensor.data_ptr, grads)), array("exp_avg"),
-            array("exp_avg_sq"), array("exp_avg_scale") if self.state_bits == 8 else None,
-            array("exp_avg_sq_scale") if self.state_bits == 8 else None, array("copies"), self._counts, self._param_dt,
-            binding._dtype_code(grads[0]), self.state_bits, self.lr, *self.betas, self.eps, self.weight_decay, step,
-            binding._ptr(grad_scale), (self.seed + step) & (2**64 - 1), binding._stream(grads[0]))
+            len(grads), self._addresses("params"), _array(list(map(torch.Tensor.data_ptr, grads))), m, v, m_scale, v_scale,
+            self._addresses("copies"), self._counts, self._param_dt, binding._dtype_code(grads[0]), self.state_bits, self.lr,
+            *self.betas, self.eps, self.weight_decay, step, binding._ptr(grad_scale), (self.seed + step) & (2**64 - 1),
+            binding._stream(grads[0]))
         if rc != 0:
             raise binding.SdgpError(rc, "sdgp_adamw_step")
         self.steps = step
