@@ -17,17 +17,18 @@ namespace {
 template <int T>
 constexpr int norm_block() { return T * rows_at_once(T); }
 
-template <int DT, int T, int NV, bool BLOCK>
+template <int DT, int T, int NV, bool BLOCK, Caching RESULTS>
 __global__ void __launch_bounds__(norm_block<T>()) norm_fwd(const Norm n, int64_t rows_per_wg) {
     using V = RowVec<DT>;
     constexpr int N = V::kN, R = norm_block<T>() / T;
+    constexpr bool kTurns = RESULTS == kStream;   // large tensors: rows in turn
     constexpr int64_t kSize = sizeof(typename V::Elem);
     __shared__ float lds[row_lds<T, 1>()];
     int turn = 0;
     const int t = threadIdx.x % T, sub = threadIdx.x / T;
     // rows in turn, or a run of them
-    const int64_t first = (int64_t)blockIdx.x * (n.large ? R : rows_per_wg), step = n.large ? (int64_t)gridDim.x * R : R;
-    const int64_t end = n.large || first + rows_per_wg > n.rows ? n.rows : first + rows_per_wg;
+    const int64_t first = (int64_t)blockIdx.x * (kTurns ? R : rows_per_wg), step = kTurns ? (int64_t)gridDim.x * R : R;
+    const int64_t end = kTurns || first + rows_per_wg > n.rows ? n.rows : first + rows_per_wg;
     const float inv_d = 1.0f / (float)n.D;
 
     float post[NV][N], pre[NV][N];
@@ -86,7 +87,7 @@ __global__ void __launch_bounds__(norm_block<T>()) norm_fwd(const Norm n, int64_
                     y[i] = add_rn(mul_rn(n.residual_scale, x[v].get(i)), a);
                 }
                 x[v].set(y);   // y from here on, rounded as it is stored
-                store_row<DT>(static_cast<char*>(n.y) + at, (v * T + t) * N, D, x[v], n.large);
+                store_row<DT, RESULTS>(static_cast<char*>(n.y) + at, (v * T + t) * N, D, x[v]);
             }
             if (n.h == nullptr) continue;
         }
@@ -105,7 +106,7 @@ __global__ void __launch_bounds__(norm_block<T>()) norm_fwd(const Norm n, int64_
             for (int i = 0; i < N; ++i) h[i] = x[v].get(i) * ry * pre[v][i];
             V q;
             q.set(h);
-            store_row<DT>(static_cast<char*>(n.h) + at, (v * T + t) * N, D, q, n.large);
+            store_row<DT, RESULTS>(static_cast<char*>(n.h) + at, (v * T + t) * N, D, q);
         }
     }
 }
@@ -144,11 +145,11 @@ __device__ __forceinline__ void load(Row<DT, NV>& row, const NormGrad& n, int64_
 // MODE: kNoBlock, or how the slab is cut.
 constexpr int kNoBlock = 2;
 
-template <int DT, int T, int NV, int MODE>
+template <int DT, int T, int NV, int MODE, Caching RESULTS>
 __global__ void __launch_bounds__(norm_block<T>()) norm_bwd(const NormGrad n) {
     using V = RowVec<DT>;
     constexpr int N = V::kN, R = norm_block<T>() / T, kColumns = T * NV * N;
-    constexpr bool BLOCK = MODE != kNoBlock;
+    constexpr bool BLOCK = MODE != kNoBlock, kTurns = RESULTS == kStream;
     constexpr int64_t kSize = sizeof(typename V::Elem);
     __shared__ float lds[R > 1 ? R * kColumns : row_lds<T, 3>()];
     int turn = 0;
@@ -204,11 +205,11 @@ __global__ void __launch_bounds__(norm_block<T>()) norm_bwd(const NormGrad n) {
         };
         int64_t first = q * n.per_gate, end = first + n.per_gate;
         if constexpr (MODE != kWholeGroups) {
-            first += (int64_t)(blockIdx.x - gate0 * n.slabs.parts) * (n.large ? R : n.slabs.len);
-            if (!n.large && first + n.slabs.len < end) end = first + n.slabs.len;
+            first += (int64_t)(blockIdx.x - gate0 * n.slabs.parts) * (kTurns ? R : n.slabs.len);
+            if (!kTurns && first + n.slabs.len < end) end = first + n.slabs.len;
         }
         const int64_t rows = MODE == kWholeGroups ? n.per_gate : end - first;   // the same for all threads
-        const int64_t step = MODE == kWholeGroups ? 1 : n.large ? R * n.slabs.parts : R;
+        const int64_t step = MODE == kWholeGroups ? 1 : kTurns ? R * n.slabs.parts : R;
         for (int64_t i0 = 0; i0 < rows; i0 += step) {
             const int64_t r = first + i0 + (MODE == kWholeGroups ? 0 : sub);
             const int D = mine && r < end ? n.D : 0;
@@ -263,10 +264,10 @@ __global__ void __launch_bounds__(norm_block<T>()) norm_bwd(const NormGrad n) {
                 }
                 V o;
                 o.set(dx);
-                store_row<DT>(static_cast<char*>(n.dx) + at, e, D, o, n.large);
+                store_row<DT, RESULTS>(static_cast<char*>(n.dx) + at, e, D, o);
                 if constexpr (BLOCK) {
                     o.set(du);
-                    store_row<DT>(static_cast<char*>(n.du) + at, e, D, o, n.large);
+                    store_row<DT, RESULTS>(static_cast<char*>(n.du) + at, e, D, o);
                 }
             }
         }
@@ -332,8 +333,9 @@ int norm_rows_launch(const Norm& n, RowShape shape, hipStream_t stream) {
     const dim3 grid((unsigned)((n.rows + per - 1) / per)), block(shape.threads * rows_at_once(shape.threads));
 #define SDGP_CASE(T, NV)                                                                                              \
     if (shape.threads == T && shape.vecs == NV) {                                                                     \
-        if (n.u != nullptr) hipLaunchKernelGGL((norm_fwd<DT, T, NV, true>), grid, block, 0, stream, n, per);          \
-        else hipLaunchKernelGGL((norm_fwd<DT, T, NV, false>), grid, block, 0, stream, n, per);                        \
+        auto kernel = n.u != nullptr ? (n.large ? norm_fwd<DT, T, NV, true, kStream> : norm_fwd<DT, T, NV, true, kKeep>)     \
+                                     : (n.large ? norm_fwd<DT, T, NV, false, kStream> : norm_fwd<DT, T, NV, false, kKeep>);  \
+        hipLaunchKernelGGL(kernel, grid, block, 0, stream, n, per);                                                   \
         return launch_status();                                                                                       \
     }
     SDGP_CASE(16, 1) SDGP_CASE(32, 1) SDGP_CASE(64, 1) SDGP_CASE(128, 1) SDGP_CASE(192, 1) SDGP_CASE(256, 1) SDGP_CASE(384, 1)
@@ -347,9 +349,12 @@ int norm_grad_launch(const NormGrad& n, RowShape shape, hipStream_t stream) {
     const dim3 grid((unsigned)n.slabs.count), block(shape.threads * rows_at_once(shape.threads));
 #define SDGP_CASE(T, NV)                                                                                              \
     if (shape.threads == T && shape.vecs == NV) {                                                                     \
-        if (n.u == nullptr) hipLaunchKernelGGL((norm_bwd<DT, T, NV, kNoBlock>), grid, block, 0, stream, n);           \
-        else if (n.slabs.kind == kInGroup) hipLaunchKernelGGL((norm_bwd<DT, T, NV, kInGroup>), grid, block, 0, stream, n); \
-        else hipLaunchKernelGGL((norm_bwd<DT, T, NV, kWholeGroups>), grid, block, 0, stream, n);                      \
+        const auto pick = [&](auto results) {                                                                         \
+            constexpr Caching C = decltype(results)::value;                                                           \
+            return n.u == nullptr ? norm_bwd<DT, T, NV, kNoBlock, C>                                                  \
+                   : n.slabs.kind == kInGroup ? norm_bwd<DT, T, NV, kInGroup, C> : norm_bwd<DT, T, NV, kWholeGroups, C>; \
+        };                                                                                                            \
+        hipLaunchKernelGGL((n.large ? pick(Cached<kStream>{}) : pick(Cached<kKeep>{})), grid, block, 0, stream, n);   \
         return launch_status();                                                                                       \
     }
     SDGP_CASE(16, 1) SDGP_CASE(32, 1) SDGP_CASE(64, 1) SDGP_CASE(128, 1) SDGP_CASE(192, 1) SDGP_CASE(256, 1) SDGP_CASE(384, 1)

@@ -43,7 +43,8 @@ typedef uint32_t u32x4_word_aligned __attribute__((ext_vector_type(4), aligned(4
 template <int DT>
 using Unaligned16 = typename std::conditional<DT == SDGP_BF16, u32x4_half_aligned, u32x4_word_aligned>::type;
 
-// kStream: the line is not needed again soon (a hint to the caches).
+// kStream: the line is not needed again soon (a hint to the caches).  A template argument: of two stores that a flag
+// chooses between, alike but for the hint, the compiler makes one without it.
 enum Caching { kKeep, kStream };
 template <Caching C>
 using Cached = std::integral_constant<Caching, C>;
@@ -73,8 +74,8 @@ __device__ __forceinline__ RowVec<DT> load_row(const void* row, int e, int n, ui
     return u.r;
 }
 
-template <int DT>
-__device__ __forceinline__ void store_row(void* row, int e, int n, const RowVec<DT>& r, bool stream = false) {
+template <int DT, Caching CACHING = kKeep>
+__device__ __forceinline__ void store_row(void* row, int e, int n, const RowVec<DT>& r) {
     constexpr int N = RowVec<DT>::kN;
     union {
         RowVec<DT> r;
@@ -88,7 +89,7 @@ __device__ __forceinline__ void store_row(void* row, int e, int n, const RowVec<
 #pragma unroll
         for (int i = 0; i < 4; ++i) q[i] = u.w[i];
         auto* at = reinterpret_cast<Unaligned16<DT>*>(p);
-        if (stream) __builtin_nontemporal_store(q, at);
+        if constexpr (CACHING == kStream) __builtin_nontemporal_store(q, at);
         else *at = q;
     } else {
 #pragma unroll

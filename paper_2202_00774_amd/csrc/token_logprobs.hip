@@ -235,7 +235,7 @@ __device__ __forceinline__ void add_chunk(Sums& t, const float (&x)[kAtOnce][N],
     t.a += a[0];
 }
 
-template <int DT, bool TOP>
+template <int DT, bool TOP, Caching LOGITS>
 __device__ __forceinline__ void scan(const void* row, int64_t first, int64_t stride, int end, float c, int top, Sums& t, Best& best,
                                      Bounds* bounds, int wave) {
     using V = RowVec<DT>;
@@ -276,7 +276,7 @@ __device__ __forceinline__ void scan(const void* row, int64_t first, int64_t str
             const char* from = static_cast<const char*>(row) + at * (int64_t)sizeof(typename V::Elem);   // the same for all lanes
 #pragma unroll
             for (int u = 0; u < kAtOnce; ++u)
-                v[u] = load_row<DT>(from + u * stride * (int64_t)sizeof(typename V::Elem), lane * N, INT32_MAX);
+                v[u] = load_row<DT, LOGITS>(from + u * stride * (int64_t)sizeof(typename V::Elem), lane * N, INT32_MAX);
         };
         load(e);
         for (; e <= last; e += step)
@@ -306,6 +306,7 @@ struct Logprobs {
     int pieces, piece;
     Sums* part_sums;   // [rows, pieces]
     Best* part_best;   // [rows, pieces, top]
+    bool stream;
 };
 
 // Results of row r from one wavefront's sums and list.
@@ -350,7 +351,7 @@ __device__ __forceinline__ void join_waves(Sums& t, Best& best, float c, Sums* p
 }
 
 // T = 64: a wavefront a row; 256: a workgroup a row, or a piece of one.
-template <int DT, int T, bool TOP>
+template <int DT, int T, bool TOP, Caching LOGITS>
 __global__ void __launch_bounds__(kBlock) logprob_rows(const Logprobs q) {
     constexpr int N = RowVec<DT>::kN, R = kBlock / T;
     __shared__ Sums part[T > kWave ? kBlock / kWave : 1];
@@ -373,7 +374,7 @@ __global__ void __launch_bounds__(kBlock) logprob_rows(const Logprobs q) {
             if (threadIdx.x == 0) bounds.least = -INFINITY;
             __syncthreads();
         }
-        scan<DT, TOP>(row, begin + (T == kWave ? 0 : wave * kWave * N), (int64_t)T * N, end, c, q.top, t, best, T > kWave ? &bounds : nullptr, wave);
+        scan<DT, TOP, LOGITS>(row, begin + (T == kWave ? 0 : wave * kWave * N), (int64_t)T * N, end, c, q.top, t, best, T > kWave ? &bounds : nullptr, wave);
         if constexpr (T > kWave) {
             join_waves<TOP>(t, best, c, part, lists);
             if (wave != 0) continue;
@@ -424,12 +425,13 @@ struct LogprobsGrad {
     int64_t ld, ld_out, rows;
     int V, token_bits, chunks;
     float scale;
+    bool stream;
 };
 
 // T threads on a chunk of a row, VECS vectors each.  The gradient is p (A + B log2 p) with A and B the row's, and
 // log2 p = c (x - m) - log2(sum) a difference and a fused operation; what rounding log2(sum) cut off is in A and B.  Seven
 // instructions an element and the exponential.
-template <int DT, int T, int VECS, bool ENTROPY>
+template <int DT, int T, int VECS, bool ENTROPY, Caching BOTH>
 __global__ void __launch_bounds__(kBlock) logprob_grad(const LogprobsGrad q) {
     using V = RowVec<DT>;
     constexpr int N = V::kN, R = kBlock / T;
@@ -445,7 +447,7 @@ __global__ void __launch_bounds__(kBlock) logprob_grad(const LogprobsGrad q) {
         const int left = (int)(q.V - first);
         V x[VECS];
 #pragma unroll
-        for (int v = 0; v < VECS; ++v) x[v] = load_row<DT>(row, (v * T + t) * N, left);
+        for (int v = 0; v < VECS; ++v) x[v] = load_row<DT, BOTH>(row, (v * T + t) * N, left);
         const float m = q.stats[2 * r], logs = q.stats[2 * r + 1];
         int64_t token = -1;
         float g = 0.0f, h = 0.0f, H = 0.0f;
@@ -478,7 +480,7 @@ __global__ void __launch_bounds__(kBlock) logprob_grad(const LogprobsGrad q) {
             }
             V o;
             o.set(d);
-            store_row<DT>(out, e, left, o);
+            store_row<DT, BOTH>(out, e, left, o);
         }
     }
 }
@@ -504,8 +506,12 @@ Cut cut_rows(int64_t rows, int64_t V, int dt) {
 template <int DT, bool TOP>
 int launch_rows(const Logprobs& q, const Cut& cut, hipStream_t stream) {
     const int64_t items = q.rows * cut.pieces;
-    if (cut.threads == kWave) hipLaunchKernelGGL((logprob_rows<DT, kWave, TOP>), dim3(grid_of((items + 3) / 4)), dim3(kBlock), 0, stream, q);
-    else hipLaunchKernelGGL((logprob_rows<DT, kBlock, TOP>), dim3(grid_of(items)), dim3(kBlock), 0, stream, q);
+    if (cut.threads == kWave)
+        hipLaunchKernelGGL((logprob_rows<DT, kWave, TOP, kKeep>), dim3(grid_of((items + 3) / 4)), dim3(kBlock), 0, stream, q);
+    else if (q.stream)
+        hipLaunchKernelGGL((logprob_rows<DT, kBlock, TOP, kStream>), dim3(grid_of(items)), dim3(kBlock), 0, stream, q);
+    else
+        hipLaunchKernelGGL((logprob_rows<DT, kBlock, TOP, kKeep>), dim3(grid_of(items)), dim3(kBlock), 0, stream, q);
     const int rc = launch_status();
     if (rc != SDGP_OK || cut.pieces == 1) return rc;
     hipLaunchKernelGGL((logprob_join<DT, TOP>), dim3(grid_of(q.rows)), dim3(kBlock), 0, stream, q);
@@ -521,13 +527,22 @@ int launch_grad(LogprobsGrad q, hipStream_t stream) {
         hipLaunchKernelGGL(kernel, dim3(grid_of((items + at_once - 1) / at_once)), dim3(kBlock), 0, stream, q);
         return launch_status();
     };
-    if (q.V <= 16 * N) return go(logprob_grad<DT, 16, 1, ENTROPY>, 16, 1);
-    if (q.V <= 64 * 2 * N) return go(logprob_grad<DT, 64, 2, ENTROPY>, 64, 2);
-    if (q.V <= 256 * 8 * N) return go(logprob_grad<DT, 256, 2, ENTROPY>, 256, 2);
-    return go(logprob_grad<DT, 256, 4, ENTROPY>, 256, 4);
+    const auto sized = [&](auto both) {
+        constexpr Caching C = decltype(both)::value;
+        if (q.V <= 16 * N) return go(logprob_grad<DT, 16, 1, ENTROPY, C>, 16, 1);
+        if (q.V <= 64 * 2 * N) return go(logprob_grad<DT, 64, 2, ENTROPY, C>, 64, 2);
+        if (q.V <= 256 * 8 * N) return go(logprob_grad<DT, 256, 2, ENTROPY, C>, 256, 2);
+        return go(logprob_grad<DT, 256, 4, ENTROPY, C>, 256, 4);
+    };
+    return q.stream ? sized(Cached<kStream>{}) : sized(Cached<kKeep>{});
 }
 
 }  // namespace
+
+// Logits that a 256 MB cache keeps nothing of for the gradient are read with the streaming hint, where rows begin on 16 bytes
+// (forward of 8192 x 65536 bf16 182 us without, 167 with it); and from 80 MB on logits and gradients pass by the caches in
+// the backward kernel (2048 x 32768 bf16, both directions, 86 and 77 us).
+static bool larger_than(int64_t megabytes, int64_t rows, int64_t V, int dt) { return rows * V * (dt == SDGP_BF16 ? 2 : 4) > megabytes << 20; }
 
 size_t token_logprobs_workspace(int64_t rows, int64_t V, int dt, int top) {
     if (rows == 0) return 0;
@@ -542,7 +557,8 @@ int token_logprobs_launch(const void* logits, int64_t ld, const void* tokens, in
     const int64_t items = rows * cut.pieces;
     Best* lists = static_cast<Best*>(workspace);
     const Logprobs q = {logits, tokens, logp, entropy, top_logp, stats, top_ids, ld, rows, (int)V, top, token_bits, scale, cut.pieces,
-                        cut.piece, reinterpret_cast<Sums*>(lists + items * top), lists};
+                        cut.piece, reinterpret_cast<Sums*>(lists + items * top), lists,
+                        larger_than(256, rows, V, dt) && is_aligned16(logits) && ld * (dt == SDGP_BF16 ? 2 : 4) % 16 == 0};
     if (dt == SDGP_BF16) return top > 0 ? launch_rows<SDGP_BF16, true>(q, cut, stream) : launch_rows<SDGP_BF16, false>(q, cut, stream);
     return top > 0 ? launch_rows<SDGP_F32, true>(q, cut, stream) : launch_rows<SDGP_F32, false>(q, cut, stream);
 }
@@ -550,7 +566,8 @@ int token_logprobs_launch(const void* logits, int64_t ld, const void* tokens, in
 int token_logprobs_bwd_launch(const void* logits, int64_t ld, const void* tokens, int token_bits, const float* stats, const float* entropy,
                               const float* g_logp, const float* g_entropy, void* dlogits, int64_t ld_out, int64_t rows, int64_t V,
                               int dt, float scale, hipStream_t stream) {
-    const LogprobsGrad q = {logits, tokens, stats, entropy, g_logp, g_entropy, dlogits, ld, ld_out, rows, (int)V, token_bits, 1, scale};
+    const LogprobsGrad q = {logits, tokens, stats, entropy, g_logp, g_entropy, dlogits, ld, ld_out, rows, (int)V, token_bits, 1, scale,
+                            larger_than(80, rows, V, dt)};
     if (dt == SDGP_BF16) return g_entropy ? launch_grad<SDGP_BF16, true>(q, stream) : launch_grad<SDGP_BF16, false>(q, stream);
     return g_entropy ? launch_grad<SDGP_F32, true>(q, stream) : launch_grad<SDGP_F32, false>(q, stream);
 }

@@ -311,3 +311,22 @@ def test_another_stream():
     side.synchronize()
     assert torch.equal(got[0], want[0]) and torch.equal(got[3], want[3])
     assert torch.equal(d, sdgp.sdgp_token_logprobs_bwd(x, tok, want[4], None, want[0]))
+
+
+@pytest.mark.parametrize("dtype,V", [(torch.bfloat16, 65536), (torch.bfloat16, 65537), (torch.float32, 33000)])
+def test_logits_larger_than_the_caches(dtype, V):
+    """Above 256 MB logits are read, above 80 MB gradients written, past the caches.  Rows are problems of their own: parts of
+    525 of them (69 MB), cut the same way, give the same bits."""
+    x = random_logits(2100, V, dtype, V)
+    x[7, ::3] = -np.inf
+    assert x.numel() * x.element_size() > 256 << 20
+    tokens = torch.randint(-1, V, (2100,), device="cuda")
+    g = torch.randn(2100, device="cuda")
+    whole = sdgp.sdgp_token_logprobs(x, tokens, top=2)
+    d = sdgp.sdgp_token_logprobs_bwd(x, tokens, whole[4], whole[1], g, g)
+    for lo in range(0, 2100, 525):
+        cut = slice(lo, lo + 525)
+        part = sdgp.sdgp_token_logprobs(x[cut], tokens[cut], top=2)
+        for a, b in zip(whole, part):
+            assert torch.equal(a[cut], b)
+        assert torch.equal(d[cut], sdgp.sdgp_token_logprobs_bwd(x[cut], tokens[cut], part[4], part[1], g[cut], g[cut]))
