@@ -335,6 +335,7 @@ int sdgp_conv_bwd_weight(const void* D, const void* dO, float* dW, int64_t B, in
  * sdgp_token_logprobs -- log probabilities of given tokens, entropy and best alternatives of every row of logits.
  *
  *   logits    [rows, V] of `dt`, row stride ld >= V elements (a vocabulary cut out of padded logits), last stride 1
+ *   V         1 .. 2^30
  *   tokens    [rows] int32 or int64 (token_bits), NULL with logp NULL.  A token < 0 is none: its log probability is 0
  *             and no gradient comes from it.  A token >= V gives NaN (and a row of NaN as gradient).
  *   scale     > 0, what the logits are multiplied with first (one over the temperature)
@@ -378,7 +379,8 @@ int sdgp_token_logprobs_bwd(const void* logits, int64_t ld, const void* tokens, 
  *   w_post, w_pre  [D] of `wdt` (fp32 or bf16), or NULL for ones
  *   h         NULL: no norm follows (then w_pre is NULL too)
  *   stats     [2, rows] fp32: the two norms' factors 1/sqrt(...), for the gradient
- *   x, u, y, h, gate `dt`; arithmetic fp32.  rows % groups == 0, D >= 1.  Outputs overlap no input.
+ *   x, u, y, h, gate `dt`; arithmetic fp32.  rows % groups == 0, 1 <= D <= 2^20.  Outputs overlap no
+ *             input.
  *
  * sdgp_block_norm_bwd -- dL/dx, dL/du, dL/dgate and the weights' gradients from dy (of the stored y; NULL: 0) and dh (NULL
  * with h NULL).  y is x where there was no block.  dx, du, dgate `dt`; dw_post, dw_pre [D] fp32, present exactly where the

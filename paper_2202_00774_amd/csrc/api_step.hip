@@ -27,7 +27,8 @@ namespace {
 
 constexpr int64_t kMaxElements = (int64_t)1 << 40;
 constexpr int kMaxTop = 64;                      // a wavefront's lanes
-constexpr int64_t kMaxWidth = (int64_t)1 << 30;  // logits or channels of a row: counted in 32 bits
+constexpr int64_t kMaxWidth = (int64_t)1 << 30;  // logits of a row: counted in 32 bits
+constexpr int64_t kMaxChannels = (int64_t)1 << 20;
 
 bool valid_dtype(int dt) { return dt == SDGP_F32 || dt == SDGP_BF16; }
 int64_t element(int dt) { return dt == SDGP_BF16 ? 2 : 4; }
@@ -54,6 +55,7 @@ int check_norm(int64_t rows, int64_t D, int64_t groups, int dt, int wdt) {
     const int rc = check_rows(rows, D, D, dt);
     if (rc != SDGP_OK) return rc;
     if (!valid_dtype(wdt)) return SDGP_ERR_DTYPE;
+    if (D > kMaxChannels) return SDGP_ERR_SHAPE;
     return groups < 0 || (groups > 0 && rows % groups != 0) ? SDGP_ERR_SHAPE : SDGP_OK;
 }
 

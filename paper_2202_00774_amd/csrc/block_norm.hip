@@ -136,9 +136,10 @@ __global__ void __launch_bounds__(kBlock) norm_grad_long_rows(const NormGrad n, 
 
 // The slabs' sums over rows of any width, one thread a column.
 __global__ void __launch_bounds__(kBlock) norm_grad_columns(const NormGrad n, const float* __restrict__ means) {
-    const int d = blockIdx.x * kBlock + threadIdx.x;
+    const int columns = (n.D + kBlock - 1) / kBlock;   // workgroups of a slab
+    const int d = (int)(blockIdx.x % columns) * kBlock + threadIdx.x;
     if (d >= n.D) return;
-    const int64_t slab = blockIdx.y;
+    const int64_t slab = blockIdx.x / columns;
     const float w = weight(n.w_post, n.wdt, d);
     int64_t first, end;
     if (n.slabs.kind == kWholeGroups) {
@@ -248,8 +249,8 @@ int block_norm_bwd_no_rows(void* dgate, int64_t gate_elements, int dt, float* dw
 
 // A slab costs its columns' sums written and read again, so it holds four rows for each that a workgroup has in hand (4099
 // x 1001 fp32: 76 us with eight rows each, 63 with four), unless that leaves fewer than 256 workgroups, one a CU; nor are
-// there more than a CU holds at 16 wavefronts.  Gates of up to 32 rows that are many (2048) are finished by the slab that
-// holds them.
+// there more than a CU holds at 16 wavefronts.  Gates of up to 32 rows that are many (2048), and any that are very many
+// (65536, which bounds the slabs), are finished by the slab that holds them.
 static Slabs make_slabs(int64_t rows, int64_t D, int64_t groups, int dt) {
     const RowShape shape = row_shape(D, dt);
     const int64_t at_once = shape.threads == 0 ? 1 : rows_at_once(shape.threads);
@@ -258,7 +259,7 @@ static Slabs make_slabs(int64_t rows, int64_t D, int64_t groups, int dt) {
     int64_t want = rows / (4 * at_once);
     const int64_t waves = shape.threads == 0 ? kBlock / kWave : shape.threads * at_once / kWave, most = 256 * (waves >= 16 ? 1 : 16 / waves);
     want = want < 256 ? 256 : want > most ? most : want;
-    if (groups > 0 && (per_gate == 1 || (per_gate <= 32 && groups >= 2048))) {
+    if (groups > 0 && (per_gate == 1 || (per_gate <= 32 && groups >= 2048) || groups >= 65536)) {
         s.kind = kWholeGroups;
         s.len = ((groups + want - 1) / want + at_once - 1) / at_once * at_once;
         s.parts = 1;
@@ -313,7 +314,7 @@ int block_norm_bwd_launch(const void* dy, const void* dh, const void* y, const v
         rc = launch_status();
         if (rc != SDGP_OK) return rc;
         if (n.part_pre || n.part_post || gate) {
-            hipLaunchKernelGGL(norm_grad_columns, dim3((unsigned)((D + kBlock - 1) / kBlock), (unsigned)slabs.count), dim3(kBlock), 0, stream, n, means);
+            hipLaunchKernelGGL(norm_grad_columns, dim3((unsigned)((D + kBlock - 1) / kBlock * slabs.count)), dim3(kBlock), 0, stream, n, means);
             rc = launch_status();
         }
     }

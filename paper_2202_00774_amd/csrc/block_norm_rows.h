@@ -1,7 +1,8 @@
 // Block norms of rows that fit the registers, forward and backward (the formulas stand in block_norm.hip).
 //
 // Bound by memory: 8 bytes an element forward (x, u in; y, h out), 12 backward (y, u, dy, dh in; dx, du out) in bf16, with
-// 15 and 30 vector instructions beside them.  Every value is loaded once and stays in registers, packed as stored,
+// 25 and 34 vector instructions beside them.  Measured: 32768 x 4096 bf16 forward 195 us (5.5 TB/s), backward 280 (5.8 TB/s) and 6
+// for the slabs' sums; 16384 x 2048 with 16 gates 45, 67 and 6.  Every value is loaded once and stays in registers, packed as stored,
 // until its row's sums are known.  Backward, the second norm's sum depends on the first's result (dY holds the
 // mean of dn t), but linearly: with v = dy + r_y dn,
 //     sum dY k a = sum v k a - r_y mean(dn t) sum t k a,        k = gate w_post,

@@ -10,9 +10,10 @@
 // weighted sum they are cut at -256 (in powers of two), where e^ is 0 already, so that a logit of -inf adds 0 and not
 // 0 * inf.  All sums are fp32.
 //
-// Bound by memory where rows are many: 2 bytes an element read forward, 4 read and written backward in bf16; beside them
-// 11 vector instructions forward, one of them an exponential, and 14 backward.  A row is one workgroup's (or, where rows are
-// short and many, one wavefront's); few long rows are cut into pieces, whose sums and lists a second kernel joins.
+// Bound by memory where rows are many: 2 bytes an element read forward, 4 read and written backward in bf16, with 8 and 12
+// vector instructions beside them, one an exponential.  A row is one workgroup's (or, where rows are short and many, one
+// wavefront's); few long rows are cut into pieces, whose sums and lists a second kernel joins.  Measured: 8192 x 65536 bf16
+// forward 167 us (6.4 TB/s), gradient 345 (6.2 TB/s); 4 x 131072 with eight alternatives 9 + 5 us, which are latencies.
 #include "rows.h"
 
 namespace sdgp {

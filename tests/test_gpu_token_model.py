@@ -118,3 +118,35 @@ def test_the_model_learns_the_chain(state_bits):
     assert right >= 28
     for k, v in model.weights.items():
         assert torch.equal(v.detach(), model.masters[k].to(torch.bfloat16)), k
+
+
+def test_a_captured_graph_replays_the_operators():
+    """Loss, gradient and norms recorded once; every replay gives what the eager calls give on the inputs of the moment."""
+    torch.manual_seed(5)
+    x = torch.randn(6, 70001, device="cuda", dtype=torch.bfloat16)               # few long rows: two kernels and a workspace
+    tokens = torch.randint(0, 70001, (6,), device="cuda")
+    g = torch.randn(6, device="cuda")
+    a, b = torch.randn(2, 300, 264, device="cuda", dtype=torch.bfloat16)
+    w = torch.randn(264, device="cuda")
+
+    def work():
+        logp, entropy, top_logp, top_ids, stats = sdgp.sdgp_token_logprobs(x, tokens, top=5)
+        d = sdgp.sdgp_token_logprobs_bwd(x, tokens, stats, entropy, g, g)
+        y, h, s = sdgp.sdgp_block_norm(a, b, None, w, w)
+        return (logp, entropy, top_logp, top_ids, d, y, h, *(t for t in sdgp.sdgp_block_norm_bwd(a, b, y, s, b, None, w, w) if t is not None))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        work()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = work()
+    for i in range(4):
+        x.copy_(torch.randn(x.shape, device="cuda"))
+        a.copy_(torch.randn(a.shape, device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        for p, q in zip(held, work()):
+            assert torch.equal(p, q), i
