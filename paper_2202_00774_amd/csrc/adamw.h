@@ -6,7 +6,10 @@
 namespace sdgp {
 
 constexpr int kAdamBlock = 256;                       // elements that share a scale in an 8-bit state
-constexpr int kAdamTile = 16;                         // blocks of a workgroup
+// Blocks of a workgroup: four wavefronts with four each in flight for fp32 states, one each for 8-bit ones, where a block's
+// arithmetic is what a wavefront waits for (24 x 8388608 elements: fp32 1010 us with 16, 1020 with 4; 8 bits 563 and 547; ResNet-50's
+// tensors in 8 bits 104 and 91).
+constexpr int adam_tile(int bits) { return bits == 8 ? 4 : 16; }
 constexpr int64_t kAdamLaunch = (int64_t)1 << 22;     // tiles of a launch: its threads are counted in 32 bits
 constexpr int64_t kAdamPart = (int64_t)1 << 31;       // elements of a tensor in one launch: counted in 32 bits, whole tiles
 

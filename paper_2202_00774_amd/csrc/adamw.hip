@@ -12,11 +12,11 @@
 // scale is taken over the block's finite values.
 //
 // Bound by memory: 28 bytes an element with fp32 states (parameter and both states in and out, gradient in), 16 with 8-bit
-// ones.  A wavefront takes a block of 256 elements, four a lane, so a block's scale is a maximum over one wavefront; four
-// blocks' loads are in flight together.  A workgroup's tile of 16 blocks lies in one tensor, which it looks up in the
-// arguments.  In 8 bits an element costs 75 vector instructions, 70 % of what fits beside its 16 bytes: codes are cut from the
-// float's bits, and what only infinities and NaN need is done where a block has them.  Measured: 24 x 8388608 elements in 8 bits
-// 560 us (5.8 TB/s), in fp32 1020 (5.9 TB/s); ResNet-50's 161 tensors 103 and 135.
+// ones.  A wavefront takes a block of 256 elements, four a lane, so a block's scale is a maximum over one wavefront.  A
+// workgroup's tile of blocks lies in one tensor, which it looks up in the arguments.  In 8 bits an element costs 75 vector
+// instructions, 70 % of what fits beside its 16 bytes: codes are cut from the float's bits, and what only infinities and NaN
+// need is done where a block has them.  Measured: 24 x 8388608 elements in 8 bits 547 us (5.9 TB/s), in fp32 1010 (6.0 TB/s);
+// ResNet-50's 161 tensors 91 and 135.
 #include "adamw.h"
 
 #include "rows.h"
@@ -25,7 +25,7 @@ namespace sdgp {
 
 namespace {
 
-constexpr int kThreads = 256, kWave = 64, kAtOnce = kAdamTile / (kThreads / kWave);   // blocks of a wavefront
+constexpr int kThreads = 256, kWave = 64;
 constexpr uint32_t kInf = 0x7F800000u;
 
 // One mixed word of (seed, element): the finalizer of common.h's hash, one word an element.
@@ -178,6 +178,7 @@ __device__ __forceinline__ uint32_t to_codes(float (&x)[4], const uint32_t (&u)[
 template <int PDT, int GDT, int BITS>
 __global__ void __launch_bounds__(kThreads) adamw_tiles(const AdamArgs<BITS> a) {
     using Tensors = AdamTensors<BITS>;
+    constexpr int kTile = adam_tile(BITS), kAtOnce = kTile / (kThreads / kWave);   // blocks of a wavefront
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
     // the last tensor that begins at this tile or before it; every lane compares one or two (a search would wait for each step)
     int at = -1;
@@ -192,7 +193,7 @@ __global__ void __launch_bounds__(kThreads) adamw_tiles(const AdamArgs<BITS> a) 
         void *m, *v;
         uint16_t* copy;
     } const t = {a.t.p[at], a.t.g[at], a.t.m[at], a.t.v[at], a.t.copy[at]};
-    const int64_t block0 = (int64_t)(blockIdx.x - a.t.first[at]) * kAdamTile + wave * kAtOnce, n = a.t.n[at];
+    const int64_t block0 = (int64_t)(blockIdx.x - a.t.first[at]) * kTile + wave * kAtOnce, n = a.t.n[at];
     if (block0 * kAdamBlock >= n) return;
     float *m_scale = nullptr, *v_scale = nullptr;
     if constexpr (BITS == 8) m_scale = a.t.m_scale[at], v_scale = a.t.v_scale[at];
@@ -229,7 +230,10 @@ __global__ void __launch_bounds__(kThreads) adamw_tiles(const AdamArgs<BITS> a) 
             m[b][i] = add_rn(mul_rn(m[b][i], a.b1), mul_rn(gi, a.one_b1));
             v[b][i] = add_rn(mul_rn(v0, a.b2), mul_rn(mul_rn(gi, gi), a.one_b2));
             r[i] = sqrtf(v[b][i]);
-            p[b][i] = fmaf(p[b][i], a.decay, -a.rate * m[b][i] * __builtin_amdgcn_rcpf(fmaf(r[i], a.inv_root_bc2, a.eps)));
+            const float den = fmaf(r[i], a.inv_root_bc2, a.eps);
+            // (a reciprocal, good to one unit, for 8-bit states: a division costs them 3 % of the time.  It knows no subnormals.)
+            const float by = BITS == 8 ? m[b][i] * __builtin_amdgcn_rcpf(den < 0x1p-126f ? 0x1p-126f : den) : m[b][i] / den;
+            p[b][i] = fmaf(p[b][i], a.decay, -a.rate * by);
         }
         store4<PDT>(t.p, e, n, p[b]);
         if (PDT == SDGP_F32 && t.copy != nullptr) store4<SDGP_BF16>(t.copy, e, n, p[b]);

@@ -76,7 +76,7 @@ struct AdamCall {
 // As many launches as the tensors fill.  A tensor longer than a launch counts goes in parts of whole tiles.
 template <int BITS>
 int adamw_launches(const AdamCall& c, sdgp::AdamArgs<BITS>& a) {
-    constexpr int64_t kTile = (int64_t)sdgp::kAdamTile * sdgp::kAdamBlock;
+    constexpr int64_t kTile = (int64_t)sdgp::adam_tile(BITS) * sdgp::kAdamBlock;
     int64_t tiles = 0, block = 0;   // tiles of this launch; a tensor's first block, counted in the call
     int k = 0;
     const auto launch = [&] {
