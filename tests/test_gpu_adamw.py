@@ -307,3 +307,25 @@ def test_another_stream():
         stream.synchronize()
         got.append(params)
     assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+def test_8_bit_more_elements_than_32_bits_count():
+    """One tensor of 2^32 + 5000 elements, a few of them moved: codes as the rule says for elements numbered past 2^32 too."""
+    n = 2**32 + 5000
+    p, g = torch.zeros(n, dtype=BF16, device="cuda"), torch.zeros(n, dtype=BF16, device="cuda")
+    places = [(0, 700), (2**31 - 300, 600), (2**32 - 300, 600), (n - 3000, 3000)]
+    for i, (at, k) in enumerate(places):
+        g[at:at + k] = tensors([k], BF16, 90 + i)[0]
+    opt = AdamW([p], state_bits=8, seed=5, **HYPER)
+    opt.step([g])
+    o1, o2 = (np.float32(1 - b) for b in HYPER["betas"])
+    for at, k in places:
+        lo, hi = at // 256 * 256, min(n, -(-(at + k) // 256) * 256)
+        part = g[lo:hi].float().cpu().numpy()
+        word = mix(6, lo + np.arange(hi - lo))
+        for key, x, bits, keep in (("exp_avg", part * o1, word & 0xFFFF, False), ("exp_avg_sq", np.sqrt(part * part * o2), word >> 16, True)):
+            codes, scales = stored(x, bits, keep)
+            assert np.array_equal(f64(opt.state()[key + "_scale"][0][lo // 256:-(-hi // 256)]), scales), (key, at)
+            assert np.array_equal(f64(opt.state()[key][0][lo:hi].float()), codes), (key, at)
+        assert ((p[lo:hi] != 0) == (g[lo:hi] != 0)).all()
+    assert (p[2**31 + 1000:2**32 - 1000] == 0).all()

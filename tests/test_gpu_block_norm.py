@@ -295,3 +295,20 @@ def test_tensors_larger_than_the_caches(dtype, rows, D, gate):
         near(dgate.view(gate, D)[g], gates[0] + gates[1], 2 * E * per * sizes + store * (np.abs(gates[0]) + np.abs(gates[1])), "dgate")
     near(dw_post, post, 2 * E * rows * sizes, "dw_post")
     near(dw_pre, pre, 2 * E * rows * sizes, "dw_pre")
+
+
+def test_more_elements_than_32_bits_count():
+    rows, D = 1100000, 2048
+    g = torch.Generator(device="cuda")
+    g.manual_seed(0)
+    x, u, dy, dh = (torch.empty(rows, D, dtype=torch.bfloat16, device="cuda").normal_(generator=g) for _ in range(4))
+    w = 1 + 0.3 * torch.randn(D, device="cuda", generator=g)
+    gate = torch.randn(1, D, device="cuda", generator=g).to(torch.bfloat16)
+    y, h, stats = sdgp.sdgp_block_norm(x, u, gate, w, w)
+    dx, du, dgate, dw_post, dw_pre = sdgp.sdgp_block_norm_bwd(dy, dh, y, stats, u, gate, w, w)
+    for cut in (slice(0, 40), slice(1048560, 1048600), slice(rows - 40, rows)):     # 2^31 elements lie between
+        py, ph, ps = sdgp.sdgp_block_norm(x[cut], u[cut], gate, w, w)
+        pdx, pdu, *_ = sdgp.sdgp_block_norm_bwd(dy[cut], dh[cut], py, ps, u[cut], gate, w, w)
+        for a, b in ((y, py), (h, ph), (dx, pdx), (du, pdu)):
+            assert torch.equal(a[cut], b)
+    assert torch.isfinite(dw_post).all() and torch.isfinite(dw_pre).all() and torch.isfinite(dgate).all()

@@ -330,3 +330,16 @@ def test_logits_larger_than_the_caches(dtype, V):
         for a, b in zip(whole, part):
             assert torch.equal(a[cut], b)
         assert torch.equal(d[cut], sdgp.sdgp_token_logprobs_bwd(x[cut], tokens[cut], part[4], part[1], g[cut], g[cut]))
+
+
+def test_rows_further_apart_than_32_bits_count():
+    room = torch.empty(2**32 + 40000, dtype=torch.bfloat16, device="cuda")
+    x = room.as_strided((3, 9001), (2**31 + 5, 1))
+    near_by = random_logits(3, 9001, torch.bfloat16, 77)
+    x.copy_(near_by)
+    tokens, g = torch.tensor([9000, 0, 5], device="cuda"), torch.randn(3, device="cuda")
+    far, want = sdgp.sdgp_token_logprobs(x, tokens, top=4), sdgp.sdgp_token_logprobs(near_by, tokens, top=4)
+    for a, b in zip(far, want):
+        assert torch.equal(a, b)
+    sdgp.sdgp_token_logprobs_bwd(x, tokens, far[4], far[1], g, g, out=x)
+    assert torch.equal(x, sdgp.sdgp_token_logprobs_bwd(near_by, tokens, want[4], want[1], g, g))
