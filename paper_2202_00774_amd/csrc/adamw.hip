@@ -13,10 +13,10 @@
 //
 // Bound by memory: 28 bytes an element with fp32 states (parameter and both states in and out, gradient in), 16 with 8-bit
 // ones.  A wavefront takes a block of 256 elements, four a lane, so a block's scale is a maximum over one wavefront.  A
-// workgroup's tile of blocks lies in one tensor, which it looks up in the arguments.  In 8 bits an element costs 75 vector
-// instructions, 70 % of what fits beside its 16 bytes: codes are cut from the float's bits, and what only infinities and NaN
+// workgroup's tile of blocks lies in one tensor, which it looks up in the arguments.  In 8 bits an element costs 84 vector
+// instructions, 89 % of what fits beside its 16 bytes: codes are cut from the float's bits, and what only infinities and NaN
 // need is done where a block has them.  Measured: 24 x 8388608 elements in 8 bits 547 us (5.9 TB/s), in fp32 1010 (6.0 TB/s);
-// ResNet-50's 161 tensors 91 and 135.
+// ResNet-50's 161 tensors 88 and 135.
 #include "adamw.h"
 
 #include "rows.h"

@@ -14,6 +14,7 @@ from __future__ import annotations
 import ctypes
 
 import torch
+from torch.autograd.graph import increment_version
 
 from . import binding
 
@@ -71,6 +72,8 @@ class AdamW:
         self._seen = {}
         for k in ("params", "copies"):
             self._addresses(k)
+        # what autograd has to know of: a graph that saved one of these must not go back through the new values
+        self._written = [t for t in (*self.params, *(self.copies or ())) if not t.is_inference()]
 
     def _addresses(self, name: str):
         tensors = getattr(self, name)
@@ -91,6 +94,9 @@ class AdamW:
             raise ValueError(f"{name} holds one value for each {BLOCK} elements of every param")
         if not scales and [t.shape for t in tensors] != self._shapes:
             raise ValueError(f"{name} must have the shapes of params")
+        places = [t.data_ptr() for t in tensors if t.numel()]
+        if len(set(places)) != len(places):      # two workgroups would step it at once
+            raise ValueError(f"a tensor is twice among {name}")
         if tensors and tensors[0].get_device() != self.params[0].get_device():
             raise ValueError(f"{name} must live on the GPU of params")
 
@@ -136,4 +142,5 @@ class AdamW:
             binding._stream(grads[0]))
         if rc != 0:
             raise binding.SdgpError(rc, "sdgp_adamw_step")
+        increment_version(self._written)
         self.steps = step

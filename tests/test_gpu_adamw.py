@@ -329,3 +329,28 @@ def test_8_bit_more_elements_than_32_bits_count():
             assert np.array_equal(f64(opt.state()[key][0][lo:hi].float()), codes), (key, at)
         assert ((p[lo:hi] != 0) == (g[lo:hi] != 0)).all()
     assert (p[2**31 + 1000:2**32 - 1000] == 0).all()
+
+
+def test_a_graph_that_saved_a_parameter_or_its_copy_knows_of_the_step():
+    w, low = torch.ones(300, device="cuda", requires_grad=True), torch.ones(300, device="cuda", dtype=BF16, requires_grad=True)
+    opt = AdamW([w], copies=[low])
+    outs = [(t * t).sum() for t in (w, low)]
+    opt.step([torch.ones(300, device="cuda")])
+    for y in outs:
+        with pytest.raises(RuntimeError, match="inplace"):
+            y.backward()
+    (w * w).sum().backward()
+    assert torch.equal(w.grad, 2 * w.detach())
+    with torch.inference_mode():                  # tensors that autograd does not follow
+        p = torch.ones(300, device="cuda")
+        AdamW([p], lr=0.5, weight_decay=0.0).step([torch.ones(300, device="cuda")])
+    assert ((p - 0.5).abs() <= 1e-6).all()        # m / (sqrt(v) + eps) is 1 but for eps and a few roundings of 2^-24
+
+
+def test_the_same_tensor_twice_is_refused():
+    p, e = torch.zeros(300, device="cuda"), torch.zeros(0, device="cuda")
+    with pytest.raises(ValueError, match="twice"):
+        AdamW([p, p])
+    with pytest.raises(ValueError, match="twice"):
+        AdamW([p, p.clone()], copies=[p.to(BF16)] * 2)
+    AdamW([e, p, e])                              # without elements there is nothing to step
