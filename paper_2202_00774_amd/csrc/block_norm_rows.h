@@ -143,14 +143,15 @@ __device__ __forceinline__ void load(Row<DT, NV>& row, const NormGrad& n, int64_
     else load_as<kKeep, T, BLOCK>(row, n, r, end, t);
 }
 
-// MODE: kNoBlock, or how the slab is cut.
-constexpr int kNoBlock = 2;
+// MODE: kNoBlock, or how the slab is cut; kRowGates: whole groups of one row each, whose gate's gradient needs no sum
+// (4099 x 1001 fp32 57.5 us, 58.5 as kWholeGroups; 4096 x 8192 bf16 199 and 221, both directions).
+constexpr int kNoBlock = 2, kRowGates = 3;
 
 template <int DT, int T, int NV, int MODE, Caching RESULTS>
 __global__ void __launch_bounds__(norm_block<T>()) norm_bwd(const NormGrad n) {
     using V = RowVec<DT>;
     constexpr int N = V::kN, R = norm_block<T>() / T, kColumns = T * NV * N;
-    constexpr bool BLOCK = MODE != kNoBlock, kTurns = RESULTS == kStream;
+    constexpr bool BLOCK = MODE != kNoBlock, kWhole = MODE == kWholeGroups || MODE == kRowGates, kTurns = RESULTS == kStream;
     constexpr int64_t kSize = sizeof(typename V::Elem);
     __shared__ float lds[R > 1 ? R * kColumns : row_lds<T, 3>()];
     int turn = 0;
@@ -161,20 +162,26 @@ __global__ void __launch_bounds__(norm_block<T>()) norm_bwd(const NormGrad n) {
     // each, they are read again for every row (in registers they spilled 300).  The next row is not asked for ahead of its
     // turn: that takes 25 registers, and a third or fourth wavefront a SIMD hides more (16384 x 2048: 134 us, without 124).
     constexpr bool kHeld = NV == 1;
-    float w_pre[NV][N], k[NV][N];
+    // Where gates are many a gate stays as it is stored, beside w_post, and k is computed for every row, so that nothing waits
+    // for the gate before the row's loads are on their way (20000 x 1001 fp32, a gate a row: 267 us without, 245 with it); not with
+    // 1024 threads, whose 128 registers do not hold both (4096 x 8192 bf16 220 us, with it 234).
+    constexpr bool kRaw = kHeld && T < 1024 && kWhole;
+    float w_pre[NV][N], k[NV][N];   // k: w_post where kRaw
+    V gates[NV];
     float sum_pre[NV][N], sum_post[NV][N];  // dh t, and dY a (kInGroup) or dY gate a (kWholeGroups)
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
         if constexpr (kHeld) load_weights<N>(n.w_pre, n.wdt, (v * T + t) * N, n.D, w_pre[v]);
+        if constexpr (kRaw) load_weights<N>(n.w_post, n.wdt, (v * T + t) * N, n.D, k[v]);
 #pragma unroll
         for (int i = 0; i < N; ++i) sum_pre[v][i] = 0.0f, sum_post[v][i] = 0.0f;
     }
 
     // the gates of this slab: one (kInGroup), or `len` of them, each sub-group of threads taking its own
-    const int64_t gate0 = MODE == kWholeGroups ? (int64_t)blockIdx.x * n.slabs.len : (int64_t)blockIdx.x / n.slabs.parts;
-    const int64_t gate1 = MODE != kWholeGroups ? gate0 + 1 : gate0 + n.slabs.len < n.groups ? gate0 + n.slabs.len : n.groups;
-    for (int64_t q0 = gate0; q0 < gate1; q0 += MODE == kWholeGroups ? R : 1) {
-        const int64_t q = MODE == kWholeGroups ? q0 + sub : q0;
+    const int64_t gate0 = kWhole ? (int64_t)blockIdx.x * n.slabs.len : (int64_t)blockIdx.x / n.slabs.parts;
+    const int64_t gate1 = !kWhole ? gate0 + 1 : gate0 + n.slabs.len < n.groups ? gate0 + n.slabs.len : n.groups;
+    for (int64_t q0 = gate0; q0 < gate1; q0 += kWhole ? R : 1) {
+        const int64_t q = kWhole ? q0 + sub : q0;
         const bool mine = q < gate1;
         const char* gate_row = static_cast<const char*>(n.gate) + (mine ? q : gate0) * n.D * kSize;
         const auto gated = [&](int e, float (&kv)[N]) {
@@ -188,7 +195,8 @@ __global__ void __launch_bounds__(norm_block<T>()) norm_bwd(const NormGrad n) {
         if constexpr (BLOCK) {
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
-                if constexpr (kHeld) gated((v * T + t) * N, k[v]);
+                if constexpr (kRaw) gates[v] = load_row<DT>(gate_row, (v * T + t) * N, n.D);
+                else if constexpr (kHeld) gated((v * T + t) * N, k[v]);
 #pragma unroll
                 for (int i = 0; i < N; ++i) sum_gate[v][i] = 0.0f;
             }
@@ -196,7 +204,7 @@ __global__ void __launch_bounds__(norm_block<T>()) norm_bwd(const NormGrad n) {
         const auto weights = [&](int v, float (&wv)[N], float (&kv)[N]) {
             if constexpr (kHeld) {
 #pragma unroll
-                for (int i = 0; i < N; ++i) wv[i] = w_pre[v][i], kv[i] = BLOCK ? k[v][i] : 0.0f;
+                for (int i = 0; i < N; ++i) wv[i] = w_pre[v][i], kv[i] = kRaw ? k[v][i] * gates[v].get(i) : BLOCK ? k[v][i] : 0.0f;
             } else {
                 int e = (v * T + t) * N;
                 asm volatile("" : "+v"(e));   // in every row anew, not once in front of them
@@ -205,14 +213,14 @@ __global__ void __launch_bounds__(norm_block<T>()) norm_bwd(const NormGrad n) {
             }
         };
         int64_t first = q * n.per_gate, end = first + n.per_gate;
-        if constexpr (MODE != kWholeGroups) {
+        if constexpr (!kWhole) {
             first += (int64_t)(blockIdx.x - gate0 * n.slabs.parts) * (kTurns ? R : n.slabs.len);
             if (!kTurns && first + n.slabs.len < end) end = first + n.slabs.len;
         }
-        const int64_t rows = MODE == kWholeGroups ? n.per_gate : end - first;   // the same for all threads
-        const int64_t step = MODE == kWholeGroups ? 1 : kTurns ? R * n.slabs.parts : R;
+        const int64_t rows = MODE == kRowGates ? 1 : kWhole ? n.per_gate : end - first;   // the same for all threads
+        const int64_t step = kWhole ? 1 : kTurns ? R * n.slabs.parts : R;
         for (int64_t i0 = 0; i0 < rows; i0 += step) {
-            const int64_t r = first + i0 + (MODE == kWholeGroups ? 0 : sub);
+            const int64_t r = first + i0 + (kWhole ? 0 : sub);
             const int D = mine && r < end ? n.D : 0;
             const int64_t at = D > 0 ? r * n.D * kSize : 0;
             Row<DT, NV> row;
@@ -259,7 +267,7 @@ __global__ void __launch_bounds__(norm_block<T>()) norm_bwd(const NormGrad n) {
                         const float a = u[v].get(i) * ru, da = dY * a;
                         dx[i] = n.residual_scale * dY;
                         du[i] = ru * (dY * kv[i] - a * mean_a);
-                        if constexpr (MODE == kWholeGroups) sum_gate[v][i] += da;
+                        if constexpr (kWhole) sum_gate[v][i] += da;
                         else sum_post[v][i] += da;
                     }
                 }
@@ -272,13 +280,20 @@ __global__ void __launch_bounds__(norm_block<T>()) norm_bwd(const NormGrad n) {
                 }
             }
         }
-        if constexpr (MODE == kWholeGroups) {
+        if constexpr (kWhole) {
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
                 const int e = (v * T + t) * N;
                 float w[N], d[N];
-                load_weights<N>(n.w_post, n.wdt, e, n.D, w);
-                const V g = load_row<DT>(gate_row, e, n.D);
+                V g;
+                if constexpr (kRaw) {
+                    g = gates[v];
+#pragma unroll
+                    for (int i = 0; i < N; ++i) w[i] = k[v][i];
+                } else {
+                    load_weights<N>(n.w_post, n.wdt, e, n.D, w);
+                    g = load_row<DT>(gate_row, e, n.D);
+                }
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
                     d[i] = sum_gate[v][i] * w[i];
@@ -353,7 +368,8 @@ int norm_grad_launch(const NormGrad& n, RowShape shape, hipStream_t stream) {
         const auto pick = [&](auto results) {                                                                         \
             constexpr Caching C = decltype(results)::value;                                                           \
             return n.u == nullptr ? norm_bwd<DT, T, NV, kNoBlock, C>                                                  \
-                   : n.slabs.kind == kInGroup ? norm_bwd<DT, T, NV, kInGroup, C> : norm_bwd<DT, T, NV, kWholeGroups, C>; \
+                   : n.slabs.kind == kInGroup ? norm_bwd<DT, T, NV, kInGroup, C>                                            \
+                   : n.per_gate == 1 ? norm_bwd<DT, T, NV, kRowGates, C> : norm_bwd<DT, T, NV, kWholeGroups, C>;              \
         };                                                                                                            \
         hipLaunchKernelGGL((n.large ? pick(Cached<kStream>{}) : pick(Cached<kKeep>{})), grid, block, 0, stream, n);   \
         return launch_status();                                                                                       \
