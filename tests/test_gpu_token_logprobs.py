@@ -343,3 +343,27 @@ def test_rows_further_apart_than_32_bits_count():
         assert torch.equal(a, b)
     sdgp.sdgp_token_logprobs_bwd(x, tokens, far[4], far[1], g, g, out=x)
     assert torch.equal(x, sdgp.sdgp_token_logprobs_bwd(near_by, tokens, want[4], want[1], g, g))
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("top", [1, 3, 4, 5, 8, 9, 16, 17, 32, 33, 64])
+def test_alternatives_of_which_the_first_chunk_has_all_few_or_none(top, dtype):
+    """A row's first 4096 bf16 or 2048 fp32 logits give a bound for the rest.  600 rows: none is cut into pieces."""
+    chunk, V = (4096, 9001) if dtype == torch.bfloat16 else (2048, 5001)
+    g = torch.Generator()
+    g.manual_seed(top)
+    x = torch.randn(600, V, generator=g)
+    x[1::6, :chunk] -= 20                                     # all of the best behind the first chunk
+    x[2::6, chunk:] -= 20                                     # all in it
+    x[3::6, :chunk] = -float("inf")                           # nothing in it
+    x[4::6, : chunk - 3] = -float("inf")                      # three logits in it
+    x[5::6] = torch.randint(0, 3, (100, V), generator=g).float()   # equal ones throughout
+    x[0, :chunk] = 7.0
+    x[6, 3:] = -float("inf")                                  # fewer than are asked for
+    x = x.to(dtype)
+    _, _, lp, ids, _ = sdgp.sdgp_token_logprobs(x.cuda(), None, top=top)
+    x64 = x.double().numpy()
+    want = np.argsort(-x64, axis=1, kind="stable")[:, :top]
+    none = np.take_along_axis(x64, want, 1) == -np.inf
+    assert np.array_equal(ids.cpu().numpy(), np.where(none, -1, want))
+    assert np.array_equal(np.isneginf(lp.cpu().numpy()), none)
