@@ -404,7 +404,7 @@ int sdgp_block_norm_bwd(const void* dy, const void* dh, const void* y, const voi
  *   p = p (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
  *
  *   params, grads, exp_avg, exp_avg_sq, exp_avg_scale, exp_avg_sq_scale, copies, numel: HOST arrays of `count` entries
- *   (read before the call returns) of device pointers and element counts; every tensor contiguous.
+ *   (read before the call returns) of device pointers and element counts; every tensor contiguous, none overlapping another.
  *   params      `param_dt`; grads `grad_dt`
  *   copies      bf16 copies of fp32 parameters, written beside them, or NULL
  *   state_bits  32: exp_avg, exp_avg_sq hold m and v in fp32, the scale arrays are NULL.
