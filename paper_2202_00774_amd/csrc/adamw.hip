@@ -231,9 +231,7 @@ __global__ void __launch_bounds__(kThreads) adamw_tiles(const AdamArgs<BITS> a) 
             v[b][i] = add_rn(mul_rn(v0, a.b2), mul_rn(mul_rn(gi, gi), a.one_b2));
             r[i] = sqrtf(v[b][i]);
             const float den = fmaf(r[i], a.inv_root_bc2, a.eps);
-            // (a reciprocal, good to one unit, for 8-bit states: a division costs them 3 % of the time.  It knows no subnormals.)
-            const float by = BITS == 8 ? m[b][i] * __builtin_amdgcn_rcpf(den < 0x1p-126f ? 0x1p-126f : den) : m[b][i] / den;
-            p[b][i] = fmaf(p[b][i], a.decay, -a.rate * by);
+            p[b][i] = fmaf(p[b][i], a.decay, -a.rate * (m[b][i] / den));
         }
         store4<PDT>(t.p, e, n, p[b]);
         if (PDT == SDGP_F32 && t.copy != nullptr) store4<SDGP_BF16>(t.copy, e, n, p[b]);
