@@ -12,6 +12,7 @@ fp32 parameter and gradient.
 from __future__ import annotations
 
 import ctypes
+from operator import attrgetter
 
 import torch
 from torch.autograd.graph import increment_version
@@ -25,14 +26,17 @@ def _array(addresses):
     return (ctypes.c_void_p * len(addresses))(*addresses)
 
 
+_dtype_of, _shape_of = attrgetter("dtype"), attrgetter("shape")
+
+
 def _check(tensors, name: str, dtype=None):
     """One dtype (this one, where it is given), one GPU, contiguous; returns the dtype."""
     if not all(map(torch.Tensor.is_contiguous, tensors)):
         raise ValueError(f"{name} must be contiguous")
-    if tensors and min(map(torch.Tensor.get_device, tensors)) < 0:
+    devices, dtypes = set(map(torch.Tensor.get_device, tensors)), set(map(_dtype_of, tensors))
+    if tensors and min(devices) < 0:
         raise ValueError(f"{name} must live on the GPU")
-    dtypes = {t.dtype for t in tensors}
-    if len(dtypes | ({dtype} if dtype else set())) > 1 or len(set(map(torch.Tensor.get_device, tensors))) > 1:
+    if len(dtypes | ({dtype} if dtype else set())) > 1 or len(devices) > 1:
         raise ValueError(f"{name} must have one dtype{f' ({dtype})' if dtype else ''} and one device")
     return next(iter(dtypes), torch.float32)
 
@@ -53,6 +57,7 @@ class AdamW:
         self.lr, self.betas, self.eps, self.weight_decay = lr, tuple(betas), eps, weight_decay
         self.state_bits, self.seed, self.steps = state_bits, int(seed), int(steps)
         self._dtype = _check(self.params, "params")
+        self._device = self.params[0].get_device() if self.params else 0
         self._param_dt = binding._dtype_code(self.params[0]) if self.params else binding.F32
         self._numel, self._shapes = [p.numel() for p in self.params], [p.shape for p in self.params]
         self._counts = (ctypes.c_int64 * len(self.params))(*self._numel)
@@ -64,10 +69,11 @@ class AdamW:
         if set(state) != set(names):
             raise ValueError(f"state holds {', '.join(names)}")
         # The states are aliases that nobody else holds, so they stay where they are.  Params and copies are the caller's, who may
-        # give them new storage: their addresses are looked at in every step, and the tensors checked when one has moved.
+        # give them new storage, and other strides or another dtype without a new address: they are checked in every step.
         self._state = {k: [t.detach() for t in state[k]] for k in names}
         for k in names:
             self._check_list(k, self._state[k])
+            self._check_places(k, self._state[k])
         self._state_arrays = [_array([t.data_ptr() for t in self._state[k]]) for k in names] + [None] * (4 - len(names))
         self._seen = {}
         for k in ("params", "copies"):
@@ -79,26 +85,30 @@ class AdamW:
         tensors = getattr(self, name)
         if tensors is None:
             return None
+        self._check_list(name, tensors)
         now = list(map(torch.Tensor.data_ptr, tensors))
         seen = self._seen.get(name)
         if seen is None or seen[0] != now:
-            self._check_list(name, tensors)
+            self._check_places(name, tensors)
             seen = self._seen[name] = (now, _array(now))
         return seen[1]
 
     def _check_list(self, name: str, tensors) -> None:
+        """What the tensors are: all that the kernel takes for granted of them but where they are."""
         scales = name.endswith("_scale")
         _check(tensors, name, {"params": self._dtype, "copies": torch.bfloat16}.get(name) or
                (torch.float32 if scales or self.state_bits == 32 else torch.float8_e4m3fn))
         if scales and [t.numel() for t in tensors] != [-(-n // BLOCK) for n in self._numel]:
             raise ValueError(f"{name} holds one value for each {BLOCK} elements of every param")
-        if not scales and [t.shape for t in tensors] != self._shapes:
+        if not scales and list(map(_shape_of, tensors)) != self._shapes:
             raise ValueError(f"{name} must have the shapes of params")
+        if tensors and tensors[0].get_device() != self._device:
+            raise ValueError(f"{name} must live on the GPU that the optimizer was made on")
+
+    def _check_places(self, name: str, tensors) -> None:
         places = [t.data_ptr() for t in tensors if t.numel()]
         if len(set(places)) != len(places):      # two workgroups would step it at once
             raise ValueError(f"a tensor is twice among {name}")
-        if tensors and tensors[0].get_device() != self.params[0].get_device():
-            raise ValueError(f"{name} must live on the GPU of params")
 
     def _zeros(self):
         def zeros():
@@ -128,10 +138,9 @@ class AdamW:
         dtypes = {g.dtype for g in grads}
         if len(dtypes) != 1 or not all(map(torch.Tensor.is_contiguous, grads)) or [g.shape for g in grads] != self._shapes:
             raise ValueError("gradients must be contiguous, of one dtype and of the params' shapes")
-        device = self.params[0].get_device()
-        if set(map(torch.Tensor.get_device, grads)) != {device}:
+        if set(map(torch.Tensor.get_device, grads)) != {self._device}:
             raise ValueError("gradients must live on the params' GPU")
-        if grad_scale is not None and (grad_scale.get_device() != device or grad_scale.dtype != torch.float32 or grad_scale.numel() != 1):
+        if grad_scale is not None and (grad_scale.get_device() != self._device or grad_scale.dtype != torch.float32 or grad_scale.numel() != 1):
             raise ValueError("grad_scale must be one float32 on the params' GPU")
         step = self.steps + 1
         m, v, m_scale, v_scale = self._state_arrays

@@ -1,0 +1,79 @@
+"""What AdamW.step looks at before it hands addresses to the library, without a GPU: the library is a stand-in that records
+the call, and tensors count as the GPU's."""
+import types
+
+import pytest
+import torch
+
+from paper_2202_00774_amd import binding
+from paper_2202_00774_amd.optim import AdamW
+
+BF16 = torch.bfloat16
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """The library's calls, as lists of addresses: (params, grads, exp_avg, exp_avg_sq, scales, scales, copies)."""
+    seen = []
+
+    def step(count, *rest):
+        seen.append([None if a is None else list(a) for a in rest[:7]])
+        return 0
+
+    monkeypatch.setattr(binding, "load", lambda: types.SimpleNamespace(sdgp_adamw_step=step))
+    monkeypatch.setattr(binding, "_stream", lambda t: 0)
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda t: 0)
+    return seen
+
+
+def optimizer(calls, *shapes, **kw):
+    """Params, their gradients and an optimizer that has made a step."""
+    params, grads = [torch.zeros(s) for s in shapes], [torch.ones(s) for s in shapes]
+    opt = AdamW(params, **kw)
+    opt.step(grads)
+    assert len(calls) == opt.steps == 1 and calls[0][0] == [p.data_ptr() for p in params]
+    return params, grads, opt
+
+
+def refused(opt, grads, calls):
+    with pytest.raises(ValueError):
+        opt.step(grads)
+    assert len(calls) == opt.steps == 1
+
+
+def test_other_strides_at_the_same_address(calls):
+    (p, _), grads, opt = optimizer(calls, (6, 6), (5,))
+    p.data = p.data.t()                                    # square: the shape is what it was
+    refused(opt, grads, calls)
+
+
+def test_another_dtype_at_the_same_address(calls):
+    (p, _), grads, opt = optimizer(calls, (6, 6), (5,))
+    p.data = torch.empty(0, dtype=BF16).set_(p.data.view(BF16).untyped_storage(), 0, (6, 6))
+    assert p.dtype == BF16 and p.is_contiguous()
+    refused(opt, grads, calls)
+
+
+def test_another_size_at_the_same_address(calls):
+    (p, _), grads, opt = optimizer(calls, (6, 6), (5,))
+    p.data = p.data[:3]
+    refused(opt, grads, calls)
+
+
+def test_copies_too(calls):
+    copy = torch.zeros(6, 6, dtype=BF16)
+    (p,), grads, opt = optimizer(calls, (6, 6), copies=[copy])
+    copy.data = copy.data.t()
+    refused(opt, grads, calls)
+    copy.data = torch.zeros(6, 6, dtype=BF16)              # whole again, somewhere else
+    opt.step(grads)
+    assert calls[1][6] == [copy.data_ptr()]
+
+
+def test_params_that_moved_to_another_gpu(calls, monkeypatch):
+    params, grads, opt = optimizer(calls, (6, 6), (5,))
+    for p in params:
+        p.data = p.data.clone()
+    there = {t.data_ptr() for t in (*params, *grads)}
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda t: int(t.data_ptr() in there))
+    refused(opt, grads, calls)                             # the states stayed
