@@ -68,30 +68,32 @@ class AdamW:
         names = ("exp_avg", "exp_avg_sq") + (("exp_avg_scale", "exp_avg_sq_scale") if state_bits == 8 else ())
         if set(state) != set(names):
             raise ValueError(f"state holds {', '.join(names)}")
-        # The states are aliases that nobody else holds, so they stay where they are.  Params and copies are the caller's, who may
-        # give them new storage, and other strides or another dtype without a new address: they are checked in every step.
         self._state = {k: [t.detach() for t in state[k]] for k in names}
+        self._seen = {}
         for k in names:
             self._check_list(k, self._state[k])
-            self._check_places(k, self._state[k])
-        self._state_arrays = [_array([t.data_ptr() for t in self._state[k]]) for k in names] + [None] * (4 - len(names))
-        self._seen = {}
-        for k in ("params", "copies"):
-            self._addresses(k)
+            self._addresses(k, self._state[k])
+        self._checked_addresses("params"), self._checked_addresses("copies")
         # what autograd has to know of: a graph that saved one of these must not go back through the new values
         self._written = [t for t in (*self.params, *(self.copies or ())) if not t.is_inference()]
 
-    def _addresses(self, name: str):
-        tensors = getattr(self, name)
-        if tensors is None:
-            return None
-        self._check_list(name, tensors)
+    # Where the tensors are is looked at in every step: the caller may give params and copies new storage, and free and allocate the
+    # states', which whoever holds state() shares.  Params and copies are the caller's objects, so their strides, shapes and dtypes may
+    # change too, without a new address, and are checked in every step; the states' are aliases of the optimizer's own.
+    def _addresses(self, name: str, tensors):
         now = list(map(torch.Tensor.data_ptr, tensors))
         seen = self._seen.get(name)
         if seen is None or seen[0] != now:
             self._check_places(name, tensors)
             seen = self._seen[name] = (now, _array(now))
         return seen[1]
+
+    def _checked_addresses(self, name: str):
+        tensors = getattr(self, name)
+        if tensors is None:
+            return None
+        self._check_list(name, tensors)
+        return self._addresses(name, tensors)
 
     def _check_list(self, name: str, tensors) -> None:
         """What the tensors are: all that the kernel takes for granted of them but where they are."""
@@ -109,6 +111,8 @@ class AdamW:
         places = [t.data_ptr() for t in tensors if t.numel()]
         if len(set(places)) != len(places):      # two workgroups would step it at once
             raise ValueError(f"a tensor is twice among {name}")
+        if any(t.untyped_storage().nbytes() < (t.storage_offset() + t.numel()) * t.element_size() for t in tensors if t.numel()):
+            raise ValueError(f"the storage of {name} is not there")
 
     def _zeros(self):
         def zeros():
@@ -143,10 +147,11 @@ class AdamW:
         if grad_scale is not None and (grad_scale.get_device() != self._device or grad_scale.dtype != torch.float32 or grad_scale.numel() != 1):
             raise ValueError("grad_scale must be one float32 on the params' GPU")
         step = self.steps + 1
-        m, v, m_scale, v_scale = self._state_arrays
+        states = [self._addresses(k, t) for k, t in self._state.items()]
+        m, v, m_scale, v_scale = states if self.state_bits == 8 else (*states, None, None)
         rc = binding.load().sdgp_adamw_step(
-            len(grads), self._addresses("params"), _array(list(map(torch.Tensor.data_ptr, grads))), m, v, m_scale, v_scale,
-            self._addresses("copies"), self._counts, self._param_dt, binding._dtype_code(grads[0]), self.state_bits, self.lr,
+            len(grads), self._checked_addresses("params"), _array(list(map(torch.Tensor.data_ptr, grads))), m, v, m_scale, v_scale,
+            self._checked_addresses("copies"), self._counts, self._param_dt, binding._dtype_code(grads[0]), self.state_bits, self.lr,
             *self.betas, self.eps, self.weight_decay, step, binding._ptr(grad_scale), (self.seed + step) & (2**64 - 1),
             binding._stream(grads[0]))
         if rc != 0:

@@ -77,3 +77,34 @@ def test_params_that_moved_to_another_gpu(calls, monkeypatch):
     there = {t.data_ptr() for t in (*params, *grads)}
     monkeypatch.setattr(torch.Tensor, "get_device", lambda t: int(t.data_ptr() in there))
     refused(opt, grads, calls)                             # the states stayed
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_states_that_were_put_away_and_brought_back(calls, bits):
+    """Whoever holds state() shares its storage, and may free it and allocate it again between steps."""
+    _, grads, opt = optimizer(calls, (600,), (5,), state_bits=bits)
+    held = opt.state()
+    hold = []
+    for tensors in held.values():
+        for t in tensors:
+            storage, was = t.untyped_storage(), t.data_ptr()
+            size = storage.nbytes()
+            storage.resize_(0)
+            while t.data_ptr() in (0, was):
+                hold.append(torch.empty(size, dtype=torch.uint8))
+                storage.resize_(0), storage.resize_(size)
+    opt.step(grads)
+    for k, name in enumerate(held):
+        assert calls[1][2 + k] == [t.data_ptr() for t in held[name]] != calls[0][2 + k]
+
+
+def test_states_that_are_not_there(calls):
+    _, grads, opt = optimizer(calls, (600,), (5,))
+    storage = opt.state()["exp_avg"][0].untyped_storage()
+    storage.resize_(0)
+    refused(opt, grads, calls)
+    storage.resize_(400)                                   # part of it
+    refused(opt, grads, calls)
+    storage.resize_(2400)
+    opt.step(grads)
+    assert calls[1][2][0] == opt.state()["exp_avg"][0].data_ptr()
