@@ -69,11 +69,10 @@ class AdamW:
         if set(state) != set(names):
             raise ValueError(f"state holds {', '.join(names)}")
         self._state = {k: [t.detach() for t in state[k]] for k in names}
-        self._seen = {}
+        self._seen, self._moved = {}, True      # addresses and their array by name; whether one has changed since they were compared
         for k in names:
             self._check_list(k, self._state[k])
-            self._addresses(k, self._state[k])
-        self._checked_addresses("params"), self._checked_addresses("copies")
+        self._places()
         # what autograd has to know of: a graph that saved one of these must not go back through the new values
         self._written = [t for t in (*self.params, *(self.copies or ())) if not t.is_inference()]
 
@@ -84,7 +83,7 @@ class AdamW:
         now = list(map(torch.Tensor.data_ptr, tensors))
         seen = self._seen.get(name)
         if seen is None or seen[0] != now:
-            self._check_places(name, tensors)
+            self._moved = True
             seen = self._seen[name] = (now, _array(now))
         return seen[1]
 
@@ -94,6 +93,15 @@ class AdamW:
             return None
         self._check_list(name, tensors)
         return self._addresses(name, tensors)
+
+    def _places(self):
+        """(params, copies, states), each an array of addresses or None."""
+        params, copies = self._checked_addresses("params"), self._checked_addresses("copies")
+        states = [self._addresses(k, t) for k, t in self._state.items()]
+        if self._moved:
+            self._check_places()
+            self._moved = False
+        return params, copies, states
 
     def _check_list(self, name: str, tensors) -> None:
         """What the tensors are: all that the kernel takes for granted of them but where they are."""
@@ -107,12 +115,14 @@ class AdamW:
         if tensors and tensors[0].get_device() != self._device:
             raise ValueError(f"{name} must live on the GPU that the optimizer was made on")
 
-    def _check_places(self, name: str, tensors) -> None:
-        places = [t.data_ptr() for t in tensors if t.numel()]
-        if len(set(places)) != len(places):      # two workgroups would step it at once
-            raise ValueError(f"a tensor is twice among {name}")
-        if any(t.untyped_storage().nbytes() < (t.storage_offset() + t.numel()) * t.element_size() for t in tensors if t.numel()):
-            raise ValueError(f"the storage of {name} is not there")
+    def _check_places(self) -> None:
+        """All that a step writes lies apart and within its storage.  (Two workgroups would step an element at once.)"""
+        tensors = [t for ts in (self.params, self.copies or (), *self._state.values()) for t in ts if t.numel()]
+        if any(t.untyped_storage().nbytes() < (t.storage_offset() + t.numel()) * t.element_size() for t in tensors):
+            raise ValueError("the storage of a param, copy or state is not there")
+        spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in tensors)
+        if any(end > begin for (_, end), (begin, _) in zip(spans, spans[1:])):
+            raise ValueError("a tensor is twice among params, copies and states, or two of them share memory")
 
     def _zeros(self):
         def zeros():
@@ -147,11 +157,11 @@ class AdamW:
         if grad_scale is not None and (grad_scale.get_device() != self._device or grad_scale.dtype != torch.float32 or grad_scale.numel() != 1):
             raise ValueError("grad_scale must be one float32 on the params' GPU")
         step = self.steps + 1
-        states = [self._addresses(k, t) for k, t in self._state.items()]
+        params, copies, states = self._places()
         m, v, m_scale, v_scale = states if self.state_bits == 8 else (*states, None, None)
         rc = binding.load().sdgp_adamw_step(
-            len(grads), self._checked_addresses("params"), _array(list(map(torch.Tensor.data_ptr, grads))), m, v, m_scale, v_scale,
-            self._checked_addresses("copies"), self._counts, self._param_dt, binding._dtype_code(grads[0]), self.state_bits, self.lr,
+            len(grads), params, _array(list(map(torch.Tensor.data_ptr, grads))), m, v, m_scale, v_scale,
+            copies, self._counts, self._param_dt, binding._dtype_code(grads[0]), self.state_bits, self.lr,
             *self.betas, self.eps, self.weight_decay, step, binding._ptr(grad_scale), (self.seed + step) & (2**64 - 1),
             binding._stream(grads[0]))
         if rc != 0:

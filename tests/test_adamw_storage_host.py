@@ -108,3 +108,24 @@ def test_states_that_are_not_there(calls):
     storage.resize_(2400)
     opt.step(grads)
     assert calls[1][2][0] == opt.state()["exp_avg"][0].data_ptr()
+
+
+def test_tensors_that_share_memory(calls):
+    room = torch.zeros(1000)
+    ok = AdamW([room[:300], room[300:301], room[301:301], room[301:]])       # side by side
+    with pytest.raises(ValueError, match="share memory"):
+        AdamW([room[:300], room[299:]])
+    with pytest.raises(ValueError, match="share memory"):
+        AdamW([room[:300], room[300:]], copies=[room.view(BF16)[1400:1700], torch.zeros(700, dtype=BF16)])
+    same = [torch.zeros(300), torch.zeros(1), torch.zeros(0), torch.zeros(699)]
+    with pytest.raises(ValueError, match="share memory"):
+        AdamW(ok.params, state={"exp_avg": same, "exp_avg_sq": same})
+    with pytest.raises(ValueError, match="share memory"):
+        AdamW([room[:300]], state={"exp_avg": [room[200:500]], "exp_avg_sq": [torch.zeros(300)]})
+    ok.step([torch.ones(p.shape) for p in ok.params])
+    ok.params[1].data = room[500:501]                                        # into another one's place
+    for _ in range(2):
+        refused(ok, [torch.ones(p.shape) for p in ok.params], calls)
+    ok.params[1].data = torch.zeros(1)
+    ok.step([torch.ones(p.shape) for p in ok.params])
+    assert len(calls) == 2
