@@ -416,7 +416,8 @@ int sdgp_block_norm_bwd(const void* dy, const void* dh, const void* y, const voi
  *               values are stored as NaN.
  *                 v = mix(seed) ^ low word of e ^ (high word of e * 0xBB67AE85), mixed as the random ranker's hash does;
  *               e counts the elements of the call, each tensor from the next multiple of 256.
- *   step        1 for the first one;  seed: another for every step (8-bit states only)
+ *   step        1 for the first one;  seed: another for every step (8-bit states only).  Both are taken as they are now, so a
+ *               captured graph would repeat one step: SDGP_ERR_VALUE on a stream that is being captured
  *   grad_scale  device pointer to one fp32, or NULL for 1: what clipping or loss scaling leaves, read on the stream
  */
 int sdgp_adamw_step(int count, void* const* params, const void* const* grads, void* const* exp_avg,

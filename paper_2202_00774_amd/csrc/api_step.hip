@@ -233,6 +233,14 @@ int sdgp_adamw_step(int count, void* const* params, const void* const* grads, vo
         if (state_bits == 32 && (!aligned(exp_avg[i], 4) || !aligned(exp_avg_sq[i], 4))) return SDGP_ERR_SHAPE;
         if (state_bits == 8 && (!aligned(exp_avg_scale[i], 4) || !aligned(exp_avg_sq_scale[i], 4))) return SDGP_ERR_SHAPE;
     }
+    if (blocks == 0) return SDGP_OK;
+    // the step's number and seed go to the kernel by value: a graph would make this one step again in every replay
+    hipStreamCaptureStatus capturing = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(static_cast<hipStream_t>(hip_stream), &capturing) != hipSuccess) {
+        (void)hipGetLastError();
+        return SDGP_ERR_HIP;
+    }
+    if (capturing != hipStreamCaptureStatusNone) return SDGP_ERR_VALUE;
     const AdamCall c = {count, params, grads, exp_avg, exp_avg_sq, exp_avg_scale, exp_avg_sq_scale, copies, numel, param_dt, grad_dt,
                         static_cast<hipStream_t>(hip_stream)};
     const double bc1 = 1.0 - std::pow(beta1, (double)step), bc2 = 1.0 - std::pow(beta2, (double)step);

@@ -141,8 +141,9 @@ class AdamW:
         return {k: [t.detach() for t in v] for k, v in self._state.items()}
 
     def step(self, grads=None, *, grad_scale: torch.Tensor | None = None) -> None:
-        """One step from ``grads`` (one dtype, fp32 or bf16; default: every param's ``.grad``).  ``grad_scale``: an fp32
-        tensor of one element on the GPU that the gradients are multiplied with (clipping, loss scaling)."""
+        """One step from ``grads`` (one dtype, fp32 or bf16; default: every param's ``.grad``, which must be there).
+        ``grad_scale``: an fp32 tensor of one element on the GPU that the gradients are multiplied with (clipping, loss
+        scaling).  Not inside a captured graph, whose replays would all be this one step."""
         grads = [p.grad for p in self.params] if grads is None else list(grads)
         if len(grads) != len(self.params) or any(g is None for g in grads):
             raise ValueError("one gradient for each param")
@@ -165,6 +166,7 @@ class AdamW:
             *self.betas, self.eps, self.weight_decay, step, binding._ptr(grad_scale), (self.seed + step) & (2**64 - 1),
             binding._stream(grads[0]))
         if rc != 0:
-            raise binding.SdgpError(rc, "sdgp_adamw_step")
+            captured = torch.cuda.is_current_stream_capturing()
+            raise binding.SdgpError(rc, "sdgp_adamw_step" + (" on a stream that is being captured" if captured else ""))
         increment_version(self._written)
         self.steps = step
