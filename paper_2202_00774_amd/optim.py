@@ -29,6 +29,19 @@ def _array(addresses):
 _dtype_of, _shape_of = attrgetter("dtype"), attrgetter("shape")
 
 
+# One call that looks at dtype, device, shape and strides of a list of tensors, where this torch has it.  It stands in for a check in
+# Python that found the same list in order (161 tensors: 16 us instead of 56); what it does not recognise is checked again.
+_guards = getattr(getattr(torch._C, "_dynamo", None), "guards", None)
+
+
+def _recognise(tensors):
+    """A function of tensors: whether they are, in all that ``_check`` looks at and in shape, what these here are."""
+    guard = getattr(_guards, "TensorGuards", None)
+    if guard is None:
+        return lambda *_: False
+    return guard(*tensors, dynamic_dims_sizes=[list(t.shape) for t in tensors], dynamic_dims_strides=[list(t.stride()) for t in tensors]).check
+
+
 def _check(tensors, name: str, dtype=None):
     """One dtype (this one, where it is given), one GPU, contiguous; returns the dtype."""
     if not all(map(torch.Tensor.is_contiguous, tensors)):
@@ -69,35 +82,35 @@ class AdamW:
         if set(state) != set(names):
             raise ValueError(f"state holds {', '.join(names)}")
         self._state = {k: [t.detach() for t in state[k]] for k in names}
+        self._watched = {k: list({t.untyped_storage().data_ptr(): t for t in ts if t.numel()}.values()) for k, ts in self._state.items()}
         self._seen, self._moved = {}, True      # addresses and their array by name; whether one has changed since they were compared
-        for k in names:
-            self._check_list(k, self._state[k])
+        self._same = dict.fromkeys(("params", "copies", "grads"), lambda *_: False)
         self._places()
         # what autograd has to know of: a graph that saved one of these must not go back through the new values
         self._written = [t for t in (*self.params, *(self.copies or ())) if not t.is_inference()]
 
     # Where the tensors are is looked at in every step: the caller may give params and copies new storage, and free and allocate the
     # states', which whoever holds state() shares.  Params and copies are the caller's objects, so their strides, shapes and dtypes may
-    # change too, without a new address, and are checked in every step; the states' are aliases of the optimizer's own.
-    def _addresses(self, name: str, tensors):
-        now = list(map(torch.Tensor.data_ptr, tensors))
+    # change too, without a new address, and are looked at in every step; the states' are aliases of the optimizer's own, and those of
+    # one storage move together, so one of them (`watched`) tells of all.
+    def _addresses(self, name: str, tensors, watched, same=None):
+        now = list(map(torch.Tensor.data_ptr, watched))
         seen = self._seen.get(name)
-        if seen is None or seen[0] != now:
-            self._moved = True
-            seen = self._seen[name] = (now, _array(now))
-        return seen[1]
-
-    def _checked_addresses(self, name: str):
-        tensors = getattr(self, name)
-        if tensors is None:
-            return None
+        if seen is not None and seen[0] == now and (same is None or same(*tensors)):
+            return seen[1]
         self._check_list(name, tensors)
-        return self._addresses(name, tensors)
+        if seen is None or seen[0] != now:
+            seen = self._seen[name] = (now, _array(now if watched is tensors else [t.data_ptr() for t in tensors]))
+            self._moved = True
+        if same is not None:
+            self._same[name] = _recognise(tensors)
+        return seen[1]
 
     def _places(self):
         """(params, copies, states), each an array of addresses or None."""
-        params, copies = self._checked_addresses("params"), self._checked_addresses("copies")
-        states = [self._addresses(k, t) for k, t in self._state.items()]
+        params = self._addresses("params", self.params, self.params, self._same["params"])
+        copies = None if self.copies is None else self._addresses("copies", self.copies, self.copies, self._same["copies"])
+        states = [self._addresses(k, t, self._watched[k]) for k, t in self._state.items()]
         if self._moved:
             self._check_places()
             self._moved = False
@@ -114,6 +127,15 @@ class AdamW:
             raise ValueError(f"{name} must have the shapes of params")
         if tensors and tensors[0].get_device() != self._device:
             raise ValueError(f"{name} must live on the GPU that the optimizer was made on")
+
+    def _check_grads(self, grads) -> None:
+        if any(g is None for g in grads):
+            raise ValueError("one gradient for each param")
+        dtypes = {g.dtype for g in grads}
+        if len(dtypes) != 1 or not all(map(torch.Tensor.is_contiguous, grads)) or [g.shape for g in grads] != self._shapes:
+            raise ValueError("gradients must be contiguous, of one dtype and of the params' shapes")
+        if set(map(torch.Tensor.get_device, grads)) != {self._device}:
+            raise ValueError("gradients must live on the params' GPU")
 
     def _check_places(self) -> None:
         """All that a step writes lies apart and within its storage.  (Two workgroups would step an element at once.)"""
@@ -145,16 +167,14 @@ class AdamW:
         ``grad_scale``: an fp32 tensor of one element on the GPU that the gradients are multiplied with (clipping, loss
         scaling).  Not inside a captured graph, whose replays would all be this one step."""
         grads = [p.grad for p in self.params] if grads is None else list(grads)
-        if len(grads) != len(self.params) or any(g is None for g in grads):
+        if len(grads) != len(self.params):
             raise ValueError("one gradient for each param")
         if not grads:
             self.steps += 1
             return
-        dtypes = {g.dtype for g in grads}
-        if len(dtypes) != 1 or not all(map(torch.Tensor.is_contiguous, grads)) or [g.shape for g in grads] != self._shapes:
-            raise ValueError("gradients must be contiguous, of one dtype and of the params' shapes")
-        if set(map(torch.Tensor.get_device, grads)) != {self._device}:
-            raise ValueError("gradients must live on the params' GPU")
+        if not self._same["grads"](*grads):
+            self._check_grads(grads)
+            self._same["grads"] = _recognise(grads)
         if grad_scale is not None and (grad_scale.get_device() != self._device or grad_scale.dtype != torch.float32 or grad_scale.numel() != 1):
             raise ValueError("grad_scale must be one float32 on the params' GPU")
         step = self.steps + 1
