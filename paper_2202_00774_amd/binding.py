@@ -585,7 +585,7 @@ def sdgp_token_logprobs_bwd(logits: torch.Tensor, tokens: torch.Tensor | None, s
         out = logits.new_empty(logits.shape)
     if out.shape != logits.shape or out.dtype != logits.dtype:
         raise ValueError("out must have the shape and dtype of logits")
-    rc = load().sdgp_token_logprobs_bwd(_ptr(logits), ld, _ptr(tokens), bits, _ptr(stats), _ptr(entropy), _ptr(g_logp),
+    rc = load().sdgp_token_logprobs_bwd(_ptr(logits), ld, None if g_logp is None else _ptr(tokens), bits, _ptr(stats), _ptr(entropy), _ptr(g_logp),
                                         _ptr(g_entropy), _ptr(out), _row_stride(out, "out"), shape.numel(), V, dt, scale,
                                         _stream(logits))
     if rc != 0:

@@ -135,7 +135,7 @@ int sdgp_token_logprobs(const void* logits, int64_t ld, const void* tokens, int 
     if (!positive(scale)) return SDGP_ERR_VALUE;
     if (rows == 0) return SDGP_OK;
     if (!logits || !entropy || !stats || (logp && !tokens) || (top > 0 && (!top_logp || !top_ids))) return SDGP_ERR_NULL;
-    if (!aligned(logits, element(dt)) || !aligned(tokens, token_bits / 8)) return SDGP_ERR_SHAPE;
+    if (!aligned(logits, element(dt)) || (logp && !aligned(tokens, token_bits / 8))) return SDGP_ERR_SHAPE;
     const size_t need = sdgp::token_logprobs_workspace(rows, V, dt, top);
     if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return SDGP_ERR_WORKSPACE;
     return sdgp::token_logprobs_launch(logits, ld, tokens, token_bits, logp, entropy, top_logp, top_ids, stats, rows, V, dt, top, scale,
@@ -152,7 +152,8 @@ int sdgp_token_logprobs_bwd(const void* logits, int64_t ld, const void* tokens, 
     if (!positive(scale)) return SDGP_ERR_VALUE;
     if (rows == 0) return SDGP_OK;
     if (!logits || !stats || !dlogits || (g_logp && !tokens) || (g_entropy && !entropy) || (!g_logp && !g_entropy)) return SDGP_ERR_NULL;
-    if (!aligned(logits, element(dt)) || !aligned(dlogits, element(dt)) || !aligned(tokens, token_bits / 8)) return SDGP_ERR_SHAPE;
+    if (!aligned(logits, element(dt)) || !aligned(dlogits, element(dt))) return SDGP_ERR_SHAPE;
+    if (g_logp && !aligned(tokens, token_bits / 8)) return SDGP_ERR_SHAPE;   // else they are not read
     return sdgp::token_logprobs_bwd_launch(logits, ld, tokens, token_bits, stats, entropy, g_logp, g_entropy, dlogits, ld_out, rows, V,
                                            dt, scale, static_cast<hipStream_t>(hip_stream));
 }
