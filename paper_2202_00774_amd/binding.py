@@ -515,11 +515,23 @@ def _row_stride(t: torch.Tensor, name: str) -> int:
     return ld
 
 
-def _per_row(t: torch.Tensor, shape, name: str, dtypes) -> torch.Tensor:
-    _dev(t, name)
+def _beside(t: torch.Tensor, name: str, x: torch.Tensor) -> torch.Tensor:
+    if t.get_device() != x.get_device():
+        raise ValueError(f"{name} must live on the GPU of the other tensors")
+    return _dev(t, name)
+
+
+def _per_row(t: torch.Tensor, shape, name: str, dtypes, x: torch.Tensor) -> torch.Tensor:
+    _beside(t, name, x)
     if t.shape != shape or t.dtype not in dtypes:
         raise ValueError(f"{name} must be {' or '.join(str(d) for d in dtypes)} {tuple(shape)}")
     return t
+
+
+def _own_workspace(need: int, workspace, x: torch.Tensor, where: str):
+    if workspace is not None:
+        _beside(workspace, "workspace", x)
+    return _workspace(need, workspace, x.device, where)
 
 
 _FLOAT, _INTS = (torch.float32,), (torch.int64, torch.int32)
@@ -537,7 +549,7 @@ def sdgp_token_logprobs(logits: torch.Tensor, tokens: torch.Tensor | None, *, to
     rows = shape.numel()
     bits = 64
     if tokens is not None:
-        _per_row(tokens, shape, "tokens", _INTS)
+        _per_row(tokens, shape, "tokens", _INTS, logits)
         bits = 64 if tokens.dtype == torch.int64 else 32
     lib = load()
     need = _need("sdgp_token_logprobs_workspace", rows, V, dt, top)
@@ -545,7 +557,7 @@ def sdgp_token_logprobs(logits: torch.Tensor, tokens: torch.Tensor | None, *, to
         raise SdgpError(-3, "sdgp_token_logprobs")
     wbytes = 0
     if need:
-        workspace, wbytes = _workspace(need, workspace, logits.device, "sdgp_token_logprobs_workspace")
+        workspace, wbytes = _own_workspace(need, workspace, logits, "sdgp_token_logprobs_workspace")
     entropy = logits.new_empty(shape, dtype=torch.float32)
     logp = None if tokens is None else torch.empty_like(entropy)
     stats = entropy.new_empty((*shape, 2))
@@ -568,23 +580,23 @@ def sdgp_token_logprobs_bwd(logits: torch.Tensor, tokens: torch.Tensor | None, s
     shape, V = logits.shape[:-1], logits.shape[-1]
     if g_logp is None and g_entropy is None:
         raise ValueError("one of g_logp and g_entropy is needed")
-    _per_row(stats, (*shape, 2), "stats", _FLOAT)
+    _per_row(stats, (*shape, 2), "stats", _FLOAT, logits)
     bits = 64
     if g_logp is not None:
         if tokens is None:
             raise ValueError("g_logp needs tokens")
-        _per_row(g_logp, shape, "g_logp", _FLOAT)
-        _per_row(tokens, shape, "tokens", _INTS)
+        _per_row(g_logp, shape, "g_logp", _FLOAT, logits)
+        _per_row(tokens, shape, "tokens", _INTS, logits)
         bits = 64 if tokens.dtype == torch.int64 else 32
     if g_entropy is not None:
         if entropy is None:
             raise ValueError("g_entropy needs entropy")
-        _per_row(g_entropy, shape, "g_entropy", _FLOAT)
-        _per_row(entropy, shape, "entropy", _FLOAT)
+        _per_row(g_entropy, shape, "g_entropy", _FLOAT, logits)
+        _per_row(entropy, shape, "entropy", _FLOAT, logits)
     if out is None:
         out = logits.new_empty(logits.shape)
-    if out.shape != logits.shape or out.dtype != logits.dtype:
-        raise ValueError("out must have the shape and dtype of logits")
+    if out.shape != logits.shape or out.dtype != logits.dtype or out.get_device() != logits.get_device():
+        raise ValueError("out must have the shape, dtype and GPU of logits")
     rc = load().sdgp_token_logprobs_bwd(_ptr(logits), ld, None if g_logp is None else _ptr(tokens), bits, _ptr(stats), _ptr(entropy), _ptr(g_logp),
                                         _ptr(g_entropy), _ptr(out), _row_stride(out, "out"), shape.numel(), V, dt, scale,
                                         _stream(logits))
@@ -595,17 +607,17 @@ def sdgp_token_logprobs_bwd(logits: torch.Tensor, tokens: torch.Tensor | None, s
 
 def _like(t, x: torch.Tensor, name: str):
     if t is not None:
-        _dev(t, name)
+        _beside(t, name, x)
         if t.shape != x.shape or t.dtype != x.dtype:
             raise ValueError(f"{name} must have the shape and dtype of the residual stream")
 
 
-def _gate_and_weights(D: int, rows: int, dtype, gate, w_post, w_pre):
+def _gate_and_weights(D: int, rows: int, x: torch.Tensor, gate, w_post, w_pre):
     """(groups, code of the weights' dtype) of checked arguments."""
     groups = 0
     if gate is not None:
-        _dev(gate, "gate")
-        if gate.shape[-1] != D or gate.dtype != dtype:
+        _beside(gate, "gate", x)
+        if gate.shape[-1] != D or gate.dtype != x.dtype:
             raise ValueError("gate must be [..., D] of the residual stream's dtype")
         groups = gate.numel() // D
         if groups == 0 and rows or groups and rows % groups:
@@ -613,7 +625,7 @@ def _gate_and_weights(D: int, rows: int, dtype, gate, w_post, w_pre):
     wdt = F32
     for w, name in ((w_post, "w_post"), (w_pre, "w_pre")):
         if w is not None:
-            _dev(w, name)
+            _beside(w, name, x)
             if w.shape != (D,):
                 raise ValueError(f"{name} must be [D]")
             wdt = _dtype_code(w)
@@ -640,7 +652,7 @@ def sdgp_block_norm(x: torch.Tensor, u: torch.Tensor | None = None, gate: torch.
         raise ValueError("w_pre is the weight of the norm that pre=False leaves out")
     D = x.shape[-1]
     rows = x.numel() // D
-    groups, wdt = _gate_and_weights(D, rows, x.dtype, gate, w_post, w_pre)
+    groups, wdt = _gate_and_weights(D, rows, x, gate, w_post, w_pre)
     y = x if u is None else torch.empty_like(x)
     h = torch.empty_like(x) if pre else None
     stats = torch.empty((2, rows), dtype=torch.float32, device=x.device)
@@ -665,12 +677,12 @@ def sdgp_block_norm_bwd(dy: torch.Tensor | None, dh: torch.Tensor | None, y: tor
         raise ValueError("gate and w_post belong to a block's output, w_pre to the norm behind it")
     D = y.shape[-1]
     rows = y.numel() // D
-    _per_row(stats, (2, rows), "stats", _FLOAT)
-    groups, wdt = _gate_and_weights(D, rows, y.dtype, gate, w_post, w_pre)
+    _per_row(stats, (2, rows), "stats", _FLOAT, y)
+    groups, wdt = _gate_and_weights(D, rows, y, gate, w_post, w_pre)
     dt = _dtype_code(y)
     lib = load()
-    workspace, wbytes = _workspace(_need("sdgp_block_norm_bwd_workspace", rows, D, groups, dt), workspace, y.device,
-                                   "sdgp_block_norm_bwd_workspace")
+    workspace, wbytes = _own_workspace(_need("sdgp_block_norm_bwd_workspace", rows, D, groups, dt), workspace, y,
+                                       "sdgp_block_norm_bwd_workspace")
     dx = torch.empty_like(y)
     du = None if u is None else torch.empty_like(y)
     dgate = None if gate is None else torch.empty_like(gate)
