@@ -42,10 +42,25 @@ def _recognise(tensors):
     return guard(*tensors, dynamic_dims_sizes=[list(t.shape) for t in tensors], dynamic_dims_strides=[list(t.stride()) for t in tensors]).check
 
 
-def _check(tensors, name: str, dtype=None):
-    """One dtype (this one, where it is given), one GPU, contiguous; returns the dtype."""
-    if not all(map(torch.Tensor.is_contiguous, tensors)):
-        raise ValueError(f"{name} must be contiguous")
+def _layout(p: torch.Tensor):
+    """The order of a param's elements in memory, which has no gaps: the one of its axes, or channels last."""
+    for layout in (torch.contiguous_format, torch.channels_last):
+        if (layout is torch.contiguous_format or p.dim() == 4) and p.is_contiguous(memory_format=layout):
+            return layout
+    raise ValueError("params must be contiguous, or four-dimensional with the channels last")
+
+
+def _in_order(tensors, layouts) -> bool:
+    """Whether the tensors lie as the params do (``layouts``: theirs, None where all are contiguous)."""
+    if layouts is None:
+        return all(map(torch.Tensor.is_contiguous, tensors))
+    return len(tensors) == len(layouts) and all(t.is_contiguous(memory_format=k) for t, k in zip(tensors, layouts) if t.dim() == 4 or k is torch.contiguous_format)
+
+
+def _check(tensors, name: str, dtype=None, layouts=None):
+    """One dtype (this one, where it is given), one GPU, laid out as the params; returns the dtype."""
+    if not _in_order(tensors, layouts):
+        raise ValueError(f"{name} must be contiguous, or lie in memory as the params do")
     devices, dtypes = set(map(torch.Tensor.get_device, tensors)), set(map(_dtype_of, tensors))
     if tensors and min(devices) < 0:
         raise ValueError(f"{name} must live on the GPU")
@@ -57,6 +72,8 @@ def _check(tensors, name: str, dtype=None):
 class AdamW:
     """Holds the states of ``params`` and steps them in place.
 
+    Params are contiguous, or four-dimensional with the channels last; gradients, copies and states lie in memory as their
+    param does, and an 8-bit state's blocks are runs of that memory.  Every param has a gradient in every step.
     ``copies``: bf16 tensors of the (fp32) params' shapes that every step writes the new values to as well.  ``state``:
     tensors to go on from instead of zeros, a dict of lists as ``state()`` returns it, ``steps`` the steps they have seen.
     """
@@ -69,7 +86,9 @@ class AdamW:
         self.copies = None if copies is None else list(copies)
         self.lr, self.betas, self.eps, self.weight_decay = lr, tuple(betas), eps, weight_decay
         self.state_bits, self.seed, self.steps = state_bits, int(seed), int(steps)
-        self._dtype = _check(self.params, "params")
+        layouts = list(map(_layout, self.params))
+        self._layouts = layouts if torch.channels_last in layouts else None
+        self._dtype = _check(self.params, "params", None, self._layouts)
         self._device = self.params[0].get_device() if self.params else 0
         self._param_dt = binding._dtype_code(self.params[0]) if self.params else binding.F32
         self._numel, self._shapes = [p.numel() for p in self.params], [p.shape for p in self.params]
@@ -120,7 +139,7 @@ class AdamW:
         """What the tensors are: all that the kernel takes for granted of them but where they are."""
         scales = name.endswith("_scale")
         _check(tensors, name, {"params": self._dtype, "copies": torch.bfloat16}.get(name) or
-               (torch.float32 if scales or self.state_bits == 32 else torch.float8_e4m3fn))
+               (torch.float32 if scales or self.state_bits == 32 else torch.float8_e4m3fn), None if scales else self._layouts)
         if scales and [t.numel() for t in tensors] != [-(-n // BLOCK) for n in self._numel]:
             raise ValueError(f"{name} holds one value for each {BLOCK} elements of every param")
         if not scales and list(map(_shape_of, tensors)) != self._shapes:
@@ -132,8 +151,8 @@ class AdamW:
         if any(g is None for g in grads):
             raise ValueError("one gradient for each param")
         dtypes = {g.dtype for g in grads}
-        if len(dtypes) != 1 or not all(map(torch.Tensor.is_contiguous, grads)) or [g.shape for g in grads] != self._shapes:
-            raise ValueError("gradients must be contiguous, of one dtype and of the params' shapes")
+        if len(dtypes) != 1 or not _in_order(grads, self._layouts) or [g.shape for g in grads] != self._shapes:
+            raise ValueError("gradients must lie in memory as the params do, be of one dtype and of the params' shapes")
         if set(map(torch.Tensor.get_device, grads)) != {self._device}:
             raise ValueError("gradients must live on the params' GPU")
 
@@ -149,8 +168,8 @@ class AdamW:
     def _zeros(self):
         def zeros():
             if self.state_bits == 32:
-                return [torch.zeros_like(p, dtype=torch.float32, memory_format=torch.contiguous_format) for p in self.params]
-            return [torch.zeros(p.shape, dtype=torch.uint8, device=p.device).view(torch.float8_e4m3fn) for p in self.params]   # e4m3's 0 is 0
+                return [torch.zeros_like(p, dtype=torch.float32) for p in self.params]
+            return [torch.zeros_like(p, dtype=torch.uint8).view(torch.float8_e4m3fn) for p in self.params]   # e4m3's 0 is 0
 
         state = {"exp_avg": zeros(), "exp_avg_sq": zeros()}
         if self.state_bits == 8:
