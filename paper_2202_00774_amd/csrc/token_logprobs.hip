@@ -488,7 +488,7 @@ __global__ void __launch_bounds__(kBlock) logprob_grad(const LogprobsGrad q) {
         }
         const bool empty = logs == -INFINITY;
         const float l2 = mul_rn(empty ? 0.0f : logs, kLog2e), off = empty ? 0.0f : fmaf(logs, kLog2e, -l2), back = exp2_hw(-off);
-        if (empty) g = h = 0.0f;
+        if (empty) g = token >= q.V ? NAN : 0.0f, h = 0.0f;
         const float B = -h * kLn2 * back, A = -(g + h * (H - kLn2 * off)) * back;
         const int64_t at = token - first;   // the token's place in this chunk
 #pragma unroll

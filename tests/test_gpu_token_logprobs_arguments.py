@@ -20,3 +20,19 @@ def test_entropy_alone_with_32_bit_tokens_that_start_anywhere():
         assert torch.equal(leaf.grad, want)
     _, entropy, _, _, stats = sdgp.sdgp_token_logprobs(x, room[1:6])
     assert torch.equal(sdgp.sdgp_token_logprobs_bwd(x, room[1:6], stats, entropy, None, torch.ones(5, device="cuda")), want)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [9, 300, 9001])
+def test_a_token_outside_the_vocabulary_of_a_row_that_leaves_nothing(dtype, V):
+    """NaN, forward and in the gradient, as in any other row: what is not a token is not an empty row's business."""
+    x = torch.full((4, V), -float("inf"), device="cuda", dtype=dtype)
+    x[3] = 1.0
+    tokens = torch.tensor([V, 0, -1, V + 5], device="cuda")
+    logp, entropy, _, _, stats = sdgp.sdgp_token_logprobs(x, tokens)
+    assert torch.equal(torch.isnan(logp), torch.tensor([True, False, False, True], device="cuda")) and logp[1] == -float("inf") and logp[2] == 0
+    g = torch.ones(4, device="cuda")
+    for h in (None, g):
+        d = sdgp.sdgp_token_logprobs_bwd(x, tokens, stats, entropy, g, h)
+        assert torch.isnan(d[0]).all() and (d[1:3] == 0).all() and torch.isnan(d[3]).all()
+    assert (sdgp.sdgp_token_logprobs_bwd(x, tokens, stats, entropy, None, g)[:3] == 0).all()
