@@ -338,7 +338,7 @@ int sdgp_conv_bwd_weight(const void* D, const void* dO, float* dW, int64_t B, in
  *   V         1 .. 2^30
  *   tokens    [rows] int32 or int64 (token_bits), NULL with logp NULL.  A token < 0 is none: its log probability is 0
  *             and no gradient comes from it.  A token >= V gives NaN (and a row of NaN as gradient).
- *   scale     > 0, what the logits are multiplied with first (one over the temperature)
+ *   scale     > 0, at most 2^127: what the logits are multiplied with first (one over the temperature)
  *   logp      [rows] fp32 or NULL: ln p(token), p = softmax(scale * logits)
  *   entropy   [rows] fp32: -sum p ln p, in nats; 0 ln 0 = 0
  *   top_ids, top_logp  [rows, top] int64 and fp32, 0 <= top <= min(64, V): the most probable tokens, best first, equal

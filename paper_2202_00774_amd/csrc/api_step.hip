@@ -48,7 +48,7 @@ int check_logits(int64_t rows, int64_t V, int64_t ld, int dt, int top) {
     return top < 0 || top > kMaxTop || top > V ? SDGP_ERR_SHAPE : SDGP_OK;
 }
 
-bool positive(double x) { return std::isfinite(x) && x > 0.0; }
+bool scale_fits(float x) { return x > 0.0f && x <= 0x1p127f; }   // times log2(e) it has an fp32 value
 
 // groups gates for rows rows: none, or a number that divides the rows.
 int check_norm(int64_t rows, int64_t D, int64_t groups, int dt, int wdt) {
@@ -132,7 +132,7 @@ int sdgp_token_logprobs(const void* logits, int64_t ld, const void* tokens, int 
     const int rc = check_logits(rows, V, ld, dt, top);
     if (rc != SDGP_OK) return rc;
     if (token_bits != 32 && token_bits != 64) return SDGP_ERR_DTYPE;
-    if (!positive(scale)) return SDGP_ERR_VALUE;
+    if (!scale_fits(scale)) return SDGP_ERR_VALUE;
     if (rows == 0) return SDGP_OK;
     if (!logits || !entropy || !stats || (logp && !tokens) || (top > 0 && (!top_logp || !top_ids))) return SDGP_ERR_NULL;
     if (!aligned(logits, element(dt)) || (logp && !aligned(tokens, token_bits / 8))) return SDGP_ERR_SHAPE;
@@ -149,7 +149,7 @@ int sdgp_token_logprobs_bwd(const void* logits, int64_t ld, const void* tokens, 
     if (rc == SDGP_OK) rc = check_logits(rows, V, ld_out, dt, 0);
     if (rc != SDGP_OK) return rc;
     if (token_bits != 32 && token_bits != 64) return SDGP_ERR_DTYPE;
-    if (!positive(scale)) return SDGP_ERR_VALUE;
+    if (!scale_fits(scale)) return SDGP_ERR_VALUE;
     if (rows == 0) return SDGP_OK;
     if (!logits || !stats || !dlogits || (g_logp && !tokens) || (g_entropy && !entropy) || (!g_logp && !g_entropy)) return SDGP_ERR_NULL;
     if (!aligned(logits, element(dt)) || !aligned(dlogits, element(dt))) return SDGP_ERR_SHAPE;
