@@ -110,7 +110,7 @@ def check(t, residual_scale=1.0, eps=1e-6, pre=True, sharp=0.1):
             near(dw, sums[key][0], bound, "dw_" + key)
     if gates:
         bound = E * (min(per, deep) + 8 * N) * gate_sums[1] + store * gate_sums[0].abs()
-        assert bound.square().mean() < 0.01 * gate_sums[0].square().mean()
+        assert bound.square().mean() < sharp ** 2 * gate_sums[0].square().mean()
         near(dgate.view(gates, D), gate_sums[0], bound, "dgate")
     again = sdgp.sdgp_block_norm_bwd(*args, residual_scale=residual_scale)
     for p, q in zip(got, again):
