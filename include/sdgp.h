@@ -347,8 +347,9 @@ int sdgp_conv_bwd_weight(const void* D, const void* dO, float* dW, int64_t B, in
  *   stats     [rows, 2] fp32: the largest logit and ln of the sum of exp(scale * (logit - largest)), for the gradient
  *
  * Sums are fp32.  -inf (a token that is not allowed) and the type's lowest value are fine anywhere.  A row that leaves
- * nothing (-inf throughout) has ln p = -inf, entropy 0 and no alternatives; its gradient is 0.  A row with a NaN or +inf
- * has NaN in every number and -1 in every index.
+ * nothing (-inf throughout) has ln p = -inf, entropy 0 and no alternatives; its gradient is 0 (that of a token >= V NaN
+ * here too).  A row with a NaN or +inf has NaN in every number and -1 in every index, but for the log probability 0 of a
+ * row without a token and the largest logit in its stats.  Probabilities below 2^-126 count as 0.
  *
  * sdgp_token_logprobs_bwd -- dL/dlogits from dL/dlogp and dL/dentropy (either may be NULL; the alternatives have none):
  *   dlogits[j] = scale * (g (j == token) - g p_j - h p_j (ln p_j + entropy)), row stride ld_out; dlogits may be logits.
@@ -379,8 +380,8 @@ int sdgp_token_logprobs_bwd(const void* logits, int64_t ld, const void* tokens, 
  *   w_post, w_pre  [D] of `wdt` (fp32 or bf16), or NULL for ones
  *   h         NULL: no norm follows (then w_pre is NULL too)
  *   stats     [2, rows] fp32: the two norms' factors 1/sqrt(...), for the gradient
- *   x, u, y, h, gate `dt`; arithmetic fp32.  rows % groups == 0, 1 <= D <= 2^20.  Outputs overlap no
- *             input.
+ *   x, u, y, h, gate `dt`; arithmetic fp32, the sums of squares too: a row whose squares add up to 2^128 or more has the
+ *             factor 0.  rows % groups == 0, 1 <= D <= 2^20.  Outputs overlap no input.
  *
  * sdgp_block_norm_bwd -- dL/dx, dL/du, dL/dgate and the weights' gradients from dy (of the stored y; NULL: 0) and dh (NULL
  * with h NULL).  y is x where there was no block.  dx, du, dgate `dt`; dw_post, dw_pre [D] fp32, present exactly where the
@@ -405,7 +406,7 @@ int sdgp_block_norm_bwd(const void* dy, const void* dh, const void* y, const voi
  *
  *   params, grads, exp_avg, exp_avg_sq, exp_avg_scale, exp_avg_sq_scale, copies, numel: HOST arrays of `count` entries
  *   (read before the call returns) of device pointers and element counts; every tensor contiguous, none overlapping another.
- *   params      `param_dt`; grads `grad_dt`
+ *   params      `param_dt` (bf16 ones are rounded to the nearest: what moves one by less than half a unit is lost); grads `grad_dt`
  *   copies      bf16 copies of fp32 parameters, written beside them, or NULL
  *   state_bits  32: exp_avg, exp_avg_sq hold m and v in fp32, the scale arrays are NULL.
  *               8:  they hold m and sqrt(v) as e4m3 codes (uint8), one scale for 256 consecutive elements in

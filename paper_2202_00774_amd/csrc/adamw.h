@@ -7,8 +7,8 @@ namespace sdgp {
 
 constexpr int kAdamBlock = 256;                       // elements that share a scale in an 8-bit state
 // Blocks of a workgroup: four wavefronts with four each in flight for fp32 states, one each for 8-bit ones, where a block's
-// arithmetic is what a wavefront waits for (24 x 8388608 elements: fp32 1010 us with 16, 1020 with 4; 8 bits 563 and 547; ResNet-50's
-// tensors in 8 bits 104 and 91).
+// arithmetic is what a wavefront waits for (with 16 and with 4 a workgroup: 24 x 8388608 elements in fp32 1011 and 1020 us, in 8 bits
+// 562 and 561; ResNet-50's tensors in fp32 135 and 132, in 8 bits 105 and 91).
 constexpr int adam_tile(int bits) { return bits == 8 ? 4 : 16; }
 constexpr int64_t kAdamLaunch = (int64_t)1 << 22;     // tiles of a launch: its threads are counted in 32 bits
 constexpr int64_t kAdamPart = (int64_t)1 << 31;       // elements of a tensor in one launch: counted in 32 bits, whole tiles

@@ -3,8 +3,9 @@
 //   g = grad * grad_scale;  m = b1 m + (1 - b1) g;  v = b2 v + (1 - b2) g^2
 //   p = p (1 - lr wd) - lr / (1 - b1^t) * m / (sqrt(v) / sqrt(1 - b2^t) + eps)
 //
-// States in 8 bits hold m and r = sqrt(v) as e4m3 codes with one scale, a power of two, for each 256 elements: codes
-// reach down to 2^-18 of a block's largest value, and with the root stored that is 2^-18 of the largest step size too.
+// States in 8 bits hold m and r = sqrt(v) as e4m3 codes with one scale, a power of two, for each 256 elements: the
+// smallest code is 2^-9 where a block's largest value is between 224 and 448, so codes reach down to 2^-17 of it, and with the
+// root stored that is 2^-17 of the largest step size too.
 // Both are rounded up or down at random, with the probability of what is cut off: v moves by a thousandth a step, far
 // less than half the distance of two codes, so rounded to the nearest it would never move again.  The random word is
 // the library's counter hash of (seed, element), so a step can be repeated bit for bit.  A root that is not zero is not
@@ -13,10 +14,10 @@
 //
 // Bound by memory: 28 bytes an element with fp32 states (parameter and both states in and out, gradient in), 16 with 8-bit
 // ones.  A wavefront takes a block of 256 elements, four a lane, so a block's scale is a maximum over one wavefront.  A
-// workgroup's tile of blocks lies in one tensor, which it looks up in the arguments.  In 8 bits an element costs 84 vector
-// instructions, 89 % of what fits beside its 16 bytes: codes are cut from the float's bits, and what only infinities and NaN
-// need is done where a block has them.  Measured: 24 x 8388608 elements in 8 bits 547 us (5.9 TB/s), in fp32 1010 (6.0 TB/s);
-// ResNet-50's 161 tensors 88 and 135.
+// workgroup's tile of blocks lies in one tensor, which it looks up in the arguments.  In 8 bits an element costs 91 vector
+// instructions, ten of them the step's division: codes are cut from the float's bits, and what only infinities and NaN
+// need is done where a block has them.  Measured: 24 x 8388608 elements with bf16 gradients in 8 bits 562 us (5.8 TB/s; at 2.4 GHz the
+// vector pipes issue for 465 of them), in fp32 1010 (6.0 TB/s); ResNet-50's 161 tensors 91 and 135.
 #include "adamw.h"
 
 #include "rows.h"
@@ -73,8 +74,8 @@ typedef uint32_t u32x2_half_aligned __attribute__((ext_vector_type(2), aligned(2
 typedef uint32_t u32_any __attribute__((aligned(1), may_alias));
 
 // Four values of a lane: elements e .. e + 3 of a tensor of n.  What lies outside is 0 and is neither read nor written.
-// Everything passes by once a step, so loads and stores have the streaming hint (634 us without, 568 with it, for 24 x 8388608
-// elements in 8 bits; 157 and 137 for ResNet-50's tensors in fp32).
+// Everything passes by once a step, so loads and stores have the streaming hint (582 us without, 562 with it, for 24 x 8388608
+// elements in 8 bits; 1112 and 1011 in fp32; 156 and 136 for ResNet-50's tensors in fp32).
 template <int DT>
 __device__ __forceinline__ void load4(const void* p, int64_t e, int64_t n, float (&f)[4]) {
     if (e + 4 <= n) {

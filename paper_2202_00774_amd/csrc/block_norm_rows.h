@@ -1,7 +1,7 @@
 // Block norms of rows that fit the registers, forward and backward (the formulas stand in block_norm.hip).
 //
 // Bound by memory: 8 bytes an element forward (x, u in; y, h out), 12 backward (y, u, dy, dh in; dx, du out) in bf16, with
-// 25 and 34 vector instructions beside them.  Measured: 32768 x 4096 bf16 forward 195 us (5.5 TB/s), backward 280 (5.8 TB/s) and 6
+// 25 and 34 vector instructions beside them.  Measured: 32768 x 4096 bf16 forward 202 us (5.3 TB/s), backward 280 (5.8 TB/s) and 6
 // for the slabs' sums; 16384 x 2048 with 16 gates 45, 67 and 6.  Every value is loaded once and stays in registers, packed as stored,
 // until its row's sums are known.  Backward, the second norm's sum depends on the first's result (dY holds the
 // mean of dn t), but linearly: with v = dy + r_y dn,
@@ -144,7 +144,7 @@ __device__ __forceinline__ void load(Row<DT, NV>& row, const NormGrad& n, int64_
 }
 
 // MODE: kNoBlock, or how the slab is cut; kRowGates: whole groups of one row each, whose gate's gradient needs no sum
-// (4099 x 1001 fp32 57.5 us, 58.5 as kWholeGroups; 4096 x 8192 bf16 199 and 221, both directions).
+// (4099 x 1001 fp32 57.3 us, 58.5 as kWholeGroups; 4096 x 8192 bf16 197 and 219, both directions).
 constexpr int kNoBlock = 2, kRowGates = 3;
 
 template <int DT, int T, int NV, int MODE, Caching RESULTS>
@@ -163,8 +163,9 @@ __global__ void __launch_bounds__(norm_block<T>()) norm_bwd(const NormGrad n) {
     // turn: that takes 25 registers, and a third or fourth wavefront a SIMD hides more (16384 x 2048: 134 us, without 124).
     constexpr bool kHeld = NV == 1;
     // Where gates are many a gate stays as it is stored, beside w_post, and k is computed for every row, so that nothing waits
-    // for the gate before the row's loads are on their way (20000 x 1001 fp32, a gate a row: 267 us without, 245 with it); not with
-    // 1024 threads, whose 128 registers do not hold both (4096 x 8192 bf16 220 us, with it 234).
+    // for the gate before the row's loads are on their way (20000 x 1001 fp32, a gate a row, both directions: 266 us without, 240 with
+    // it).  With 1024 threads, of 128 registers each, k is computed beforehand (4096 x 8192 bf16, a gate a row, 197 us either way; the gradient
+    // of 16400 x 8000 with eight rows a gate 491, as stored 497; with a gate a row 4100 x 8000 184, as stored 164).
     constexpr bool kRaw = kHeld && T < 1024 && kWhole;
     float w_pre[NV][N], k[NV][N];   // k: w_post where kRaw
     V gates[NV];

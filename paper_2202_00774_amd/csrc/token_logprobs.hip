@@ -10,10 +10,10 @@
 // weighted sum they are cut at -256 (in powers of two), where e^ is 0 already, so that a logit of -inf adds 0 and not
 // 0 * inf.  All sums are fp32.
 //
-// Bound by memory where rows are many: 2 bytes an element read forward, 4 read and written backward in bf16, with 8 and 12
-// vector instructions beside them, one an exponential.  A row is one workgroup's (or, where rows are short and many, one
+// Bound by memory where rows are many: 2 bytes an element read forward, 4 read and written backward in bf16, with 8 vector
+// instructions beside them forward, 10 backward and 12 with the entropy's gradient, one an exponential.  A row is one workgroup's (or, where rows are short and many, one
 // wavefront's); few long rows are cut into pieces, whose sums and lists a second kernel joins.  Measured: 8192 x 65536 bf16
-// forward 167 us (6.4 TB/s), gradient 345 (6.2 TB/s); 4 x 131072 with eight alternatives 9 + 5 us, which are latencies.
+// forward 169 us (6.4 TB/s), gradient 353 (6.1 TB/s); 4 x 131072 with eight alternatives 9 + 5 us, which are latencies.
 #include "rows.h"
 
 namespace sdgp {
@@ -26,6 +26,8 @@ constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f
 constexpr float kFloor2 = -256.0f;   // exponents of two below this count as this: 2^-256 is 0 in fp32
 constexpr int kMaxTop = 64;          // a wavefront keeps its best logits one a lane
 
+// 2^x by the one instruction: good to a unit in the last place, and 0 below 2^-126.  So a probability that small counts as 0: beside
+// the row's largest term, which is 1, that is nothing; in the gradient it is what the type hardly holds.
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // max, sum of 2^(c (x - max)), sum of 2^(c (x - max)) * c (x - max)
@@ -456,8 +458,8 @@ struct LogprobsGrad {
 };
 
 // T threads on a chunk of a row, VECS vectors each.  The gradient is p (A + B log2 p) with A and B the row's, and
-// log2 p = c (x - m) - log2(sum) a difference and a fused operation; what rounding log2(sum) cut off is in A and B.  Seven
-// instructions an element and the exponential.
+// log2 p = c (x - m) - log2(sum) a difference and a fused operation; what rounding log2(sum) cut off is in A and B.  Counted:
+// 9.6 vector instructions an element, 11.8 with the entropy.
 template <int DT, int T, int VECS, bool ENTROPY, Caching BOTH>
 __global__ void __launch_bounds__(kBlock) logprob_grad(const LogprobsGrad q) {
     using V = RowVec<DT>;
@@ -515,7 +517,11 @@ __global__ void __launch_bounds__(kBlock) logprob_grad(const LogprobsGrad q) {
 unsigned grid_of(int64_t items) { return (unsigned)(items < (1 << 20) ? items : (1 << 20)); }
 
 // How rows are cut.  A workgroup looks through 2 * 256 vectors at once, so a piece is at least one such chunk; rows that
-// are fewer than the workgroups the chip holds are cut until there are about 1024 pieces.
+// are fewer than the workgroups the chip holds are cut until there are about 1024 pieces.  bf16, in pieces and whole: 4 x 131072 5.7
+// and 13.9 us, 128 x 131072 12.3 and 15.4, 256 x 131072 19.5 and 24.4; near the rule's end the second kernel costs more than the
+// pieces bring, 256 x 50021 11.1 and 10.0, 511 x 131072 31.6 and 29.0.  Rows of one chunk are many from 1024 on: a wavefront each
+// and a workgroup each 3.7 and 4.7 us at 1024 x 1000, 5.7 and 5.5 at 1024 x 4000, 8.5 and 16.6 at 8192 x 1000, but 4.8 and
+// 3.9 at 256 x 4000, and 12.6 and 9.3 there with five alternatives.
 struct Cut {
     int threads, pieces, piece;
 };
@@ -568,7 +574,9 @@ int launch_grad(LogprobsGrad q, hipStream_t stream) {
 
 // Logits that a 256 MB cache keeps nothing of for the gradient are read with the streaming hint, where rows begin on 16 bytes
 // (forward of 8192 x 65536 bf16 182 us without, 167 with it); and from 80 MB on logits and gradients pass by the caches in
-// the backward kernel (2048 x 32768 bf16, both directions, 86 and 77 us).
+// the backward kernel.  By itself that kernel is always quicker so (bf16 x 32768, kept and past: 16 MB 9.7 and 7.5 us, 84 MB
+// 36.2 and 32.4, 268 MB 99 and 94); but what is kept is there for the layer that reads the gradient next (forward, gradient and a pruned
+// layer of 256 inputs: 67 MB 210 and 240 us, 84 MB 218 and 249, 134 MB 265 and 279, 268 MB 364 and 354).
 static bool larger_than(int64_t megabytes, int64_t rows, int64_t V, int dt) { return rows * V * (dt == SDGP_BF16 ? 2 : 4) > megabytes << 20; }
 
 size_t token_logprobs_workspace(int64_t rows, int64_t V, int dt, int top) {

@@ -6,7 +6,7 @@
 
 An 8-bit state holds e4m3 codes (``torch.float8_e4m3fn`` tensors of the parameters' shapes) with one power of two for each
 256 elements, the first moment and the square root of the second, rounded up or down at random by the library's counter
-hash of ``seed + step``: a step can be repeated bit for bit.  14 bytes of memory traffic an element instead of 28 with an
+hash of ``seed + step``: a step can be repeated bit for bit.  16 bytes of memory traffic an element instead of 28 with an
 fp32 parameter and gradient.
 """
 from __future__ import annotations
