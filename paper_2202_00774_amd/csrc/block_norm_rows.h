@@ -184,11 +184,12 @@ __global__ void __launch_bounds__(norm_block<T>()) norm_bwd(const NormGrad n) {
     for (int64_t q0 = gate0; q0 < gate1; q0 += kWhole ? R : 1) {
         const int64_t q = kWhole ? q0 + sub : q0;
         const bool mine = q < gate1;
+        const int Dg = mine ? n.D : 0;   // threads without a gate hold zeros, not another's: 0 times its infinities is a NaN
         const char* gate_row = static_cast<const char*>(n.gate) + (mine ? q : gate0) * n.D * kSize;
         const auto gated = [&](int e, float (&kv)[N]) {
             load_weights<N>(n.w_post, n.wdt, e, n.D, kv);
             if (n.gate == nullptr) return;
-            const V g = load_row<DT>(gate_row, e, n.D);
+            const V g = load_row<DT>(gate_row, e, Dg);
 #pragma unroll
             for (int i = 0; i < N; ++i) kv[i] *= g.get(i);
         };
@@ -196,7 +197,7 @@ __global__ void __launch_bounds__(norm_block<T>()) norm_bwd(const NormGrad n) {
         if constexpr (BLOCK) {
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
-                if constexpr (kRaw) gates[v] = load_row<DT>(gate_row, (v * T + t) * N, n.D);
+                if constexpr (kRaw) gates[v] = load_row<DT>(gate_row, (v * T + t) * N, Dg);
                 else if constexpr (kHeld) gated((v * T + t) * N, k[v]);
 #pragma unroll
                 for (int i = 0; i < N; ++i) sum_gate[v][i] = 0.0f;
@@ -293,7 +294,7 @@ __global__ void __launch_bounds__(norm_block<T>()) norm_bwd(const NormGrad n) {
                     for (int i = 0; i < N; ++i) w[i] = k[v][i];
                 } else {
                     load_weights<N>(n.w_post, n.wdt, e, n.D, w);
-                    g = load_row<DT>(gate_row, e, n.D);
+                    g = load_row<DT>(gate_row, e, Dg);
                 }
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
