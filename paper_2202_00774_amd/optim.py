@@ -101,38 +101,32 @@ class AdamW:
         if set(state) != set(names):
             raise ValueError(f"state holds {', '.join(names)}")
         self._state = {k: [t.detach() for t in state[k]] for k in names}
-        self._watched = {k: list({t.untyped_storage().data_ptr(): t for t in ts if t.numel()}.values()) for k, ts in self._state.items()}
-        self._seen, self._moved = {}, True      # addresses and their array by name; whether one has changed since they were compared
-        self._same = dict.fromkeys(("params", "copies", "grads"), lambda *_: False)
+        # the states of one storage move together: one of them tells of all
+        self._followed = list({t.untyped_storage().data_ptr(): t for ts in self._state.values() for t in ts if t.numel()}.values())
+        self._seen, self._arrays, self._same, self._same_grads = None, None, lambda *_: False, lambda *_: False
         self._places()
         # what autograd has to know of: a graph that saved one of these must not go back through the new values
         self._written = [t for t in (*self.params, *(self.copies or ())) if not t.is_inference()]
 
-    # Where the tensors are is looked at in every step: the caller may give params and copies new storage, and free and allocate the
-    # states', which whoever holds state() shares.  Params and copies are the caller's objects, so their strides, shapes and dtypes may
-    # change too, without a new address, and are looked at in every step; the states' are aliases of the optimizer's own, and those of
-    # one storage move together, so one of them (`watched`) tells of all.
-    def _addresses(self, name: str, tensors, watched, same=None):
-        now = list(map(torch.Tensor.data_ptr, watched))
-        seen = self._seen.get(name)
-        if seen is not None and seen[0] == now and (same is None or same(*tensors)):
-            return seen[1]
-        self._check_list(name, tensors)
-        if seen is None or seen[0] != now:
-            seen = self._seen[name] = (now, _array(now if watched is tensors else [t.data_ptr() for t in tensors]))
-            self._moved = True
-        if same is not None:
-            self._same[name] = _recognise(tensors)
-        return seen[1]
-
     def _places(self):
-        """(params, copies, states), each an array of addresses or None."""
-        params = self._addresses("params", self.params, self.params, self._same["params"])
-        copies = None if self.copies is None else self._addresses("copies", self.copies, self.copies, self._same["copies"])
-        states = [self._addresses(k, t, self._watched[k]) for k, t in self._state.items()]
-        if self._moved:
+        """(params, copies, states): arrays of addresses, None for what there is not.
+
+        Where the tensors are is looked at in every step: the caller may give params and copies new storage, and free and allocate
+        the states', which whoever holds state() shares.  Params and copies are the caller's objects, so their strides, shapes and
+        dtypes may change too, without a new address, and are looked at as well; the states' are aliases of the optimizer's own."""
+        theirs = self.params if self.copies is None else self.params + self.copies
+        now = list(map(torch.Tensor.data_ptr, theirs + self._followed))
+        if now != self._seen or not self._same(*theirs):
+            self._check_list("params", self.params)
+            if self.copies is not None:
+                self._check_list("copies", self.copies)
+            for name, tensors in self._state.items():
+                self._check_list(name, tensors)
             self._check_places()
-            self._moved = False
+            lists = (self.params, self.copies, *self._state.values())
+            self._arrays = [None if ts is None else _array([t.data_ptr() for t in ts]) for ts in lists]
+            self._seen, self._same = now, _recognise(theirs)
+        params, copies, *states = self._arrays
         return params, copies, states
 
     def _check_list(self, name: str, tensors) -> None:
@@ -191,9 +185,9 @@ class AdamW:
         if not grads:
             self.steps += 1
             return
-        if not self._same["grads"](*grads):
+        if not self._same_grads(*grads):
             self._check_grads(grads)
-            self._same["grads"] = _recognise(grads)
+            self._same_grads = _recognise(grads)
         if grad_scale is not None and (grad_scale.get_device() != self._device or grad_scale.dtype != torch.float32 or grad_scale.numel() != 1):
             raise ValueError("grad_scale must be one float32 on the params' GPU")
         step = self.steps + 1
