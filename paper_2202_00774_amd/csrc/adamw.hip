@@ -16,8 +16,8 @@
 // ones.  A wavefront takes a block of 256 elements, four a lane, so a block's scale is a maximum over one wavefront.  A
 // workgroup's tile of blocks lies in one tensor, which it looks up in the arguments.  In 8 bits an element costs 91 vector
 // instructions, ten of them the step's division: codes are cut from the float's bits, and what only infinities and NaN
-// need is done where a block has them.  Measured: 24 x 8388608 elements with bf16 gradients in 8 bits 562 us (5.8 TB/s; at 2.4 GHz the
-// vector pipes issue for 465 of them), in fp32 1010 (6.0 TB/s); ResNet-50's 161 tensors 91 and 135.
+// need is done where a block has them.  Measured: 24 x 8388608 elements with bf16 gradients in 8 bits 562 us (5.8 TB/s; the vector
+// pipes are busy for 94 % of them), in fp32 1010 (6.0 TB/s); ResNet-50's 161 tensors 91 and 135.
 #include "adamw.h"
 
 #include "rows.h"
