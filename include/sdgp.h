@@ -349,10 +349,12 @@ int sdgp_conv_bwd_weight(const void* D, const void* dO, float* dW, int64_t B, in
  * Sums are fp32.  -inf (a token that is not allowed) and the type's lowest value are fine anywhere.  A row that leaves
  * nothing (-inf throughout) has ln p = -inf, entropy 0 and no alternatives; its gradient is 0 (that of a token >= V NaN
  * here too).  A row with a NaN or +inf has NaN in every number and -1 in every index, but for the log probability 0 of a
- * row without a token and the largest logit in its stats.  Probabilities below 2^-126 count as 0.
+ * row without a token and the largest logit in its stats.  Probabilities below 2^-126 count as 0 in the entropy and the
+ * gradients (not in ln p).
  *
  * sdgp_token_logprobs_bwd -- dL/dlogits from dL/dlogp and dL/dentropy (either may be NULL; the alternatives have none):
- *   dlogits[j] = scale * (g (j == token) - g p_j - h p_j (ln p_j + entropy)), row stride ld_out; dlogits may be logits.
+ *   dlogits[j] = scale * (g (j == token) - g p_j - h p_j (ln p_j + entropy)), row stride ld_out; dlogits may be logits,
+ *   with its stride, and overlaps them nowhere else.
  *   stats, entropy: what the forward call left.  This is the dL/dO that the last linear layer's
  *   sdgp_linear_bwd_data takes.
  *
