@@ -152,10 +152,16 @@ class AdamW:
 
     def _check_places(self) -> None:
         """All that a step writes lies apart and within its storage.  (Two workgroups would step an element at once.)"""
-        tensors = [t for ts in (self.params, self.copies or (), *self._state.values()) for t in ts if t.numel()]
-        if any(t.untyped_storage().nbytes() < (t.storage_offset() + t.numel()) * t.element_size() for t in tensors):
-            raise ValueError("the storage of a param, copy or state is not there")
-        spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in tensors)
+        spans = []
+        for t in (t for ts in (self.params, self.copies or (), *self._state.values()) for t in ts):
+            size = t.nbytes
+            if size == 0:
+                continue
+            storage, begin = t.untyped_storage(), t.data_ptr()
+            if begin + size > storage.data_ptr() + storage.nbytes():
+                raise ValueError("the storage of a param, copy or state is not there")
+            spans.append((begin, begin + size))
+        spans.sort()
         if any(end > begin for (_, end), (begin, _) in zip(spans, spans[1:])):
             raise ValueError("a tensor is twice among params, copies and states, or two of them share memory")
 
