@@ -13,7 +13,7 @@
 // Bound by memory where rows are many: 2 bytes an element read forward, 4 read and written backward in bf16, with 8 vector
 // instructions beside them forward, 10 backward and 12 with the entropy's gradient, one an exponential.  A row is one workgroup's (or, where rows are short and many, one
 // wavefront's); few long rows are cut into pieces, whose sums and lists a second kernel joins.  Measured: 8192 x 65536 bf16
-// forward 169 us (6.4 TB/s), gradient 353 (6.1 TB/s); 4 x 131072 with eight alternatives 9 + 5 us, which are latencies.
+// forward 169 us (6.4 TB/s), gradient 355 to 361 (6.0 TB/s); 4 x 131072 with eight alternatives 9 + 5 us, which are latencies.
 #include "rows.h"
 
 namespace sdgp {
@@ -500,9 +500,8 @@ __global__ void __launch_bounds__(kBlock) logprob_grad(const LogprobsGrad q) {
         const float l2 = mul_rn(empty ? 0.0f : logs, kLog2e), off = empty ? 0.0f : fmaf(logs, kLog2e, -l2), back = exp2_hw(-off);
         if (empty) g = token >= q.V ? NAN : 0.0f, h = 0.0f;
         const float B = -h * kLn2 * back, A = -(g + h * (H - kLn2 * off)) * back;
-        const int64_t at = token - first;   // the token's place in this chunk
-        float y = 0.0f;                     // its logit, less the largest
-        bool here = false;
+        // the token's place in this chunk; one outside the vocabulary has none
+        const int at = token >= first && token < q.V && token - first < T * VECS * N ? (int)(token - first) : -1;
 #pragma unroll
         for (int v = 0; v < VECS; ++v) {
             const int e = (v * T + t) * N;
@@ -512,23 +511,23 @@ __global__ void __launch_bounds__(kBlock) logprob_grad(const LogprobsGrad q) {
                 const float l = fmaf(x[v].get(i) - m, c, -l2), p = exp2_hw(l);
                 d[i] = ENTROPY ? p * fmaf(B, fmaxf(l, kFloor2), A) : p * A;
             }
-            if (at >= e && at < e + N && at < left && token >= 0) {   // one outside the vocabulary is no element
+            if (at >= e && at < e + N) {
+                // g (1 - p) from ln p: 1 - p of a token that is almost certain would be what p's rounding left of it (16384 x 100
+                // fp32 8.4 us as that difference, 9.1 so; 8192 x 65536 bf16 357 and 361)
+                float y = 0.0f;
 #pragma unroll
                 for (int i = 0; i < N; ++i) y = e + i == at ? x[v].get(i) - m : y;
-                here = true;
+                float own = g * one_less_exp(y * q.scale - (empty ? 0.0f : logs));
+                if constexpr (ENTROPY) {
+                    const float l = fmaf(y, c, -l2);
+                    own += exp2_hw(l) * fmaf(B, fmaxf(l, kFloor2), -(h * (H - kLn2 * off)) * back);
+                }
+#pragma unroll
+                for (int i = 0; i < N; ++i) d[i] = e + i == at ? own : d[i];
             }
             V o;
             o.set(d);
             store_row<DT, BOTH>(out, e, left, o);
-        }
-        if (here) {
-            // The token's own element over the p (A + B log2 p) just written there: g (1 - p) from ln p, since 1 - p of a token that
-            // is almost certain would be what p's rounding left of it.  (16384 x 100 fp32 8.4 us as that difference, 9.3; rows of 1000
-            // and more 1 or 2 % more.)
-            const float l = fmaf(y, c, -l2), other = exp2_hw(l) * fmaf(B, fmaxf(l, kFloor2), -(h * (H - kLn2 * off)) * back);
-            const float d = g * one_less_exp(y * q.scale - (empty ? 0.0f : logs)) + (ENTROPY ? other : 0.0f);
-            if constexpr (DT == SDGP_BF16) reinterpret_cast<uint16_t*>(out)[at] = (uint16_t)float_to_bf16(d);
-            else reinterpret_cast<float*>(out)[at] = d;
         }
     }
 }
