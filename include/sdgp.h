@@ -430,6 +430,45 @@ int sdgp_adamw_step(int count, void* const* params, const void* const* grads, vo
                     uint64_t seed, void* hip_stream);
 
 /*
+ * sdgp_attention -- softmax attention of packed sequences with grouped heads.
+ *
+ *   s = scale * q . k over the keys that a query sees;  o = softmax(s) v;  lse = ln sum exp s
+ *
+ *   q         Tq tokens of H heads, k and v Tk tokens of Hk heads, H a multiple of Hk: query head h reads key head h / (H / Hk).
+ *             `dt`, heads of D <= 128 values with stride 1
+ *   strides   HOST array of six (read before the call returns): elements between tokens and between heads of q, of k and of v
+ *   offsets_q, offsets_k  [sequences + 1] int32: sequence i is tokens offsets[i] .. offsets[i + 1] - 1; ascending, within 0 .. T.
+ *             Both or neither: without them every sequence has Tq / sequences and Tk / sequences tokens.  Tokens that no sequence
+ *             holds see and are seen by nothing.  Offsets that are wrong give wrong results, and nothing outside the tensors is touched.
+ *   lengths_k [sequences] int32, only without offsets, or NULL: how many of its Tk / sequences tokens a sequence has (a cache)
+ *   causal    non-zero: of a sequence with nq queries and nk keys, query t sees keys 0 .. t + nk - nq (the last query the last
+ *             key); else all of its sequence's
+ *   scale     1e-30 .. 1e30
+ *   o         [Tq, H, D] of `dt`;  lse [Tq, H] fp32.  A query that sees no key has o = 0 and lse = -inf.
+ *
+ * Products of bf16 tensors are taken in bf16 with fp32 sums (probabilities rounded to bf16), those of fp32 tensors in fp32;
+ * softmax statistics are fp32.  A NaN or infinity in k or v may reach all queries of its sequence and head group, also those that do
+ * not see its token; one in q stays with its query.
+ *
+ * sdgp_attention_bwd -- dq [Tq, H, D], dk and dv [Tk, Hk, D] of `dt` from dO [Tq, H, D], the inputs and what the forward call
+ *   left.  Everything that is contiguous above is so here; gradients of a key head are the sums over its query heads, in a fixed
+ *   order: the same bits from call to call.  Tokens without a sequence, and keys that no query sees, have gradient 0.
+ *
+ * workspace: sdgp_attention_workspace(...) / sdgp_attention_bwd_workspace(...) bytes, 16-byte aligned, contents undefined
+ * afterwards ((size_t)-1 for invalid arguments; 0 where the call needs none).  Tq * H and Tk * H at most 2^30.
+ */
+size_t sdgp_attention_workspace(int64_t sequences, int64_t Tq, int64_t Tk, int64_t H, int64_t Hk, int D, int dt);
+int sdgp_attention(const void* q, const void* k, const void* v, const int64_t* strides, const int32_t* offsets_q,
+                   const int32_t* offsets_k, const int32_t* lengths_k, int64_t sequences, void* o, float* lse, int64_t Tq,
+                   int64_t Tk, int64_t H, int64_t Hk, int D, int dt, int causal, float scale, void* workspace,
+                   size_t workspace_bytes, void* hip_stream);
+size_t sdgp_attention_bwd_workspace(int64_t Tq, int64_t H);
+int sdgp_attention_bwd(const void* dO, const void* q, const void* k, const void* v, const void* o, const float* lse,
+                       const int64_t* strides, const int32_t* offsets_q, const int32_t* offsets_k, int64_t sequences, void* dq,
+                       void* dk, void* dv, int64_t Tq, int64_t Tk, int64_t H, int64_t Hk, int D, int dt, int causal, float scale,
+                       void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
  * Measurement aid: what the GPU sustains on the two resources the path is bound by (the benchmark reports its
  * roofline fractions against the published peaks and, beside them, against these).  One launch on `hip_stream`; the
  * caller times it.

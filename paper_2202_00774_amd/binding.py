@@ -30,6 +30,7 @@ EXPORTS = ("sdgp_prune", "sdgp_linear_bwd_data", "sdgp_conv_bwd_data", "sdgp_con
            "sdgp_conv_fwd_workspace", "sdgp_conv_fwd", "sdgp_conv_bwd_weight_workspace", "sdgp_conv_bwd_weight",
            "sdgp_token_logprobs_workspace", "sdgp_token_logprobs", "sdgp_token_logprobs_bwd",
            "sdgp_block_norm", "sdgp_block_norm_bwd_workspace", "sdgp_block_norm_bwd", "sdgp_adamw_step",
+           "sdgp_attention_workspace", "sdgp_attention", "sdgp_attention_bwd_workspace", "sdgp_attention_bwd",
            "sdgp_peak_probe", "sdgp_status_string", "sdgp_version")
 
 
@@ -114,6 +115,14 @@ def load():
             lib.sdgp_block_norm_bwd.argtypes = [vp] * 13 + [i64, i64, i64, i32, i32, f32, vp, sz, vp]
             lib.sdgp_adamw_step.restype = i32
             lib.sdgp_adamw_step.argtypes = [i32] + [vp] * 8 + [i32, i32, i32, f64, f64, f64, f64, f64, i64, vp, u64, vp]
+            lib.sdgp_attention_workspace.restype = sz
+            lib.sdgp_attention_workspace.argtypes = [i64, i64, i64, i64, i64, i32, i32]
+            lib.sdgp_attention.restype = i32
+            lib.sdgp_attention.argtypes = [vp] * 7 + [i64, vp, vp, i64, i64, i64, i64, i32, i32, i32, f32, vp, sz, vp]
+            lib.sdgp_attention_bwd_workspace.restype = sz
+            lib.sdgp_attention_bwd_workspace.argtypes = [i64, i64]
+            lib.sdgp_attention_bwd.restype = i32
+            lib.sdgp_attention_bwd.argtypes = [vp] * 9 + [i64, vp, vp, vp, i64, i64, i64, i64, i32, i32, i32, f32, vp, sz, vp]
             lib.sdgp_peak_probe.restype = i32
             lib.sdgp_peak_probe.argtypes = [i32, vp, vp, sz, i32, ctypes.POINTER(ctypes.c_double), vp]
             lib.sdgp_status_string.restype = ctypes.c_char_p
@@ -693,3 +702,118 @@ def sdgp_block_norm_bwd(dy: torch.Tensor | None, dh: torch.Tensor | None, y: tor
     if rc != 0:
         raise SdgpError(rc, "sdgp_block_norm_bwd")
     return dx, du, dgate, dw_post, dw_pre
+
+
+# ---------------------------------------------- packed sequences: attention, positions, losses of the log probabilities
+
+_current_gpu = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _launch(name: str, x: torch.Tensor, *args) -> None:
+    """Calls the library on the GPU of ``x``, whichever the current one is."""
+    call = getattr(load(), name)
+    if x.get_device() == _current_gpu():
+        rc = call(*args, _stream(x))
+    else:
+        with torch.cuda.device(x.get_device()):
+            rc = call(*args, _stream(x))
+    if rc != 0:
+        raise SdgpError(rc, name)
+
+
+def _heads(t: torch.Tensor, name: str, packed: bool, x: torch.Tensor | None = None):
+    """(distance of two tokens, of two heads) of ``t``, [T, heads, D] packed or [B, L, heads, D]."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must live on the GPU")
+    if x is not None and (t.get_device() != x.get_device() or t.dtype != x.dtype):
+        raise ValueError(f"{name} must have the dtype and the GPU of the other tensors")
+    if t.dim() != (3 if packed else 4):
+        raise ValueError(f"{name} must be {'[T, heads, D] with offsets' if packed else '[B, L, heads, D] without offsets'}")
+    stride, shape = t.stride(), t.shape
+    if shape[-1] > 1 and stride[-1] != 1:
+        raise ValueError(f"the values of a head of {name} must have stride 1")
+    if packed:
+        return stride[0], stride[1]
+    if shape[0] > 1 and shape[1] > 1 and stride[0] != shape[1] * stride[1]:
+        raise ValueError(f"the tokens of {name} must be evenly spaced")
+    return (stride[1] if shape[1] > 1 else stride[0]), stride[2]
+
+
+def _offsets(offsets, name: str, x: torch.Tensor) -> torch.Tensor:
+    _beside(offsets, name, x)
+    if offsets.dtype != torch.int32 or offsets.dim() != 1 or offsets.numel() < 1:
+        raise ValueError(f"{name} must be int32 [sequences + 1]")
+    return offsets
+
+
+def _attention_sizes(q, k, v, offsets, offsets_k, scale):
+    """Checked arguments: (strides, offsets, offsets_k, sequences, Tq, Tk, H, Hk, D, dtype, scale)."""
+    packed = offsets is not None
+    strides = (*_heads(q, "q", packed), *_heads(k, "k", packed, q), *_heads(v, "v", packed, q))
+    if v.shape != k.shape or k.shape[-1] != q.shape[-1] or (not packed and k.shape[0] != q.shape[0]):
+        raise ValueError("k and v must have one shape, with q's head size and batch")
+    H, D = q.shape[-2:]
+    Hk = k.shape[-2]
+    if Hk == 0 or H % Hk or H == 0:
+        raise ValueError("the heads of q must be a multiple of those of k and v")
+    if packed:
+        _offsets(offsets, "offsets", q)
+        if offsets_k is None:
+            offsets_k = offsets
+            if k.shape[0] != q.shape[0]:
+                raise ValueError("k has other tokens than q: offsets_k is needed")
+        elif _offsets(offsets_k, "offsets_k", q).numel() != offsets.numel():
+            raise ValueError("offsets and offsets_k must be of one length")
+        sequences, Tq, Tk = offsets.numel() - 1, q.shape[0], k.shape[0]
+    else:
+        if offsets_k is not None:
+            raise ValueError("offsets_k belongs to offsets")
+        sequences, Tq, Tk = q.shape[0], q.shape[0] * q.shape[1], k.shape[0] * k.shape[1]
+    if scale is None:
+        scale = D ** -0.5
+    return (ctypes.c_int64 * 6)(*strides), offsets, offsets_k, sequences, Tq, Tk, H, Hk, D, _dtype_code(q), scale
+
+
+def sdgp_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets: torch.Tensor | None = None,
+                   offsets_k: torch.Tensor | None = None, *, lengths: torch.Tensor | None = None, causal: bool = True,
+                   scale: float | None = None, workspace: torch.Tensor | None = None):
+    """``(o, lse)``: softmax attention, query head h of ``q`` on key head h // (H / Hk) of ``k`` and ``v``.
+
+    With ``offsets`` (int32 [sequences + 1]) q is [T, H, D], k and v [T, Hk, D], sequences one behind the other; ``offsets_k``
+    where the keys' differ.  Without, q is [B, L, H, D], k and v [B, Lk, Hk, D], and ``lengths`` (int32 [B]) says how many
+    of the Lk keys there are (a cache).  Tokens and heads may be strided.  ``causal``: the last query sees all keys, the one
+    before all but the last, and so on.  ``scale``: D ** -0.5 by default."""
+    strides, offsets, offsets_k, S, Tq, Tk, H, Hk, D, dt, scale = _attention_sizes(q, k, v, offsets, offsets_k, scale)
+    if lengths is not None:
+        if offsets is not None:
+            raise ValueError("lengths are for keys without offsets")
+        _per_row(lengths, (S,), "lengths", (torch.int32,), q)
+    need = _need("sdgp_attention_workspace", S, Tq, Tk, H, Hk, D, dt)
+    if need == _INVALID:
+        raise SdgpError(-3, "sdgp_attention")
+    wbytes = 0
+    if need:
+        workspace, wbytes = _own_workspace(need, workspace, q, "sdgp_attention_workspace")
+    o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    lse = torch.empty(q.shape[:-1], dtype=torch.float32, device=q.device)
+    _launch("sdgp_attention", q, _ptr(q), _ptr(k), _ptr(v), strides, _ptr(offsets), _ptr(offsets_k), _ptr(lengths), S, _ptr(o), _ptr(lse),
+            Tq, Tk, H, Hk, D, dt, int(causal), scale, _ptr(workspace) if need else None, wbytes)
+    return o, lse
+
+
+def sdgp_attention_bwd(do: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, lse: torch.Tensor,
+                       offsets: torch.Tensor | None = None, offsets_k: torch.Tensor | None = None, *, causal: bool = True,
+                       scale: float | None = None, workspace: torch.Tensor | None = None):
+    """``(dq, dk, dv)`` from the gradient of ``o`` and what ``sdgp_attention`` took and returned."""
+    strides, offsets, offsets_k, S, Tq, Tk, H, Hk, D, dt, scale = _attention_sizes(q, k, v, offsets, offsets_k, scale)
+    for t, name in ((do, "do"), (o, "o")):
+        _per_row(t, q.shape, name, (q.dtype,), q)
+    _per_row(lse, q.shape[:-1], "lse", _FLOAT, q)
+    need = _need("sdgp_attention_bwd_workspace", Tq, H)
+    if need == _INVALID:
+        raise SdgpError(-3, "sdgp_attention_bwd")
+    workspace, wbytes = _own_workspace(need, workspace, q, "sdgp_attention_bwd_workspace")
+    dq, dk, dv = (torch.empty(t.shape, dtype=q.dtype, device=q.device) for t in (q, k, v))
+    _launch("sdgp_attention_bwd", q, _ptr(do), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), strides, _ptr(offsets), _ptr(offsets_k), S,
+            _ptr(dq), _ptr(dk), _ptr(dv), Tq, Tk, H, Hk, D, dt, int(causal), scale, _ptr(workspace), wbytes)
+    return dq, dk, dv

@@ -1,0 +1,309 @@
+// Attention over packed sequences: arguments, where a workgroup's tile lies, and tiles in LDS as the matrix instructions
+// take them.  The kernels' mathematics stands in attention_fwd.h and attention_bwd.h.
+#pragma once
+
+#include <type_traits>
+
+#include "common.h"
+#include "fastdiv.h"
+
+namespace sdgp {
+
+#define SDGP_SHARED __attribute__((address_space(3)))
+
+struct Attention {
+    const void *q, *k, *v;
+    int64_t q_token, q_head, k_token, k_head, v_token, v_head;   // strides in elements
+    const int32_t *off_q, *off_k, *len_k;                        // null: S sequences of Lq and Lk tokens each
+    int S, Lq, Lk, Tq, Tk, H, Hk, G, D, causal;
+    FastDiv by_group;                                            // rows / G
+    float scale, c;                                              // c = scale log2 e
+    void* o;
+    float* lse;
+    int parts;                                                   // forward: pieces of a row's keys
+    float *part_o, *part_ml;                                     // [parts, Tq H, D], [parts, Tq H, 2]
+    const void *d_o, *o_in;
+    float* delta;
+    void *dq, *dk, *dv;
+};
+
+// A key head's queries are the rows (token, head of the group), token by token: its keys are read once for all heads of
+// the group, and their gradients are sums over these rows.
+struct Sequence {
+    int q0, nq, k0, nk;
+};
+
+__device__ __forceinline__ int clamp_int(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
+
+// The tokens of sequence i; offsets that are wrong stay within the tensors.
+__device__ __forceinline__ Sequence sequence_at(const Attention& a, int i) {
+    Sequence s;
+    if (a.off_q) {
+        s.q0 = clamp_int(a.off_q[i], 0, a.Tq);
+        s.nq = clamp_int(a.off_q[i + 1], s.q0, a.Tq) - s.q0;
+        s.k0 = clamp_int(a.off_k[i], 0, a.Tk);
+        s.nk = clamp_int(a.off_k[i + 1], s.k0, a.Tk) - s.k0;
+    } else {
+        s.q0 = i * a.Lq, s.nq = a.Lq;
+        s.k0 = i * a.Lk, s.nk = a.len_k ? clamp_int(a.len_k[i], 0, a.Lk) : a.Lk;
+    }
+    return s;
+}
+
+// Rows that no sequence holds: in front of the first one (i == -1) and behind the last (i == S).  They see nothing.
+template <bool KEYS>
+__device__ __forceinline__ Sequence rows_outside(const Attention& a, bool behind) {
+    const int T = KEYS ? a.Tk : a.Tq;
+    const int32_t* off = KEYS ? a.off_k : a.off_q;
+    const int at = clamp_int(off[behind ? a.S : 0], 0, T);
+    Sequence s = {0, 0, 0, 0};
+    if (KEYS) s.k0 = behind ? at : 0, s.nk = behind ? T - at : at;
+    else s.q0 = behind ? at : 0, s.nq = behind ? T - at : at;
+    return s;
+}
+
+// Tile `index` of all sequences' tiles of UNIT rows (KEYS: of keys; else of queries, G a token): false behind the last.  With
+// offsets, a wavefront adds up the sequences' tiles 64 at a time (every wavefront for itself; the results are uniform).
+template <bool KEYS, int UNIT>
+__device__ __forceinline__ bool find_tile(const Attention& a, int index, Sequence& s, int& tile, int& tiles) {
+    if (a.off_q == nullptr) {
+        tiles = ((KEYS ? a.Lk : a.Lq * a.G) + UNIT - 1) / UNIT;
+        const int i = index / tiles;
+        if (i >= a.S) return false;
+        s = sequence_at(a, i);
+        if (KEYS) s.nk = a.Lk;                                   // (lengths: forward only)
+        tile = index - i * tiles;
+        return true;
+    }
+    const int lane = threadIdx.x & 63;
+    int before = 0;
+    for (int first = -1; first <= a.S; first += 64) {
+        const int i = first + lane;
+        Sequence mine = {0, 0, 0, 0};
+        if (i <= a.S) mine = i >= 0 && i < a.S ? sequence_at(a, i) : rows_outside<KEYS>(a, i >= 0);
+        const int n = ((KEYS ? mine.nk : mine.nq * a.G) + UNIT - 1) / UNIT;
+        int upto = n;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int x = __shfl_up(upto, o);
+            if (lane >= o) upto += x;
+        }
+        const uint64_t past = __ballot(before + upto > index);
+        if (past != 0) {
+            const int at = __builtin_ctzll(past);
+            s.q0 = __builtin_amdgcn_readlane(mine.q0, at), s.nq = __builtin_amdgcn_readlane(mine.nq, at);
+            s.k0 = __builtin_amdgcn_readlane(mine.k0, at), s.nk = __builtin_amdgcn_readlane(mine.nk, at);
+            tiles = __builtin_amdgcn_readlane(n, at);
+            tile = index - before - (__builtin_amdgcn_readlane(upto, at) - tiles);
+            return true;
+        }
+        before += __builtin_amdgcn_readlane(upto, 63);
+    }
+    return false;
+}
+
+// Upper bound of what find_tile finds.
+inline int64_t most_tiles(bool packed, int64_t S, int64_t T, int64_t L, int64_t each, int64_t unit) {
+    return packed ? T * each / unit + S + 2 : S * ((L * each + unit - 1) / unit);
+}
+
+// ------------------------------------------------------------------------------------------- operands and tiles
+
+typedef __bf16 attn_bf16x8 __attribute__((ext_vector_type(8)));
+typedef short attn_s16x4 __attribute__((ext_vector_type(4)));
+typedef short attn_s16x8 __attribute__((ext_vector_type(8)));
+typedef float attn_f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t attn_u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t attn_u32x4_half __attribute__((ext_vector_type(4), aligned(2), may_alias));
+
+// Eight values of the summed axis for a lane's row: lanes 0 .. 31 hold rows 0 .. 31 and the first eight of sixteen steps,
+// lanes 32 .. 63 the same rows and the other eight.  fp32 values are multiplied one a half at a time (32x32x2); which eight
+// belong together is the same for both operands, so their order is free.
+template <int DT>
+struct Operand;
+
+template <>
+struct Operand<SDGP_BF16> {
+    static constexpr int kSize = 2;
+    attn_u32x4 w;
+    __device__ __forceinline__ void set(const float (&x)[8]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = float2_to_bf16x2(x[2 * i], x[2 * i + 1]);
+    }
+    __device__ __forceinline__ float get(int i) const { return bits_to_float((i & 1) ? (w[i / 2] & 0xFFFF0000u) : (w[i / 2] << 16)); }
+};
+
+template <>
+struct Operand<SDGP_F32> {
+    static constexpr int kSize = 4;
+    float x[8];
+    __device__ __forceinline__ void set(const float (&y)[8]) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = y[i];
+    }
+    __device__ __forceinline__ float get(int i) const { return x[i]; }
+};
+
+__device__ __forceinline__ attn_f32x16 multiply(const Operand<SDGP_BF16>& a, const Operand<SDGP_BF16>& b, attn_f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(attn_bf16x8, a.w), __builtin_bit_cast(attn_bf16x8, b.w), c, 0, 0, 0);
+}
+__device__ __forceinline__ attn_f32x16 multiply(const Operand<SDGP_F32>& a, const Operand<SDGP_F32>& b, attn_f32x16 c) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x[i], b.x[i], c, 0, 0, 0);
+    return c;
+}
+
+// Row of element i (of 16) of a 32x32 result; the column is lane % 32.
+__device__ __forceinline__ int result_row(int i, int half) { return 8 * (i / 4) + 4 * half + i % 4; }
+
+// Sixteen bytes of a row of n elements from element e on; what lies outside is 0 and is not read.  Rows begin anywhere.
+template <int DT>
+__device__ __forceinline__ attn_u32x4 load_chunk(const char* row, int e, int n) {
+    constexpr int N = 16 / Operand<DT>::kSize;
+    if (e + N <= n) return *reinterpret_cast<const attn_u32x4_half*>(row + e * Operand<DT>::kSize);
+    union {
+        attn_u32x4 q;
+        uint16_t h[8];
+        uint32_t w[4];
+    } u;
+    u.q = attn_u32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < N - 1; ++i) {
+        if (e + i >= n) break;
+        if constexpr (DT == SDGP_BF16) u.h[i] = reinterpret_cast<const uint16_t*>(row)[e + i];
+        else u.w[i] = reinterpret_cast<const uint32_t*>(row)[e + i];
+    }
+    return u.q;
+}
+
+// Eight values from element e on, as an operand.
+template <int DT>
+__device__ __forceinline__ Operand<DT> load_operand(const char* row, int e, int n) {
+    Operand<DT> f;
+    if constexpr (DT == SDGP_BF16) {
+        f.w = load_chunk<DT>(row, e, n);
+    } else {
+        const attn_u32x4 a = load_chunk<DT>(row, e, n), b = load_chunk<DT>(row, e + 4, n);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f.x[i] = bits_to_float(a[i]), f.x[4 + i] = bits_to_float(b[i]);
+    }
+    return f;
+}
+
+// A tile of rows of up to DC values in LDS.  Its sixteen-byte chunks change places within a row (XOR with a number of the
+// row) so that both ways of reading it meet all banks: `rows`, sixteen lanes at one chunk of sixteen rows; `columns`, four
+// rows of four neighbouring chunks.
+template <int DT, int DC>
+struct Tile {
+    static constexpr int kRow = (DC <= 64 ? 64 : 128) * Operand<DT>::kSize;   // bytes
+    static constexpr int kChunks = kRow / 16;
+
+    static __device__ __forceinline__ int place(int row) {
+        return kChunks == 8 ? ((row & 2) << 1 | ((row >> 2) & 3)) : ((row & 3) << 2 | ((row >> 2) & 3));
+    }
+    static __device__ __forceinline__ int at(int row, int chunk) { return row * kRow + ((chunk ^ place(row)) << 4); }
+
+    // Rows r0 + lane % 32, values 16 step + 8 (lane / 32) ..: an operand summed over the values.  r0 % 32 == 0.
+    static __device__ __forceinline__ Operand<DT> rows(SDGP_SHARED char* tile, int r0, int step, int lane) {
+        const int row = lane & 31, half = lane >> 5;
+        Operand<DT> f;
+        if constexpr (DT == SDGP_BF16) {
+            f.w = *(SDGP_SHARED attn_u32x4*)(tile + r0 * kRow + at(row, 2 * step + half));
+        } else {
+            const attn_u32x4 a = *(SDGP_SHARED attn_u32x4*)(tile + r0 * kRow + at(row, 4 * step + 2 * half));
+            const attn_u32x4 b = *(SDGP_SHARED attn_u32x4*)(tile + r0 * kRow + at(row, 4 * step + 2 * half + 1));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f.x[i] = bits_to_float(a[i]), f.x[4 + i] = bits_to_float(b[i]);
+        }
+        return f;
+    }
+
+    // Column 32 block + lane % 32 of rows r0 + result_row(0 .. 7, lane / 32): an operand summed over the rows, its eight in the
+    // order in which a lane holds half a result's rows, so that results are the other operand as they are.  r0 % 16 == 0.
+    static __device__ __forceinline__ Operand<DT> columns(SDGP_SHARED char* tile, int r0, int block, int lane) {
+        const int half = lane >> 5;
+        Operand<DT> f;
+        if constexpr (DT == SDGP_BF16) {
+            // the transposing read: of sixteen lanes, each four on one row, lane i receives column i of the four rows
+            const int row = 4 * half + ((lane & 15) >> 2), chunk = 4 * block + ((lane >> 3) & 2) + ((lane & 3) >> 1);
+            attn_s16x4 x[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+                x[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (SDGP_SHARED attn_s16x4*)(tile + r0 * kRow + at(row + 8 * u, chunk) + (lane & 1) * 8));
+            const attn_s16x8 all = {x[0][0], x[0][1], x[0][2], x[0][3], x[1][0], x[1][1], x[1][2], x[1][3]};
+            f.w = __builtin_bit_cast(attn_u32x4, all);
+        } else {
+            const int col = lane & 31;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int row = result_row(i, half);
+                f.x[i] = *(SDGP_SHARED float*)(tile + r0 * kRow + at(row, 8 * block + (col >> 2)) + (col & 3) * 4);
+            }
+        }
+        return f;
+    }
+};
+
+// Copies rows of a tensor into a tile by way of registers, so that a tile's loads fly while the one before it is worked on.
+// THREADS threads; ROWS rows of DC values.
+template <int DT, int DC, int ROWS, int THREADS>
+struct Stage {
+    using T = Tile<DT, DC>;
+    static constexpr int kNeed = DC * Operand<DT>::kSize / 16;          // chunks of a row that anyone reads
+    static constexpr int kEach = (ROWS * T::kChunks + THREADS - 1) / THREADS;
+    attn_u32x4 held[kEach];
+
+    // row(i): the address of row i, or null for a row of zeros
+    template <class Row>
+    __device__ __forceinline__ void load(Row&& row, int D) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int x = (int)threadIdx.x + i * THREADS, r = x / T::kChunks, chunk = x % T::kChunks;
+            held[i] = attn_u32x4{0, 0, 0, 0};
+            if (chunk < kNeed && r < ROWS) {
+                const char* p = row(r);
+                if (p != nullptr) held[i] = load_chunk<DT>(p, chunk * (16 / Operand<DT>::kSize), D);
+            }
+        }
+    }
+    __device__ __forceinline__ void store(SDGP_SHARED char* tile) const {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int x = (int)threadIdx.x + i * THREADS, r = x / T::kChunks, chunk = x % T::kChunks;
+            if (chunk < kNeed && r < ROWS) *(SDGP_SHARED attn_u32x4*)(tile + T::at(r, chunk)) = held[i];
+        }
+    }
+};
+
+// The larger and the sum of a lane's value and that of the lane 32 away.
+__device__ __forceinline__ float halves_max(float x) { return fmaxf(x, __shfl_xor(x, 32)); }
+__device__ __forceinline__ float halves_sum(float x) { return x + __shfl_xor(x, 32); }
+
+// Stores a 32-column block of results, transposed: lane % 32 is a row of memory, the result's rows its values.
+template <int DT>
+__device__ __forceinline__ void store_block(char* row, const attn_f32x16& x, int block, int half, int D, float factor) {
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        const int e = 32 * block + 8 * g + 4 * half;
+        const float y[4] = {x[4 * g] * factor, x[4 * g + 1] * factor, x[4 * g + 2] * factor, x[4 * g + 3] * factor};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (DT == SDGP_BF16) {
+                if (i & 1) continue;
+                const uint32_t w = float2_to_bf16x2(y[i], y[i + 1]);
+                uint16_t* p = reinterpret_cast<uint16_t*>(row) + e + i;
+                if (e + i + 1 < D) {
+                    typedef uint32_t word_half __attribute__((aligned(2), may_alias));
+                    *reinterpret_cast<word_half*>(p) = w;
+                } else if (e + i < D) {
+                    *p = (uint16_t)w;
+                }
+            } else if (e + i < D) {
+                reinterpret_cast<float*>(row)[e + i] = y[i];
+            }
+        }
+    }
+}
+
+}  // namespace sdgp

@@ -1,0 +1,82 @@
+// Which attention kernels a call takes, and the room its pieces need.
+//
+// The forward pass gives 128 rows (query tokens times heads of a group) to a workgroup, or 32 rows to four wavefronts that split
+// the keys, where sequences have few rows (single tokens).  Where that leaves the chip short of workgroups the keys are cut into up
+// to 64 parts, whose sums a second kernel joins.
+#include <math.h>
+
+#include "attention.h"
+#include "attention_api.h"
+
+namespace sdgp {
+
+template <int DT>
+int attention_fwd_launch(const Attention& a, int64_t tiles, bool few, hipStream_t stream);
+template <int DT>
+int attention_bwd_launch(const Attention& a, int64_t row_tiles, int64_t key_tiles, hipStream_t stream);
+
+namespace {
+
+struct Split {
+    bool few;
+    int parts;
+};
+
+// By the sequences' mean lengths: of packed ones the host knows no more.
+Split choose(int64_t S, int64_t Tq, int64_t Tk, int64_t H, int64_t Hk) {
+    const int64_t n = S > 0 ? S : 1, rows = (Tq + n - 1) / n * (H / Hk), keys = (Tk + n - 1) / n;
+    Split s;
+    s.few = rows <= 32;
+    const int64_t unit = s.few ? 32 : 128, groups = n * ((rows + unit - 1) / unit) * Hk;
+    int64_t parts = groups > 0 ? (s.few ? 1024 : 512) / groups : 1;
+    const int64_t most = keys / 128;
+    parts = parts > most ? most : parts;
+    s.parts = (int)(parts < 1 ? 1 : parts > 64 ? 64 : parts);
+    return s;
+}
+
+Attention arguments(const AttentionCall& c) {
+    Attention a = {};
+    a.q = c.q, a.k = c.k, a.v = c.v;
+    a.q_token = c.strides[0], a.q_head = c.strides[1], a.k_token = c.strides[2], a.k_head = c.strides[3], a.v_token = c.strides[4], a.v_head = c.strides[5];
+    a.off_q = c.offsets_q, a.off_k = c.offsets_k, a.len_k = c.lengths_k;
+    a.S = (int)c.S, a.Tq = (int)c.Tq, a.Tk = (int)c.Tk, a.H = (int)c.H, a.Hk = (int)c.Hk, a.G = (int)(c.H / c.Hk), a.D = c.D, a.causal = c.causal;
+    a.Lq = c.S > 0 ? (int)(c.Tq / c.S) : 0, a.Lk = c.S > 0 ? (int)(c.Tk / c.S) : 0;
+    a.by_group = fast_div((uint32_t)a.G);
+    a.scale = c.scale, a.c = c.scale * 1.44269504088896341f;
+    a.parts = 1;
+    return a;
+}
+
+}  // namespace
+
+size_t attention_workspace(int64_t S, int64_t Tq, int64_t Tk, int64_t H, int64_t Hk, int D) {
+    const Split s = choose(S, Tq, Tk, H, Hk);
+    return s.parts == 1 ? 0 : (size_t)s.parts * (size_t)(Tq * H) * (size_t)(D + 2) * sizeof(float);
+}
+
+int attention_launch(const AttentionCall& c, void* o, float* lse, void* workspace, hipStream_t stream) {
+    Attention a = arguments(c);
+    const Split s = choose(c.S, c.Tq, c.Tk, c.H, c.Hk);
+    a.o = o, a.lse = lse, a.parts = s.parts;
+    a.part_o = static_cast<float*>(workspace);
+    a.part_ml = a.part_o + (s.parts == 1 ? 0 : (int64_t)s.parts * c.Tq * c.H * c.D);
+    const int64_t tiles = most_tiles(c.offsets_q != nullptr, c.S, c.Tq, a.Lq, a.G, s.few ? 32 : 128);
+    if (tiles * a.Hk * a.parts > 0x7FFFFFFF) return SDGP_ERR_SHAPE;
+    return c.dt == SDGP_BF16 ? attention_fwd_launch<SDGP_BF16>(a, tiles, s.few, stream) : attention_fwd_launch<SDGP_F32>(a, tiles, s.few, stream);
+}
+
+int attention_bwd_launch_all(const AttentionCall& c, const void* d_o, const void* o, const float* lse, void* dq, void* dk, void* dv,
+                             void* workspace, hipStream_t stream) {
+    Attention a = arguments(c);
+    a.d_o = d_o, a.o_in = o, a.lse = const_cast<float*>(lse), a.dq = dq, a.dk = dk, a.dv = dv;
+    a.delta = static_cast<float*>(workspace);
+    const bool packed = c.offsets_q != nullptr;
+    const int64_t row_tiles = c.Tq == 0 ? 0 : most_tiles(packed, c.S, c.Tq, a.Lq, a.G, 128);
+    const int64_t key_tiles = c.Tk == 0 ? 0 : most_tiles(packed, c.S, c.Tk, a.Lk, 1, 128);
+    if (row_tiles * a.Hk > 0x7FFFFFFF || key_tiles * a.Hk > 0x7FFFFFFF) return SDGP_ERR_SHAPE;
+    return c.dt == SDGP_BF16 ? attention_bwd_launch<SDGP_BF16>(a, row_tiles, key_tiles, stream)
+                             : attention_bwd_launch<SDGP_F32>(a, row_tiles, key_tiles, stream);
+}
+
+}  // namespace sdgp
