@@ -469,6 +469,67 @@ int sdgp_attention_bwd(const void* dO, const void* q, const void* k, const void*
                        void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /*
+ * sdgp_rotary -- queries and keys turned by their positions on one or several axes.
+ *
+ *   angle of pair i = positions[t, axis of i] * freqs[i];  (a, b) -> (a cos - b sin, a sin + b cos), in every head alike
+ *
+ *   q, k       T tokens of H and Hk heads of D values of `dt` (2 <= D <= 4096, last stride 1); Hk 0 with k and k_out NULL: q alone
+ *   q_out, k_out  where they go: the inputs themselves with their strides, or apart from both inputs and from each other
+ *   strides    HOST array of eight: elements between tokens and between heads of q, k, q_out, k_out (of the outputs at least D)
+ *   positions  [T, axes] int32 or int64 (position_bits), below 2^53 in magnitude
+ *   freqs      [F] fp32, radians a position, F the sum of axis_pairs, 2 F <= D; values from 2 F on stay as they are
+ *   axis_pairs HOST array of `axes` (1 .. 8) counts of at least 1: the first axis turns the first axis_pairs[0] pairs, and so on
+ *   interleaved  0: pair i is (i, F + i);  else (2 i, 2 i + 1)
+ *   inverse    non-zero: by the opposite angles, which is the gradient's way back
+ *
+ * Angles are exact but for sines and cosines, which are fp32, as is the arithmetic.  H, Hk <= 4096, (H + Hk) D <= 2^22, T < 2^31.
+ */
+int sdgp_rotary(const void* q, const void* k, void* q_out, void* k_out, const int64_t* strides, const void* positions,
+                int position_bits, const float* freqs, const int32_t* axis_pairs, int axes, int64_t T, int64_t H, int64_t Hk,
+                int64_t D, int dt, int interleaved, int inverse, void* hip_stream);
+
+/*
+ * Losses over sequences of token log probabilities (sdgp_token_logprobs' logp, or any), and their gradients.
+ *
+ *   logp, old_logp, ref_logp  [T] fp32;  mask [T] bytes, 0 for tokens that do not count, or NULL: what stands at those is not
+ *              looked at, their gradient is 0, as that of tokens without a sequence
+ *   offsets    [sequences + 1] int32, ascending, within 0 .. T (T < 2^31): sequence i is tokens offsets[i] .. offsets[i + 1] - 1;
+ *              NULL: T / sequences tokens each
+ *
+ * sdgp_policy_loss -- the clipped policy loss with a KL term.
+ *   r = exp(logp - old_logp);  l = -min(r A, clip(r, 1 - low, 1 + high) A) + kl (e^x - 1 - x),  x = ref_logp - logp
+ *   advantages A [T] with `each`, else [sequences];  0 <= low <= 1, high >= 0 (infinity: no bound), kl >= 0; ref_logp may be NULL
+ *              with kl = 0.  Whether a ratio is cut is decided on logp - old_logp in 64 bits.
+ *   by_sequence  0: the loss is the mean of l over the tokens that count; else the mean of the sequences' means, over the
+ *              sequences that have such tokens.  Without any the loss is 0.
+ *   out        [3] fp32: the loss, the mean of e^x - 1 - x and the share of tokens whose ratio is cut
+ *   weights    [sequences] fp32: of a token of each sequence in the mean, for the gradient
+ * sdgp_policy_loss_bwd -- dlogp [T] = g * weights * dl/dlogp;  g: device pointer to one fp32, dL/dloss.  (`out`[1] and [2] have none.)
+ *
+ * sdgp_preference_loss -- sequences 2 i are preferred to sequences 2 i + 1.
+ *   score = beta * the sum over a sequence's tokens that count (`average`: their mean) of logp - ref_logp (NULL: 0)
+ *   z = score(2 i) - score(2 i + 1) - margin;  loss = mean over pairs of -(1 - smoothing) ln sigma(z) - smoothing ln sigma(-z)
+ *   loss [1], margins [sequences / 2] (z), weights [sequences]: dloss/dlogp of a sequence's tokens.  0 <= smoothing < 1.
+ *   Without pairs the loss is 0; a sequence without tokens that count scores 0.
+ * sdgp_preference_loss_bwd -- dlogp [T] = g * weights.  (margins have none.)
+ *
+ * Sums are taken in 64 bits and in a fixed order: the same bits from call to call.
+ * workspace: sdgp_sequence_loss_workspace(...) bytes, 16-byte aligned, contents undefined afterwards.
+ */
+size_t sdgp_sequence_loss_workspace(int64_t T, int64_t sequences);
+int sdgp_policy_loss(const float* logp, const float* old_logp, const float* ref_logp, const float* advantages, int each,
+                     const uint8_t* mask, const int32_t* offsets, int64_t sequences, int64_t T, float low, float high, float kl,
+                     int by_sequence, float* out, float* weights, void* workspace, size_t workspace_bytes, void* hip_stream);
+int sdgp_policy_loss_bwd(const float* g, const float* weights, const float* logp, const float* old_logp, const float* ref_logp,
+                         const float* advantages, int each, const uint8_t* mask, const int32_t* offsets, int64_t sequences,
+                         int64_t T, float low, float high, float kl, float* dlogp, void* hip_stream);
+int sdgp_preference_loss(const float* logp, const float* ref_logp, const uint8_t* mask, const int32_t* offsets,
+                         int64_t sequences, int64_t T, double beta, double margin, double smoothing, int average, float* loss,
+                         float* margins, float* weights, void* workspace, size_t workspace_bytes, void* hip_stream);
+int sdgp_preference_loss_bwd(const float* g, const float* weights, const uint8_t* mask, const int32_t* offsets,
+                             int64_t sequences, int64_t T, float* dlogp, void* hip_stream);
+
+/*
  * Measurement aid: what the GPU sustains on the two resources the path is bound by (the benchmark reports its
  * roofline fractions against the published peaks and, beside them, against these).  One launch on `hip_stream`; the
  * caller times it.

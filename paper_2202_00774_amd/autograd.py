@@ -17,6 +17,13 @@ Around such layers, for a language model (nothing is pruned there; fp32 or bf16 
     y, h = sdgp_block_norm(x, u, gate, w_post, w_pre)         # norm after a block, gate, residual, norm before the next
     logp, entropy, top_logp, top_ids = sdgp_token_logprobs(logits, tokens, top=5)
     (-logp.mean()).backward()                                 # dL/dlogits is the dL/dO the last linear layer prunes
+
+Between the layers of packed sequences (offsets: int32 [sequences + 1]), and in place of a plain likelihood:
+
+    q, k = sdgp_rotary(q, k, positions, freqs)                # q [T, H, D], k [T, Hk, D]
+    o = sdgp_attention(q, k, v, offsets)
+    loss, kl, clipped = sdgp_policy_loss(logp, old_logp, advantages, ref_logp, mask, offsets, kl=0.04)
+    loss, margins = sdgp_preference_loss(logp, ref_logp, mask, offsets, beta=0.1)
 """
 from __future__ import annotations
 
@@ -152,3 +159,105 @@ def sdgp_block_norm(x: torch.Tensor, u: torch.Tensor | None = None, gate: torch.
     if u is None:
         return x, _BlockNormFn.apply(x, None, gate, w_post, w_pre, residual_scale, eps, pre)
     return _BlockNormFn.apply(x, u, gate, w_post, w_pre, residual_scale, eps, pre)
+
+
+class _AttentionFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, offsets, offsets_k, causal, scale):
+        o, lse = binding.sdgp_attention(q, k, v, offsets, offsets_k, causal=causal, scale=scale)
+        ctx.save_for_backward(q, k, v, o, lse, offsets, offsets_k)
+        ctx.cfg = (causal, scale)
+        return o
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, do):
+        q, k, v, o, lse, offsets, offsets_k = ctx.saved_tensors
+        causal, scale = ctx.cfg
+        dq, dk, dv = binding.sdgp_attention_bwd(do.contiguous(), q, k, v, o, lse, offsets, offsets_k, causal=causal, scale=scale)
+        return dq, dk, dv, None, None, None, None
+
+
+class _RotaryFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, positions, freqs, axes, interleaved):
+        ctx.save_for_backward(positions, freqs)
+        ctx.cfg = (axes, interleaved)
+        ctx.set_materialize_grads(False)
+        return binding.sdgp_rotary(q, k, positions, freqs, axes, interleaved=interleaved)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dq, dk):
+        positions, freqs = ctx.saved_tensors
+        axes, interleaved = ctx.cfg
+        if dq is None and dk is None:
+            return (None,) * 6
+        dq, dk = (None if d is None else d.contiguous() for d in (dq, dk))
+        how = (positions, freqs, axes)
+        if dq is None:
+            dk, _ = binding.sdgp_rotary(dk, None, *how, interleaved=interleaved, inverse=True)
+        else:
+            dq, dk = binding.sdgp_rotary(dq, dk, *how, interleaved=interleaved, inverse=True)
+        return dq, dk, None, None, None, None
+
+
+class _PolicyLossFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logp, old_logp, advantages, ref_logp, mask, offsets, clip, kl, average):
+        loss, mean_kl, clipped, weights = binding.sdgp_policy_loss(logp, old_logp, advantages, ref_logp, mask, offsets, clip=clip, kl=kl,
+                                                                   average=average)
+        ctx.save_for_backward(weights, logp, old_logp, advantages, ref_logp, mask, offsets)
+        ctx.cfg = {"clip": clip, "kl": kl, "average": average}
+        ctx.mark_non_differentiable(mean_kl, clipped)
+        return loss, mean_kl, clipped
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, g, *_):
+        return (binding.sdgp_policy_loss_bwd(g.float(), *ctx.saved_tensors, **ctx.cfg),) + (None,) * 8
+
+
+class _PreferenceLossFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logp, ref_logp, mask, offsets, beta, margin, smoothing, average):
+        loss, margins, weights = binding.sdgp_preference_loss(logp, ref_logp, mask, offsets, beta=beta, margin=margin, smoothing=smoothing,
+                                                              average=average)
+        ctx.save_for_backward(weights, logp, mask, offsets)
+        ctx.mark_non_differentiable(margins)
+        return loss, margins
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, g, *_):
+        return (binding.sdgp_preference_loss_bwd(g.float(), *ctx.saved_tensors),) + (None,) * 7
+
+
+def sdgp_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets: torch.Tensor | None = None,
+                   offsets_k: torch.Tensor | None = None, causal: bool = True, scale: float | None = None) -> torch.Tensor:
+    """Softmax attention with grouped heads: q [T, H, D], k and v [T, Hk, D] of packed sequences (``offsets``, and
+    ``offsets_k`` where the keys' differ), or [B, L, heads, D] without offsets."""
+    return _AttentionFn.apply(q, k, v, offsets, offsets_k, causal, scale)
+
+
+def sdgp_rotary(q: torch.Tensor, k: torch.Tensor | None, positions: torch.Tensor, freqs: torch.Tensor, axes=None,
+                interleaved: bool = False):
+    """``(q, k)`` turned by their positions (on several ``axes``, where positions are [..., axes]); k may be None.
+    Gradients go back to q and k alone."""
+    return _RotaryFn.apply(q, k, positions, freqs, axes, interleaved)
+
+
+def sdgp_policy_loss(logp: torch.Tensor, old_logp: torch.Tensor, advantages: torch.Tensor, ref_logp: torch.Tensor | None = None,
+                     mask: torch.Tensor | None = None, offsets: torch.Tensor | None = None, clip=(0.2, 0.2), kl: float = 0.0,
+                     average: str = "tokens"):
+    """``(loss, kl, clipped)``: the clipped policy loss with its KL term, the mean divergence and the share of ratios that are
+    cut.  Gradients go back to ``logp`` through the loss alone."""
+    return _PolicyLossFn.apply(logp, old_logp, advantages, ref_logp, mask, offsets, clip, kl, average)
+
+
+def sdgp_preference_loss(logp: torch.Tensor, ref_logp: torch.Tensor | None = None, mask: torch.Tensor | None = None,
+                         offsets: torch.Tensor | None = None, beta: float = 0.1, margin: float = 0.0, smoothing: float = 0.0,
+                         average: bool = False):
+    """``(loss, margins)`` of preferred sequences (0, 2, ..) against rejected ones (1, 3, ..).  Gradients go back to ``logp``
+    through the loss alone."""
+    return _PreferenceLossFn.apply(logp, ref_logp, mask, offsets, beta, margin, smoothing, average)

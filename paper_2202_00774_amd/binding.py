@@ -31,6 +31,8 @@ EXPORTS = ("sdgp_prune", "sdgp_linear_bwd_data", "sdgp_conv_bwd_data", "sdgp_con
            "sdgp_token_logprobs_workspace", "sdgp_token_logprobs", "sdgp_token_logprobs_bwd",
            "sdgp_block_norm", "sdgp_block_norm_bwd_workspace", "sdgp_block_norm_bwd", "sdgp_adamw_step",
            "sdgp_attention_workspace", "sdgp_attention", "sdgp_attention_bwd_workspace", "sdgp_attention_bwd",
+           "sdgp_rotary", "sdgp_sequence_loss_workspace", "sdgp_policy_loss", "sdgp_policy_loss_bwd", "sdgp_preference_loss",
+           "sdgp_preference_loss_bwd",
            "sdgp_peak_probe", "sdgp_status_string", "sdgp_version")
 
 
@@ -123,6 +125,18 @@ def load():
             lib.sdgp_attention_bwd_workspace.argtypes = [i64, i64]
             lib.sdgp_attention_bwd.restype = i32
             lib.sdgp_attention_bwd.argtypes = [vp] * 9 + [i64, vp, vp, vp, i64, i64, i64, i64, i32, i32, i32, f32, vp, sz, vp]
+            lib.sdgp_rotary.restype = i32
+            lib.sdgp_rotary.argtypes = [vp] * 6 + [i32, vp, vp, i32, i64, i64, i64, i64, i32, i32, i32, vp]
+            lib.sdgp_sequence_loss_workspace.restype = sz
+            lib.sdgp_sequence_loss_workspace.argtypes = [i64, i64]
+            lib.sdgp_policy_loss.restype = i32
+            lib.sdgp_policy_loss.argtypes = [vp] * 4 + [i32, vp, vp, i64, i64, f32, f32, f32, i32, vp, vp, vp, sz, vp]
+            lib.sdgp_policy_loss_bwd.restype = i32
+            lib.sdgp_policy_loss_bwd.argtypes = [vp] * 6 + [i32, vp, vp, i64, i64, f32, f32, f32, vp, vp]
+            lib.sdgp_preference_loss.restype = i32
+            lib.sdgp_preference_loss.argtypes = [vp] * 4 + [i64, i64, f64, f64, f64, i32, vp, vp, vp, vp, sz, vp]
+            lib.sdgp_preference_loss_bwd.restype = i32
+            lib.sdgp_preference_loss_bwd.argtypes = [vp] * 4 + [i64, i64, vp, vp]
             lib.sdgp_peak_probe.restype = i32
             lib.sdgp_peak_probe.argtypes = [i32, vp, vp, sz, i32, ctypes.POINTER(ctypes.c_double), vp]
             lib.sdgp_status_string.restype = ctypes.c_char_p
@@ -817,3 +831,181 @@ def sdgp_attention_bwd(do: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: to
     _launch("sdgp_attention_bwd", q, _ptr(do), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), strides, _ptr(offsets), _ptr(offsets_k), S,
             _ptr(dq), _ptr(dk), _ptr(dv), Tq, Tk, H, Hk, D, dt, int(causal), scale, _ptr(workspace), wbytes)
     return dq, dk, dv
+
+
+def _tokens(t: torch.Tensor, name: str, x: torch.Tensor | None = None):
+    """(distance of two tokens, of two heads) of ``t`` ([..., heads, D], the tokens evenly spaced)."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must live on the GPU")
+    if x is not None and (t.get_device() != x.get_device() or t.dtype != x.dtype):
+        raise ValueError(f"{name} must have the dtype and the GPU of the other tensors")
+    if t.dim() < 2 or t.shape[-1] < 2:
+        raise ValueError(f"expected {name} [..., heads, D]")
+    stride, shape = t.stride(), t.shape
+    if stride[-1] != 1:
+        raise ValueError(f"the values of a head of {name} must have stride 1")
+    token = expect = None
+    for n, s in zip(reversed(shape[:-2]), reversed(stride[:-2])):
+        if n == 1:
+            continue
+        if expect is not None and s != expect:
+            raise ValueError(f"the tokens of {name} must be evenly spaced")
+        token, expect = (s if token is None else token), s * n
+    return (shape[-1] if token is None else token), stride[-2]
+
+
+def _apart(out: torch.Tensor, x: torch.Tensor, name: str) -> None:
+    """``out`` is ``x`` itself, or their memory does not meet."""
+    if out.data_ptr() == x.data_ptr() and out.stride() == x.stride():
+        return
+    span = lambda t: sum((n - 1) * s for n, s in zip(t.shape, t.stride())) * t.element_size() + t.element_size()  # noqa: E731
+    if out.numel() and out.data_ptr() < x.data_ptr() + span(x) and x.data_ptr() < out.data_ptr() + span(out):
+        raise ValueError(f"the output for {name} must be {name} itself, or lie apart from it")
+
+
+def sdgp_rotary(q: torch.Tensor, k: torch.Tensor | None, positions: torch.Tensor, freqs: torch.Tensor, axes=None, *,
+                interleaved: bool = False, inverse: bool = False, out=None):
+    """``(q, k)`` turned by their positions; k may be None.
+
+    ``q`` [..., H, D] and ``k`` [..., Hk, D] (tokens and heads may be strided), ``positions`` [...] or [..., axes] (int32 or
+    int64), ``freqs`` fp32 [F], radians a position, 2 F <= D; values from 2 F on stay as they are.  ``axes``: how many of the
+    F pairs each axis of the positions turns.  Pair i is (i, F + i), with ``interleaved`` (2 i, 2 i + 1).  ``inverse``: by
+    the opposite angles, which takes gradients back.  ``out``: the pair of tensors to write, q and k themselves or others."""
+    q_strides = _tokens(q, "q")
+    tokens = q.shape[:-2]
+    T, (H, D) = tokens.numel(), q.shape[-2:]
+    _beside(positions, "positions", q), _beside(freqs, "freqs", q)
+    if freqs.dtype != torch.float32 or freqs.dim() != 1 or not 1 <= 2 * freqs.numel() <= D:
+        raise ValueError("freqs must be float32 [F], at most half a head's values")
+    axes = (freqs.numel(),) if axes is None else tuple(int(n) for n in axes)
+    if sum(axes) != freqs.numel() or any(n < 1 for n in axes) or len(axes) > 8:
+        raise ValueError("axes are up to 8 numbers of pairs that add up to the frequencies")
+    if positions.dtype not in _INTS or positions.shape != (*tokens, len(axes)) and (len(axes) > 1 or positions.shape != tokens):
+        raise ValueError("positions must be int32 or int64, one for each token and axis")
+    Hk, k_strides = 0, (0, 0)
+    if k is not None:
+        k_strides = _tokens(k, "k", q)
+        Hk = k.shape[-2]
+        if k.shape[:-2] != tokens or k.shape[-1] != D or Hk == 0:
+            raise ValueError("k must have q's tokens and head size, and heads")
+    if out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        k_out = None if k is None else torch.empty(k.shape, dtype=q.dtype, device=q.device)
+    else:
+        q_out, k_out = out
+        if (k_out is None) != (k is None):
+            raise ValueError("out holds a tensor for each of q and k")
+    out_strides = []
+    for y, x, name in ((q_out, q, "q"), (k_out, k, "k")):
+        if x is None:
+            out_strides += [0, 0]
+            continue
+        if y.shape != x.shape:
+            raise ValueError("outputs must have the shapes of q and k")
+        token, head = _tokens(y, "out", q)
+        if out is not None:
+            _apart(y, x, name)
+            if T > 1 and token < D or x.shape[-2] > 1 and head < D:
+                raise ValueError("the heads of an output must not share memory")
+        out_strides += [token, head]
+    if H == 0:
+        raise ValueError("expected q with heads")
+    _launch("sdgp_rotary", q, _ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out), (ctypes.c_int64 * 8)(*q_strides, *k_strides, *out_strides),
+            _ptr(positions), 64 if positions.dtype == torch.int64 else 32, _ptr(freqs), (ctypes.c_int32 * len(axes))(*axes), len(axes),
+            T, H, Hk, D, _dtype_code(q), int(interleaved), int(inverse))
+    return q_out, k_out
+
+
+def _sequence_sizes(x: torch.Tensor, name: str, mask, offsets):
+    """(T, sequences) of ``x``, [T] with offsets, [sequences, L] or [L] without; checks mask and offsets."""
+    _dev(x, name)
+    if x.dtype != torch.float32 or x.dim() != 1 and (x.dim() != 2 or offsets is not None):
+        raise ValueError(f"{name} must be float32, [T] with offsets, [sequences, L] or [L] without")
+    if mask is not None:
+        _per_row(mask, x.shape, "mask", (torch.bool, torch.uint8), x)
+    if offsets is not None:
+        return x.numel(), _offsets(offsets, "offsets", x).numel() - 1
+    return x.numel(), x.shape[0] if x.dim() == 2 else 1
+
+
+def _policy_arguments(logp, old_logp, advantages, ref_logp, mask, offsets, clip, kl):
+    T, S = _sequence_sizes(logp, "logp", mask, offsets)
+    _per_row(old_logp, logp.shape, "old_logp", _FLOAT, logp)
+    if ref_logp is not None:
+        _per_row(ref_logp, logp.shape, "ref_logp", _FLOAT, logp)
+    elif kl:
+        raise ValueError("kl needs ref_logp")
+    _beside(advantages, "advantages", logp)
+    each = advantages.shape == logp.shape
+    if advantages.dtype != torch.float32 or not each and advantages.shape != (S,):
+        raise ValueError("advantages must be float32, one for each token or one for each sequence")
+    low, high = clip
+    return (_ptr(old_logp), _ptr(ref_logp), _ptr(advantages), int(each), _ptr(mask), _ptr(offsets), S, T, low, high, kl), S, T
+
+
+_AVERAGES = ("tokens", "sequences")
+
+
+def sdgp_policy_loss(logp: torch.Tensor, old_logp: torch.Tensor, advantages: torch.Tensor, ref_logp: torch.Tensor | None = None,
+                     mask: torch.Tensor | None = None, offsets: torch.Tensor | None = None, *, clip=(0.2, 0.2), kl: float = 0.0,
+                     average: str = "tokens", workspace: torch.Tensor | None = None):
+    """The clipped policy loss with a KL term: ``(loss, kl, clipped, weights)``.
+
+    ``logp``, ``old_logp``, ``ref_logp``: fp32 [T] with ``offsets`` (int32 [sequences + 1]), [sequences, L] or [L] without.
+    ``advantages``: of that shape, or [sequences].  ``mask``: bool or uint8, which tokens count.  The mean is over tokens, or
+    with ``average="sequences"`` over the sequences' means.  ``kl`` and ``clipped`` are the mean divergence and the share of
+    ratios that are cut; ``weights`` is for ``sdgp_policy_loss_bwd``."""
+    if average not in _AVERAGES:
+        raise ValueError('average is "tokens" or "sequences"')
+    args, S, T = _policy_arguments(logp, old_logp, advantages, ref_logp, mask, offsets, clip, kl)
+    workspace, wbytes = _own_workspace(_need("sdgp_sequence_loss_workspace", T, S), workspace, logp, "sdgp_sequence_loss_workspace")
+    out, weights = logp.new_empty(3), logp.new_empty(S)
+    _launch("sdgp_policy_loss", logp, _ptr(logp), *args, int(average == "sequences"), _ptr(out), _ptr(weights), _ptr(workspace), wbytes)
+    return (*out.unbind(0), weights)
+
+
+def _one(g: torch.Tensor, x: torch.Tensor) -> torch.Tensor:
+    _beside(g, "g", x)
+    if g.dtype != torch.float32 or g.numel() != 1:
+        raise ValueError("g must be one float32")
+    return g
+
+
+def sdgp_policy_loss_bwd(g: torch.Tensor, weights: torch.Tensor, logp: torch.Tensor, old_logp: torch.Tensor, advantages: torch.Tensor,
+                         ref_logp: torch.Tensor | None = None, mask: torch.Tensor | None = None, offsets: torch.Tensor | None = None, *,
+                         clip=(0.2, 0.2), kl: float = 0.0, average: str = "tokens") -> torch.Tensor:
+    """dL/dlogp from ``g`` = dL/dloss (one fp32 on the GPU) and what ``sdgp_policy_loss`` took and returned."""
+    args, S, _ = _policy_arguments(logp, old_logp, advantages, ref_logp, mask, offsets, clip, kl)
+    _one(g, logp), _per_row(weights, (S,), "weights", _FLOAT, logp)
+    dlogp = torch.empty_like(logp)
+    _launch("sdgp_policy_loss_bwd", logp, _ptr(g), _ptr(weights), _ptr(logp), *args, _ptr(dlogp))
+    return dlogp
+
+
+def sdgp_preference_loss(logp: torch.Tensor, ref_logp: torch.Tensor | None = None, mask: torch.Tensor | None = None,
+                         offsets: torch.Tensor | None = None, *, beta: float = 0.1, margin: float = 0.0, smoothing: float = 0.0,
+                         average: bool = False, workspace: torch.Tensor | None = None):
+    """The loss of preferred sequences (0, 2, ..) against the rejected ones behind them (1, 3, ..): ``(loss, margins, weights)``.
+
+    A sequence scores beta times the sum (``average``: the mean) of logp - ref_logp over its tokens that count; ``margins`` are
+    the pairs' differences less ``margin``.  Shapes as for ``sdgp_policy_loss``; ``weights`` is for ``sdgp_preference_loss_bwd``."""
+    T, S = _sequence_sizes(logp, "logp", mask, offsets)
+    if S % 2:
+        raise ValueError("sequences come in pairs")
+    if ref_logp is not None:
+        _per_row(ref_logp, logp.shape, "ref_logp", _FLOAT, logp)
+    workspace, wbytes = _own_workspace(_need("sdgp_sequence_loss_workspace", T, S), workspace, logp, "sdgp_sequence_loss_workspace")
+    loss, margins, weights = logp.new_empty(()), logp.new_empty(S // 2), logp.new_empty(S)
+    _launch("sdgp_preference_loss", logp, _ptr(logp), _ptr(ref_logp), _ptr(mask), _ptr(offsets), S, T, beta, margin, smoothing, int(average),
+            _ptr(loss), _ptr(margins), _ptr(weights), _ptr(workspace), wbytes)
+    return loss, margins, weights
+
+
+def sdgp_preference_loss_bwd(g: torch.Tensor, weights: torch.Tensor, logp: torch.Tensor, mask: torch.Tensor | None = None,
+                             offsets: torch.Tensor | None = None) -> torch.Tensor:
+    """dL/dlogp from ``g`` = dL/dloss (one fp32 on the GPU) and the forward call's ``weights``; of logp only the shape is used."""
+    T, S = _sequence_sizes(logp, "logp", mask, offsets)
+    _one(g, logp), _per_row(weights, (S,), "weights", _FLOAT, logp)
+    dlogp = torch.empty_like(logp)
+    _launch("sdgp_preference_loss_bwd", logp, _ptr(g), _ptr(weights), _ptr(mask), _ptr(offsets), S, T, _ptr(dlogp))
+    return dlogp

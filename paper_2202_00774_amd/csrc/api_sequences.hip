@@ -4,6 +4,8 @@
 #include <math.h>
 
 #include "attention_api.h"
+#include "rotary.h"
+#include "sequence_loss.h"
 
 namespace {
 
@@ -38,6 +40,38 @@ int check_attention(const sdgp::AttentionCall& c) {
     for (const void* p : {c.q, c.k, c.v})
         if (!aligned(p, element(c.dt))) return SDGP_ERR_SHAPE;
     return SDGP_OK;
+}
+
+constexpr int64_t kMostTokens = (int64_t)1 << 40;
+
+// The sequences' tokens, without their addresses.
+int check_sequences(int64_t T, int64_t S, bool packed) {
+    if (T < 0 || S < 0 || S > 0x7FFFFFFF - 1024 || T > kMostTokens) return SDGP_ERR_SHAPE;
+    if (packed ? T > 0x7FFFFFFF : S == 0 ? T > 0 : T % S != 0 || T / S > 0x7FFFFFFF) return SDGP_ERR_SHAPE;   // offsets have 32 bits
+    return SDGP_OK;
+}
+
+int check_tokens(const sdgp::Sequences& s) {
+    if (s.T > 0 && !s.logp) return SDGP_ERR_NULL;
+    return aligned(s.logp, 4) && aligned(s.ref, 4) && aligned(s.offsets, 4) ? SDGP_OK : SDGP_ERR_SHAPE;
+}
+
+sdgp::Sequences sequences_of(const float* logp, const float* ref, const uint8_t* mask, const int32_t* offsets, int64_t T, int64_t S) {
+    return {logp, ref, mask, offsets, T, (int)S, S > 0 ? (int)(T / S < 0x7FFFFFFF ? T / S : 0x7FFFFFFF) : 0};
+}
+
+int check_policy(const sdgp::Sequences& s, int64_t S, const float* old, const float* advantages, int each, float low, float high, float kl) {
+    int rc = check_sequences(s.T, S, s.offsets != nullptr);
+    if (rc != SDGP_OK) return rc;
+    if (!(low >= 0.0f && low <= 1.0f) || !(high >= 0.0f) || !isfinite(kl) || kl < 0.0f || (kl > 0.0f && s.T > 0 && !s.ref)) return SDGP_ERR_VALUE;
+    rc = check_tokens(s);
+    if (rc != SDGP_OK) return rc;
+    if ((s.T > 0 && !old) || ((each ? s.T : S) > 0 && !advantages)) return SDGP_ERR_NULL;
+    return aligned(old, 4) && aligned(advantages, 4) ? SDGP_OK : SDGP_ERR_SHAPE;
+}
+
+sdgp::PolicyLoss policy_of(const sdgp::Sequences& s, const float* old, const float* advantages, int each, int by_sequence, float low, float high, float kl) {
+    return {s, old, advantages, each != 0, by_sequence != 0, kl, low, high, log1p(-(double)low), log1p((double)high)};
 }
 
 }  // namespace
@@ -83,6 +117,99 @@ int sdgp_attention_bwd(const void* dO, const void* q, const void* k, const void*
     const size_t need = sdgp_attention_bwd_workspace(Tq, H);
     if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return SDGP_ERR_WORKSPACE;
     return sdgp::attention_bwd_launch_all(c, dO, o, lse, dq, dk, dv, workspace, static_cast<hipStream_t>(hip_stream));
+}
+
+int sdgp_rotary(const void* q, const void* k, void* q_out, void* k_out, const int64_t* strides, const void* positions, int position_bits,
+                const float* freqs, const int32_t* axis_pairs, int axes, int64_t T, int64_t H, int64_t Hk, int64_t D, int dt,
+                int interleaved, int inverse, void* hip_stream) {
+    if (!valid_dtype(dt) || (position_bits != 32 && position_bits != 64)) return SDGP_ERR_DTYPE;
+    if (T < 0 || H < 1 || Hk < 0 || D < 2 || D > 4096 || H > 4096 || Hk > 4096 || axes < 1 || axes > sdgp::kMaxAxes) return SDGP_ERR_SHAPE;
+    if (T > 0x7FFFFFFF || (H + Hk) * D > (int64_t)1 << 22) return SDGP_ERR_SHAPE;
+    if (!strides || !axis_pairs) return SDGP_ERR_NULL;
+    sdgp::Rotary a = {};
+    int64_t pairs = 0;
+    for (int i = 0; i < axes; ++i) {
+        if (axis_pairs[i] < 1) return SDGP_ERR_SHAPE;
+        pairs += axis_pairs[i];
+        if (2 * pairs > D) return SDGP_ERR_SHAPE;
+        a.end[i] = (int)pairs;
+    }
+    for (int i = 0; i < 8; ++i)
+        if (strides[i] < 0 || strides[i] > kMostStride) return SDGP_ERR_SHAPE;
+    if (T == 0) return SDGP_OK;
+    if (!q || !q_out || !positions || !freqs || (Hk > 0) != (k != nullptr) || (Hk > 0) != (k_out != nullptr)) return SDGP_ERR_NULL;
+    for (const void* p : {q, k, (const void*)q_out, (const void*)k_out})
+        if (!aligned(p, element(dt))) return SDGP_ERR_SHAPE;
+    if (!aligned(positions, position_bits / 8) || !aligned(freqs, 4)) return SDGP_ERR_SHAPE;
+    // every output element is written once
+    if ((T > 1 && strides[4] < D) || (H > 1 && strides[5] < D) || (Hk > 0 && T > 1 && strides[6] < D) || (Hk > 1 && strides[7] < D)) return SDGP_ERR_SHAPE;
+    a.q = q, a.k = k, a.q_out = q_out, a.k_out = k_out;
+    a.q_token = strides[0], a.q_head = strides[1], a.k_token = strides[2], a.k_head = strides[3];
+    a.q_out_token = strides[4], a.q_out_head = strides[5], a.k_out_token = strides[6], a.k_out_head = strides[7];
+    a.positions = positions, a.freqs = freqs, a.T = T, a.H = (int)H, a.Hk = (int)Hk, a.D = (int)D, a.F = (int)pairs, a.axes = axes;
+    a.position_bits = position_bits, a.inverse = inverse != 0;
+    return sdgp::rotary_launch(a, dt, interleaved != 0, static_cast<hipStream_t>(hip_stream));
+}
+
+size_t sdgp_sequence_loss_workspace(int64_t T, int64_t sequences) {
+    if (T < 0 || sequences < 0 || sequences > 0x7FFFFFFF - 1024 || T > kMostTokens) return (size_t)-1;
+    return sdgp::sequence_loss_workspace(T, sequences);
+}
+
+int sdgp_policy_loss(const float* logp, const float* old_logp, const float* ref_logp, const float* advantages, int each,
+                     const uint8_t* mask, const int32_t* offsets, int64_t sequences, int64_t T, float low, float high, float kl,
+                     int by_sequence, float* out, float* weights, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    const sdgp::Sequences s = sequences_of(logp, ref_logp, mask, offsets, T, sequences);
+    const int rc = check_policy(s, sequences, old_logp, advantages, each, low, high, kl);
+    if (rc != SDGP_OK) return rc;
+    if (!out || (sequences > 0 && !weights)) return SDGP_ERR_NULL;
+    if (!aligned(out, 4) || !aligned(weights, 4)) return SDGP_ERR_SHAPE;
+    const size_t need = sdgp::sequence_loss_workspace(T, sequences);
+    if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return SDGP_ERR_WORKSPACE;
+    return sdgp::policy_loss_launch(policy_of(s, old_logp, advantages, each, by_sequence, low, high, kl), out, weights, workspace,
+                                    static_cast<hipStream_t>(hip_stream));
+}
+
+int sdgp_policy_loss_bwd(const float* g, const float* weights, const float* logp, const float* old_logp, const float* ref_logp,
+                         const float* advantages, int each, const uint8_t* mask, const int32_t* offsets, int64_t sequences, int64_t T,
+                         float low, float high, float kl, float* dlogp, void* hip_stream) {
+    const sdgp::Sequences s = sequences_of(logp, ref_logp, mask, offsets, T, sequences);
+    const int rc = check_policy(s, sequences, old_logp, advantages, each, low, high, kl);
+    if (rc != SDGP_OK) return rc;
+    if (T == 0) return SDGP_OK;
+    if (!g || (sequences > 0 && !weights) || !dlogp) return SDGP_ERR_NULL;
+    if (!aligned(g, 4) || !aligned(weights, 4) || !aligned(dlogp, 4)) return SDGP_ERR_SHAPE;
+    return sdgp::policy_loss_bwd_launch(policy_of(s, old_logp, advantages, each, 0, low, high, kl), g, weights, dlogp,
+                                        static_cast<hipStream_t>(hip_stream));
+}
+
+int sdgp_preference_loss(const float* logp, const float* ref_logp, const uint8_t* mask, const int32_t* offsets, int64_t sequences,
+                         int64_t T, double beta, double margin, double smoothing, int average, float* loss, float* margins,
+                         float* weights, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    const sdgp::Sequences s = sequences_of(logp, ref_logp, mask, offsets, T, sequences);
+    int rc = check_sequences(T, sequences, offsets != nullptr);
+    if (rc != SDGP_OK) return rc;
+    if (sequences % 2 != 0) return SDGP_ERR_SHAPE;
+    if (!isfinite(beta) || !isfinite(margin) || !(smoothing >= 0.0 && smoothing < 1.0)) return SDGP_ERR_VALUE;
+    rc = check_tokens(s);
+    if (rc != SDGP_OK) return rc;
+    if (!loss || (sequences > 0 && (!margins || !weights))) return SDGP_ERR_NULL;
+    if (!aligned(loss, 4) || !aligned(margins, 4) || !aligned(weights, 4)) return SDGP_ERR_SHAPE;
+    const size_t need = sdgp::sequence_loss_workspace(T, sequences);
+    if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return SDGP_ERR_WORKSPACE;
+    return sdgp::preference_loss_launch({s, beta, margin, smoothing, average != 0}, loss, margins, weights, workspace,
+                                        static_cast<hipStream_t>(hip_stream));
+}
+
+int sdgp_preference_loss_bwd(const float* g, const float* weights, const uint8_t* mask, const int32_t* offsets, int64_t sequences,
+                             int64_t T, float* dlogp, void* hip_stream) {
+    const int rc = check_sequences(T, sequences, offsets != nullptr);
+    if (rc != SDGP_OK) return rc;
+    if (T == 0) return SDGP_OK;
+    if (!g || (sequences > 0 && !weights) || !dlogp) return SDGP_ERR_NULL;
+    if (!aligned(g, 4) || !aligned(weights, 4) || !aligned(dlogp, 4) || !aligned(offsets, 4)) return SDGP_ERR_SHAPE;
+    return sdgp::preference_loss_bwd_launch(sequences_of(nullptr, nullptr, mask, offsets, T, sequences), g, weights, dlogp,
+                                            static_cast<hipStream_t>(hip_stream));
 }
 
 }  // extern "C"
