@@ -18,6 +18,7 @@ struct Attention {
     int S, Lq, Lk, Tq, Tk, H, Hk, G, D, causal;
     FastDiv by_group;                                            // rows / G
     float scale, c;                                              // c = scale log2 e
+    bool fast;                                                   // Feed<..., FAST>
     void* o;
     float* lse;
     int parts;                                                   // forward: pieces of a row's keys
@@ -190,6 +191,23 @@ __device__ __forceinline__ Operand<DT> load_operand(const char* row, int e, int 
     return f;
 }
 
+// The same of rows of whole chunks on sixteen bytes.
+template <int DT, bool FAST>
+__device__ __forceinline__ Operand<DT> load_operand(const char* row, int e, int n) {
+    if constexpr (!FAST) return load_operand<DT>(row, e, n);
+    constexpr int N = 16 / Operand<DT>::kSize;                          // an operand is 8 / N chunks
+    union {
+        Operand<DT> f;
+        attn_u32x4 w[8 / N];
+    } u;
+#pragma unroll
+    for (int i = 0; i < 8 / N; ++i) {
+        u.w[i] = attn_u32x4{0, 0, 0, 0};
+        if (e + i * N < n) u.w[i] = *reinterpret_cast<const attn_u32x4*>(row + (e + i * N) * Operand<DT>::kSize);
+    }
+    return u.f;
+}
+
 // A tile of rows of up to DC values in LDS.  Its sixteen-byte chunks change places within a row (XOR with a number of the
 // row) so that both ways of reading it meet all banks: `rows`, sixteen lanes at one chunk of sixteen rows; `columns`, four
 // rows of four neighbouring chunks.
@@ -203,15 +221,25 @@ struct Tile {
     }
     static __device__ __forceinline__ int at(int row, int chunk) { return row * kRow + ((chunk ^ place(row)) << 4); }
 
-    // Rows r0 + lane % 32, values 16 step + 8 (lane / 32) ..: an operand summed over the values.  r0 % 32 == 0.
-    static __device__ __forceinline__ Operand<DT> rows(SDGP_SHARED char* tile, int r0, int step, int lane) {
-        const int row = lane & 31, half = lane >> 5;
+    // A lane's place in a tile, for `rows` and for `columns`.  Which chunk and which block of columns comes last into an address, as
+    // an XOR of its lower bits: the one register serves every read of the tile.  Tiles begin on a multiple of a row.
+    static __device__ __forceinline__ uint32_t rows_lane(SDGP_SHARED char* tile, int lane) {
+        return (uint32_t)(uintptr_t)tile + (uint32_t)at(lane & 31, (lane >> 5) * (DT == SDGP_BF16 ? 1 : 2));
+    }
+    static __device__ __forceinline__ uint32_t columns_lane(SDGP_SHARED char* tile, int lane) {
+        if constexpr (DT == SDGP_BF16)   // of sixteen lanes, each four on one row: the transposing read hands lane i column i of the four rows
+            return (uint32_t)(uintptr_t)tile + (uint32_t)(at(4 * (lane >> 5) + ((lane & 15) >> 2), ((lane >> 3) & 2) + ((lane & 3) >> 1)) + (lane & 1) * 8);
+        return (uint32_t)(uintptr_t)tile + (uint32_t)(at(4 * (lane >> 5), (lane & 31) >> 2) + (lane & 3) * 4);
+    }
+
+    // Rows r0 + lane % 32 of the tile `plus` bytes on, values 16 step + 8 (lane / 32) ..: an operand summed over the values.  r0 % 32 == 0.
+    static __device__ __forceinline__ Operand<DT> rows(uint32_t lane_at, int r0, int step, int plus = 0) {
         Operand<DT> f;
         if constexpr (DT == SDGP_BF16) {
-            f.w = *(SDGP_SHARED attn_u32x4*)(tile + r0 * kRow + at(row, 2 * step + half));
+            f.w = *(SDGP_SHARED attn_u32x4*)(uintptr_t)((lane_at ^ (uint32_t)(step << 5)) + (uint32_t)(r0 * kRow + plus));
         } else {
-            const attn_u32x4 a = *(SDGP_SHARED attn_u32x4*)(tile + r0 * kRow + at(row, 4 * step + 2 * half));
-            const attn_u32x4 b = *(SDGP_SHARED attn_u32x4*)(tile + r0 * kRow + at(row, 4 * step + 2 * half + 1));
+            const attn_u32x4 a = *(SDGP_SHARED attn_u32x4*)(uintptr_t)((lane_at ^ (uint32_t)(step << 6)) + (uint32_t)(r0 * kRow + plus));
+            const attn_u32x4 b = *(SDGP_SHARED attn_u32x4*)(uintptr_t)((lane_at ^ (uint32_t)(step << 6 | 16)) + (uint32_t)(r0 * kRow + plus));
 #pragma unroll
             for (int i = 0; i < 4; ++i) f.x[i] = bits_to_float(a[i]), f.x[4 + i] = bits_to_float(b[i]);
         }
@@ -220,58 +248,108 @@ struct Tile {
 
     // Column 32 block + lane % 32 of rows r0 + result_row(0 .. 7, lane / 32): an operand summed over the rows, its eight in the
     // order in which a lane holds half a result's rows, so that results are the other operand as they are.  r0 % 16 == 0.
-    static __device__ __forceinline__ Operand<DT> columns(SDGP_SHARED char* tile, int r0, int block, int lane) {
-        const int half = lane >> 5;
+    static __device__ __forceinline__ Operand<DT> columns(uint32_t lane_at, int r0, int block, int plus = 0) {
         Operand<DT> f;
         if constexpr (DT == SDGP_BF16) {
-            // the transposing read: of sixteen lanes, each four on one row, lane i receives column i of the four rows
-            const int row = 4 * half + ((lane & 15) >> 2), chunk = 4 * block + ((lane >> 3) & 2) + ((lane & 3) >> 1);
             attn_s16x4 x[2];
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int u = 0; u < 2; ++u)                                 // eight rows on, `place` differs by two
                 x[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (SDGP_SHARED attn_s16x4*)(tile + r0 * kRow + at(row + 8 * u, chunk) + (lane & 1) * 8));
+                    (SDGP_SHARED attn_s16x4*)(uintptr_t)((lane_at ^ (uint32_t)(block << 6 | u << 5)) + (uint32_t)((r0 + 8 * u) * kRow + plus)));
             const attn_s16x8 all = {x[0][0], x[0][1], x[0][2], x[0][3], x[1][0], x[1][1], x[1][2], x[1][3]};
             f.w = __builtin_bit_cast(attn_u32x4, all);
         } else {
-            const int col = lane & 31;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int row = result_row(i, half);
-                f.x[i] = *(SDGP_SHARED float*)(tile + r0 * kRow + at(row, 8 * block + (col >> 2)) + (col & 3) * 4);
+            for (int i = 0; i < 8; ++i) {                               // row i % 4 + 8 (i / 4) of the lane's four
+                static_assert(kChunks >= 16, "fp32 rows");
+                const uint32_t places = (uint32_t)((i & 3) << 2 | (i >> 2) << 1);
+                f.x[i] = *(SDGP_SHARED float*)(uintptr_t)((lane_at ^ ((uint32_t)(block << 7) ^ places << 4)) + (uint32_t)((r0 + (i & 3) + 8 * (i >> 2)) * kRow + plus));
             }
         }
         return f;
     }
 };
 
-// Copies rows of a tensor into a tile by way of registers, so that a tile's loads fly while the one before it is worked on.
-// THREADS threads; ROWS rows of DC values.
-template <int DT, int DC, int ROWS, int THREADS>
-struct Stage {
-    using T = Tile<DT, DC>;
-    static constexpr int kNeed = DC * Operand<DT>::kSize / 16;          // chunks of a row that anyone reads
-    static constexpr int kEach = (ROWS * T::kChunks + THREADS - 1) / THREADS;
-    attn_u32x4 held[kEach];
+// A value that the compiler computes where it stands and not ahead of a loop: registers are worth more there.
+__device__ __forceinline__ uint32_t here(uint32_t x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
 
-    // row(i): the address of row i, or null for a row of zeros
-    template <class Row>
-    __device__ __forceinline__ void load(Row&& row, int D) {
+// Brings rows of a tensor into a tile while the one before it is worked on: `start` asks for them, `finish` comes before the
+// barrier behind which they are read.  256 threads; ROWS rows of up to DC values, zeros behind the tensor's last row.
+//
+// FAST: straight into LDS (buffer loads, whose bounds check makes the zeros), sixteen bytes a lane, each lane the chunk that belongs
+// where its bytes land.  Rows on sixteen bytes, D a whole number of chunks.  Else by way of registers, from any element on.
+template <int DT, int DC, int ROWS, bool FAST>
+struct Feed;
+
+template <int DT, int DC, int ROWS>
+struct Feed<DT, DC, ROWS, true> {
+    using T = Tile<DT, DC>;
+    static constexpr int kEach = ROWS * T::kChunks / 256;               // instructions a wavefront
+    static constexpr int kStep = 256 / T::kChunks;                      // rows between them
+    static constexpr int kPlaces = kStep % 16 == 0 ? 1 : 2;             // `place` tells sixteen rows apart
+    static_assert(kEach * 256 == ROWS * T::kChunks && kStep * kPlaces % 16 == 0, "whole instructions");
+    static constexpr uint32_t kNone = 0x7FFFFFF0u;                      // behind every record
+    const char* base;
+    int64_t row;
+    int width;
+    uint32_t first[kPlaces];
+
+    __device__ __forceinline__ Feed(const char* tensor, int64_t row_bytes, int D) : base(tensor), row(row_bytes), width(D * Operand<DT>::kSize) {
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int x = (int)threadIdx.x + i * THREADS, r = x / T::kChunks, chunk = x % T::kChunks;
-            held[i] = attn_u32x4{0, 0, 0, 0};
-            if (chunk < kNeed && r < ROWS) {
-                const char* p = row(r);
-                if (p != nullptr) held[i] = load_chunk<DT>(p, chunk * (16 / Operand<DT>::kSize), D);
-            }
+        for (int i = 0; i < kPlaces; ++i) {
+            const int r = (int)threadIdx.x / T::kChunks + i * kStep, chunk = ((int)threadIdx.x % T::kChunks) ^ T::place(r);
+            first[i] = chunk * 16 < width ? (uint32_t)(r * (int)row_bytes + chunk * 16) : kNone;
         }
     }
-    __device__ __forceinline__ void store(SDGP_SHARED char* tile) const {
+    // rows r0 .. r0 + ROWS - 1 of `rows`
+    __device__ __forceinline__ void start(SDGP_SHARED char* tile, int r0, int rows) {
+        const uint64_t at = (uint64_t)(uintptr_t)(base + r0 * row);
+        const int64_t left = (int64_t)(rows - r0 - 1) * row + width;
+        const int records = rows <= r0 ? 0 : left < 0x7FFFFFF0 ? (int)left : 0x7FFFFFF0;
+        attn_u32x4 v;
+        v[0] = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)at);
+        v[1] = (uint32_t)__builtin_amdgcn_readfirstlane((int)((uint32_t)(at >> 32) & 0xFFFFu));
+        v[2] = (uint32_t)__builtin_amdgcn_readfirstlane(records);
+        v[3] = 0x00027000u;
+        const uint32_t to = (uint32_t)(uintptr_t)tile + ((uint32_t)__builtin_amdgcn_readfirstlane((int)threadIdx.x / 64) << 10);
+        const uint32_t lds = (uint32_t)__builtin_amdgcn_readfirstlane((int)to);
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            const int x = (int)threadIdx.x + i * THREADS, r = x / T::kChunks, chunk = x % T::kChunks;
-            if (chunk < kNeed && r < ROWS) *(SDGP_SHARED attn_u32x4*)(tile + T::at(r, chunk)) = held[i];
+            const uint32_t from = first[i % kPlaces];
+            const uint32_t offset = from == kNone ? from : from + (uint32_t)(i / kPlaces * kPlaces * kStep) * (uint32_t)row;
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds + i * 4096), "v"(offset), "s"(v) : "memory");
+        }
+    }
+    __device__ __forceinline__ void finish(SDGP_SHARED char*) { __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8)); }   // vmcnt 0
+};
+
+template <int DT, int DC, int ROWS>
+struct Feed<DT, DC, ROWS, false> {
+    using T = Tile<DT, DC>;
+    static constexpr int kNeed = DC * Operand<DT>::kSize / 16;          // chunks of a row that anyone reads
+    static constexpr int kEach = ROWS * T::kChunks / 256;
+    attn_u32x4 held[kEach];
+    const char* base;
+    int64_t row;
+    int D;
+
+    __device__ __forceinline__ Feed(const char* tensor, int64_t row_bytes, int width) : base(tensor), row(row_bytes), D(width) {}
+    __device__ __forceinline__ void start(SDGP_SHARED char*, int r0, int rows) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int x = (int)threadIdx.x + i * 256, r = x / T::kChunks, chunk = x % T::kChunks;
+            held[i] = attn_u32x4{0, 0, 0, 0};
+            if (chunk < kNeed && r0 + r < rows) held[i] = load_chunk<DT>(base + (r0 + r) * row, chunk * (16 / Operand<DT>::kSize), D);
+        }
+    }
+    __device__ __forceinline__ void finish(SDGP_SHARED char* tile) const {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int x = (int)threadIdx.x + i * 256, r = x / T::kChunks, chunk = x % T::kChunks;
+            if (chunk < kNeed) *(SDGP_SHARED attn_u32x4*)(tile + T::at(r, chunk)) = held[i];
         }
     }
 };

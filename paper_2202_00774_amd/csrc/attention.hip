@@ -45,6 +45,15 @@ Attention arguments(const AttentionCall& c) {
     a.by_group = fast_div((uint32_t)a.G);
     a.scale = c.scale, a.c = c.scale * 1.44269504088896341f;
     a.parts = 1;
+    // Feed<..., FAST>: whole chunks on sixteen bytes, a token's distance of at least a head and within what a tile's offsets count
+    const int64_t size = c.dt == SDGP_BF16 ? 2 : 4;
+    uintptr_t all = reinterpret_cast<uintptr_t>(c.q) | reinterpret_cast<uintptr_t>(c.k) | reinterpret_cast<uintptr_t>(c.v) | (uintptr_t)(c.D * size);
+    a.fast = true;
+    for (int i = 0; i < 6; ++i) {
+        all |= (uintptr_t)(c.strides[i] * size);
+        if (i % 2 == 0 && (c.strides[i] < c.D || c.strides[i] * size >= 1 << 23)) a.fast = false;
+    }
+    a.fast = a.fast && (all & 15u) == 0 && c.H * c.D * size < 1 << 23;
     return a;
 }
 
@@ -71,6 +80,7 @@ int attention_bwd_launch_all(const AttentionCall& c, const void* d_o, const void
     Attention a = arguments(c);
     a.d_o = d_o, a.o_in = o, a.lse = const_cast<float*>(lse), a.dq = dq, a.dk = dk, a.dv = dv;
     a.delta = static_cast<float*>(workspace);
+    a.fast = a.fast && (reinterpret_cast<uintptr_t>(d_o) & 15u) == 0;
     const bool packed = c.offsets_q != nullptr;
     const int64_t row_tiles = c.Tq == 0 ? 0 : most_tiles(packed, c.S, c.Tq, a.Lq, a.G, 128);
     const int64_t key_tiles = c.Tk == 0 ? 0 : most_tiles(packed, c.S, c.Tk, a.Lk, 1, 128);

@@ -22,12 +22,12 @@ struct AttentionDq {
     static constexpr int kTile = kKeys * T::kRow, kBuffer = 2 * kTile, kLds = 2 * kBuffer;
 };
 
-template <int DT, int DC>
+template <int DT, int DC, bool FAST>
 __global__ void __launch_bounds__(256, DT == SDGP_BF16 ? 2 : 1) attention_dq_kernel(const Attention a) {
     using L = AttentionDq<DT, DC>;
     using T = typename L::T;
     constexpr int SIZE = Operand<DT>::kSize, STEPS = DC / 16, DB = DC / 32;
-    __shared__ __attribute__((aligned(16))) char lds_bytes[L::kLds];
+    __shared__ __attribute__((aligned(512))) char lds_bytes[L::kLds];
     SDGP_SHARED char* lds = (SDGP_SHARED char*)lds_bytes;
 
     const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
@@ -58,9 +58,9 @@ __global__ void __launch_bounds__(256, DT == SDGP_BF16 ? 2 : 1) attention_dq_ker
         const char* po = static_cast<const char*>(a.o_in) + out_row * a.D * SIZE;
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) {
-            q[i] = load_operand<DT>(p, 16 * i + 8 * half, width);
-            dO[i] = load_operand<DT>(pd, 16 * i + 8 * half, width);
-            const Operand<DT> o = load_operand<DT>(po, 16 * i + 8 * half, width);
+            q[i] = load_operand<DT, FAST>(p, 16 * i + 8 * half, width);
+            dO[i] = load_operand<DT, FAST>(pd, 16 * i + 8 * half, width);
+            const Operand<DT> o = load_operand<DT, FAST>(po, 16 * i + 8 * half, width);
 #pragma unroll
             for (int e = 0; e < 8; ++e) delta = __builtin_fmaf(dO[i].get(e), o.get(e), delta);
         }
@@ -74,24 +74,30 @@ __global__ void __launch_bounds__(256, DT == SDGP_BF16 ? 2 : 1) attention_dq_ker
     const int64_t k_row = a.k_token * SIZE, v_row = a.v_token * SIZE;
     const int end = (most + L::kKeys - 1) / L::kKeys;
 
-    Stage<DT, DC, L::kKeys, L::kThreads> sk, sv;
-    const auto fetch = [&](int n) {
-        sk.load([&](int r) { const int at = n * L::kKeys + r; return at < s.nk ? keys + at * k_row : nullptr; }, a.D);
-        sv.load([&](int r) { const int at = n * L::kKeys + r; return at < s.nk ? values + at * v_row : nullptr; }, a.D);
+    Feed<DT, DC, L::kKeys, FAST> fk(keys, k_row, a.D), fv(values, v_row, a.D);
+    const auto buffer = [&](int n) { return lds + (n & 1) * L::kBuffer; };
+    const auto start = [&](int n) {
+        fk.start(buffer(n), n * L::kKeys, s.nk);
+        fv.start(buffer(n) + L::kTile, n * L::kKeys, s.nk);
+    };
+    const auto finish = [&](int n) {
+        fk.finish(buffer(n));
+        fv.finish(buffer(n) + L::kTile);
+        __syncthreads();
     };
     attn_f32x16 dq[DB];
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) dq[d][i] = 0.0f;
-    if (end > 0) fetch(0);
+    if (end > 0) {
+        start(0);
+        finish(0);
+    }
     for (int n = 0; n < end; ++n) {
-        SDGP_SHARED char* kt = lds + (n & 1) * L::kBuffer;
-        SDGP_SHARED char* vt = kt + L::kTile;
-        sk.store(kt);
-        sv.store(vt);
-        __syncthreads();
-        if (n + 1 < end) fetch(n + 1);
+        SDGP_SHARED char *kt = buffer(n), *vt = kt + L::kTile;
+        if (n + 1 < end) start(n + 1);
+        const uint32_t k_rows = T::rows_lane(kt, lane), v_rows = T::rows_lane(vt, lane), k_columns = T::columns_lane(kt, lane);
 #pragma unroll
         for (int b = 0; b < L::kBlocks; ++b) {
             const int key0 = n * L::kKeys + 32 * b;
@@ -100,9 +106,9 @@ __global__ void __launch_bounds__(256, DT == SDGP_BF16 ? 2 : 1) attention_dq_ker
 #pragma unroll
             for (int i = 0; i < 16; ++i) x[i] = dp[i] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < STEPS; ++i) x = multiply(T::rows(kt, 32 * b, i, lane), q[i], x);
+            for (int i = 0; i < STEPS; ++i) x = multiply(T::rows(k_rows, 32 * b, i), q[i], x);
 #pragma unroll
-            for (int i = 0; i < STEPS; ++i) dp = multiply(T::rows(vt, 32 * b, i, lane), dO[i], dp);
+            for (int i = 0; i < STEPS; ++i) dp = multiply(T::rows(v_rows, 32 * b, i), dO[i], dp);
 #pragma unroll
             for (int i = 0; i < 16; ++i) x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.c, -lse2)) * (dp[i] - delta);
             if (key0 + 32 > fewest) {
@@ -121,14 +127,16 @@ __global__ void __launch_bounds__(256, DT == SDGP_BF16 ? 2 : 1) attention_dq_ker
 #pragma unroll
             for (int d = 0; d < DB; ++d)
 #pragma unroll
-                for (int u = 0; u < 2; ++u) dq[d] = multiply(T::columns(kt, 32 * b + 16 * u, d, lane), ds[u], dq[d]);
+                for (int u = 0; u < 2; ++u) dq[d] = multiply(T::columns(k_columns, 32 * b + 16 * u, d), ds[u], dq[d]);
         }
+        if (n + 1 < end) finish(n + 1);
     }
     if (row >= rows) return;
 #pragma unroll
     for (int d = 0; d < DB; ++d) store_block<DT>(static_cast<char*>(a.dq) + out_row * a.D * SIZE, dq[d], d, half, a.D, a.scale);
 }
 
+// The queries pass by in tiles of kRows tokens of one head; a group's heads one after the other.
 template <int DT, int DC>
 struct AttentionDkv {
     static constexpr int kThreads = 256, kKeys = 128, kRows = DT == SDGP_BF16 ? 64 : 32, kBlocks = kRows / 32;
@@ -136,14 +144,13 @@ struct AttentionDkv {
     static constexpr int kTile = kRows * T::kRow, kBuffer = 2 * kTile, kLds = 2 * kBuffer;
 };
 
-template <int DT, int DC>
-__global__ void __launch_bounds__(256, 1) attention_dkv_kernel(const Attention a) {
+template <int DT, int DC, bool FAST>
+__global__ void __launch_bounds__(256, DT == SDGP_BF16 ? 2 : 1) attention_dkv_kernel(const Attention a) {
     using L = AttentionDkv<DT, DC>;
     using T = typename L::T;
-    constexpr int SIZE = Operand<DT>::kSize, STEPS = DC / 16, DB = DC / 32;
-    __shared__ __attribute__((aligned(16))) char lds_bytes[L::kLds];
+    constexpr int SIZE = Operand<DT>::kSize, STEPS = DC / 16, DB = DC / 32, NB = L::kBlocks;
+    __shared__ __attribute__((aligned(512))) char lds_bytes[L::kLds];
     __shared__ __attribute__((aligned(16))) float lds_lse[2][L::kRows], lds_delta[2][L::kRows];
-    __shared__ __attribute__((aligned(16))) int lds_seen[2][L::kRows];
     SDGP_SHARED char* lds = (SDGP_SHARED char*)lds_bytes;
 
     const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
@@ -151,10 +158,8 @@ __global__ void __launch_bounds__(256, 1) attention_dkv_kernel(const Attention a
     Sequence s;
     int tile, tiles;
     if (!find_tile<true, L::kKeys>(a, blockIdx.x / a.Hk, s, tile, tiles)) return;   // the first keys have the most rows
-    const int rows = s.nq * a.G, key0 = tile * L::kKeys + 32 * wave, key = key0 + (lane & 31);
-    const auto seen = [&](int r) {
-        return a.causal ? clamp_int((int)divide((uint32_t)r, a.by_group) + 1 + s.nk - s.nq, 0, s.nk) : s.nk;
-    };
+    const int key0 = tile * L::kKeys + 32 * wave, key = key0 + (lane & 31);
+    const int ahead = s.nk - s.nq;                                      // token t sees the keys up to t + ahead, if causal
     const int width = key < s.nk ? a.D : 0;
     const int64_t key_row = s.k0 + (key < s.nk ? key : 0);
     Operand<DT> k[STEPS], v[STEPS];
@@ -163,103 +168,124 @@ __global__ void __launch_bounds__(256, 1) attention_dkv_kernel(const Attention a
         const char* pv = static_cast<const char*>(a.v) + (key_row * a.v_token + (int64_t)head * a.v_head) * SIZE;
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) {
-            k[i] = load_operand<DT>(pk, 16 * i + 8 * half, width);
-            v[i] = load_operand<DT>(pv, 16 * i + 8 * half, width);
+            k[i] = load_operand<DT, FAST>(pk, 16 * i + 8 * half, width);
+            v[i] = load_operand<DT, FAST>(pv, 16 * i + 8 * half, width);
         }
     }
-    // The first token that sees this tile's first key, and the tiles of rows from there on.
-    int from = a.causal ? tile * L::kKeys + s.nq - s.nk : 0;
-    from = clamp_int(from, 0, s.nq);
-    const int begin = from * a.G / L::kRows, end = s.nk > 0 ? (rows + L::kRows - 1) / L::kRows : 0;
+    // The first token that sees this tile's first key, and the tiles of tokens from there on, of each head.
+    const int from = a.causal ? clamp_int(tile * L::kKeys - ahead, 0, s.nq) : 0;
+    const int first = from / L::kRows, each = s.nk > 0 ? (s.nq + L::kRows - 1) / L::kRows - first : 0, end = each * a.G;
 
-    Stage<DT, DC, L::kRows, L::kThreads> sq, sd;
+    const int64_t q_row = a.q_token * SIZE, d_row = (int64_t)a.H * a.D * SIZE;
+    const char* queries = static_cast<const char*>(a.q) + ((int64_t)s.q0 * a.q_token + (int64_t)head * a.G * a.q_head) * SIZE;
+    const char* grads = static_cast<const char*>(a.d_o) + ((int64_t)s.q0 * a.H + head * a.G) * a.D * SIZE;
+    Feed<DT, DC, L::kRows, FAST> fq(queries, q_row, a.D), fd(grads, d_row, a.D);
     float next_lse = 0.0f, next_delta = 0.0f;
-    int next_seen = 0;
-    const auto fetch = [&](int n) {
-        const auto place = [&](int r, int& tok, int& g) {
-            const int at = n * L::kRows + r;
-            tok = (int)divide((uint32_t)at, a.by_group), g = at - tok * a.G;
-            return at < rows;
-        };
-        sq.load([&](int r) -> const char* {
-            int tok, g;
-            if (!place(r, tok, g)) return nullptr;
-            return static_cast<const char*>(a.q) + ((int64_t)(s.q0 + tok) * a.q_token + (int64_t)(head * a.G + g) * a.q_head) * SIZE;
-        }, a.D);
-        sd.load([&](int r) -> const char* {
-            int tok, g;
-            if (!place(r, tok, g)) return nullptr;
-            return static_cast<const char*>(a.d_o) + ((int64_t)(s.q0 + tok) * a.H + head * a.G + g) * a.D * SIZE;
-        }, a.D);
+    int next = first, g = 0;                                            // the tile that is asked for next, and its head
+    const auto buffer = [&](int n) { return lds + (n & 1) * L::kBuffer; };
+    const auto start = [&](int n) {
+        fq.start(buffer(n), next * L::kRows, s.nq);
+        fd.start(buffer(n) + L::kTile, next * L::kRows, s.nq);
         if ((int)threadIdx.x < L::kRows) {
-            int tok, g;
-            next_lse = next_delta = 0.0f, next_seen = 0x7FFFFFFF;        // rows behind the last: zeros throughout
-            if (place((int)threadIdx.x, tok, g)) {
-                const int64_t at = (int64_t)(s.q0 + tok) * a.H + head * a.G + g;
+            const int t = next * L::kRows + (int)threadIdx.x;
+            next_lse = next_delta = 0.0f;                               // tokens behind the last: zeros throughout
+            if (t < s.nq) {
+                const int64_t at = (int64_t)(s.q0 + t) * a.H + head * a.G + g;
                 next_lse = a.lse[at] * kLog2E, next_delta = a.delta[at];
-                next_seen = seen(n * L::kRows + (int)threadIdx.x);
             }
         }
+        if (++next == first + each) {
+            next = first, ++g;
+            fq.base += a.q_head * SIZE;
+            fd.base += a.D * SIZE;
+        }
+    };
+    const auto finish = [&](int n) {
+        fq.finish(buffer(n));
+        fd.finish(buffer(n) + L::kTile);
+        if ((int)threadIdx.x < L::kRows) lds_lse[n & 1][threadIdx.x] = next_lse, lds_delta[n & 1][threadIdx.x] = next_delta;
+        __syncthreads();
     };
     attn_f32x16 dk[DB], dv[DB];
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) dk[d][i] = dv[d][i] = 0.0f;
-    if (begin < end) fetch(begin);
-    for (int n = begin; n < end; ++n) {
-        const int turn = n & 1;
-        SDGP_SHARED char* qt = lds + turn * L::kBuffer;
-        SDGP_SHARED char* dt = qt + L::kTile;
-        sq.store(qt);
-        sd.store(dt);
-        if ((int)threadIdx.x < L::kRows)
-            lds_lse[turn][threadIdx.x] = next_lse, lds_delta[turn][threadIdx.x] = next_delta, lds_seen[turn][threadIdx.x] = next_seen;
-        __syncthreads();
-        if (n + 1 < end) fetch(n + 1);
+    // One block of 32 tokens.  Operands from LDS are asked for kAhead products before they are needed, and no earlier: the keys'
+    // operands and sums fill three quarters of the registers of two wavefronts a SIMD, which cover each other's other work.
+    const auto block = [&](int b, int turn, int t0, bool masked) __attribute__((always_inline)) {
+        constexpr int kAhead = 2;
+        SDGP_SHARED char* tiles = lds + turn * L::kBuffer + b * 32 * T::kRow;    // of queries, and kTile on of gradients
+        Operand<DT> f[kAhead + 1];
+        attn_f32x16 x, dp;
 #pragma unroll
-        for (int b = 0; b < L::kBlocks; ++b) {
-            const int r0 = n * L::kRows + 32 * b, last = rows - 1 < r0 + 31 ? rows - 1 : r0 + 31;
-            if (r0 >= rows || seen(last) <= key0) continue;
-            attn_f32x16 x, dp;
+        for (int i = 0; i < 16; ++i) x[i] = dp[i] = 0.0f;
+        const uint32_t rows_at = here(T::rows_lane(tiles, lane));
+        const auto rows = [&](int i) { return i < STEPS ? T::rows(rows_at, 0, i) : T::rows(rows_at, 0, i - STEPS, L::kTile); };
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = dp[i] = 0.0f;
+        for (int i = 0; i < kAhead; ++i) f[i] = rows(i);
 #pragma unroll
-            for (int i = 0; i < STEPS; ++i) x = multiply(T::rows(qt, 32 * b, i, lane), k[i], x);
-#pragma unroll
-            for (int i = 0; i < STEPS; ++i) dp = multiply(T::rows(dt, 32 * b, i, lane), v[i], dp);
-            float p[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int r = 32 * b + result_row(i, half);
-                p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.c, -lds_lse[turn][r]));
-            }
-            if (seen(r0) < key0 + 32) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (key >= lds_seen[turn][32 * b + result_row(i, half)]) p[i] = 0.0f;
-            }
-            Operand<DT> po[2], ds[2];
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                float y[8], z[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int r = 32 * b + result_row(8 * u + i, half);
-                    y[i] = p[8 * u + i];
-                    z[i] = y[i] * (dp[8 * u + i] - lds_delta[turn][r]);
-                }
-                po[u].set(y);
-                ds[u].set(z);
-            }
-#pragma unroll
-            for (int d = 0; d < DB; ++d)
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    dv[d] = multiply(T::columns(dt, 32 * b + 16 * u, d, lane), po[u], dv[d]);
-                    dk[d] = multiply(T::columns(qt, 32 * b + 16 * u, d, lane), ds[u], dk[d]);
-                }
+        for (int i = 0; i < 2 * STEPS; ++i) {
+            if (i + kAhead < 2 * STEPS) f[(i + kAhead) % (kAhead + 1)] = rows(i + kAhead);
+            __builtin_amdgcn_sched_barrier(0);
+            if (i < STEPS) x = multiply(f[i % (kAhead + 1)], k[i], x);
+            else dp = multiply(f[i % (kAhead + 1)], v[i - STEPS], dp);
+            __builtin_amdgcn_sched_barrier(0);
         }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int r = 32 * b + result_row(i, half);
+            x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.c, -lds_lse[turn][r]));
+            dp[i] = x[i] * (dp[i] - lds_delta[turn][r]);
+        }
+        if (masked) {
+            const int behind = (int)here((uint32_t)(key - t0 - ahead - 4 * half));   // (and not without the branch)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (behind > result_row(i, 0)) x[i] = dp[i] = 0.0f;
+        }
+        Operand<DT> p[2], ds[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            float y[8], z[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = x[8 * u + i], z[i] = dp[8 * u + i];
+            p[u].set(y);
+            ds[u].set(z);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        // dv and dk in turn: block i / 4, rows 16 (i / 2 % 2) ..
+        const uint32_t columns_at = here(T::columns_lane(tiles, lane));
+        const auto columns = [&](int i) { return T::columns(columns_at, 16 * (i / 2 & 1), i / 4, i & 1 ? 0 : L::kTile); };
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) f[i] = columns(i);
+#pragma unroll
+        for (int i = 0; i < 4 * DB; ++i) {
+            if (i + kAhead < 4 * DB) f[(i + kAhead) % (kAhead + 1)] = columns(i + kAhead);
+            __builtin_amdgcn_sched_barrier(0);
+            if (i & 1) dk[i / 4] = multiply(f[i % (kAhead + 1)], ds[i / 2 & 1], dk[i / 4]);
+            else dv[i / 4] = multiply(f[i % (kAhead + 1)], p[i / 2 & 1], dv[i / 4]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    if (end > 0) {
+        start(0);
+        finish(0);
+    }
+    int now = first;
+    for (int n = 0; n < end; ++n) {
+        if (n + 1 < end) start(n + 1);
+        const int turn = n & 1, t0 = now * L::kRows;
+        if (++now == first + each) now = first;
+        if (key0 < s.nk) {
+#pragma unroll 1
+            for (int b = 0; b < NB; ++b) {
+                const int at = t0 + 32 * b;
+                if (a.causal && at + 31 + ahead < key0) continue;       // none of the tokens sees any of the keys
+                block(b, turn, at, a.causal && at + ahead < key0 + 31);
+            }
+        }
+        if (n + 1 < end) finish(n + 1);
     }
     if (key >= s.nk) return;
     const int64_t to = (key_row * a.Hk + head) * a.D * SIZE;

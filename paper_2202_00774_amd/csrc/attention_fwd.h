@@ -17,23 +17,25 @@ template <int DT, int DC, bool FEW>
 struct AttentionFwd {
     static constexpr int kWaves = 4, kThreads = 64 * kWaves;
     static constexpr int kRows = FEW ? 32 : 32 * kWaves;
-    static constexpr int kKeys = FEW ? 32 * kWaves : (DT == SDGP_BF16 ? 64 : 32);
+    static constexpr int kSplit = Tile<DT, DC>::kRow == 512 ? 2 : 4;   // FEW: wavefronts that have keys (two where LDS holds no more)
+    static constexpr int kKeys = FEW ? 32 * kSplit : (DT == SDGP_BF16 ? 64 : 32);
     static constexpr int kBlocks = FEW ? 1 : kKeys / 32;               // of 32 keys, a wavefront
-    static constexpr int kBuffers = FEW ? 1 : 2;
     using T = Tile<DT, DC>;
-    static constexpr int kTile = kKeys * T::kRow, kBuffer = 2 * kTile;
-    static constexpr int kLds = kBuffers * kBuffer;
+    static constexpr int kTile = kKeys * T::kRow, kBuffer = 2 * kTile, kLds = 2 * kBuffer;
 };
+
+// Wavefronts a SIMD, as LDS and registers allow.
+constexpr int attention_fwd_waves(int dt, int dc, bool few) { return (few || dt == SDGP_F32) && (dc > 64 || (few && dt == SDGP_F32)) ? 1 : 2; }
 
 __device__ __forceinline__ float log2_sum(float mc, float l) { return (mc + __builtin_amdgcn_logf(l)) * 0.693147180559945309f; }
 
-template <int DT, int DC, bool FEW>
-__global__ void __launch_bounds__(256, DT == SDGP_F32 && DC > 64 ? 1 : 2) attention_fwd_kernel(const Attention a) {
+template <int DT, int DC, bool FEW, bool FAST>
+__global__ void __launch_bounds__(256, attention_fwd_waves(DT, DC, FEW)) attention_fwd_kernel(const Attention a) {
     using L = AttentionFwd<DT, DC, FEW>;
     using T = typename L::T;
     constexpr int SIZE = Operand<DT>::kSize, STEPS = DC / 16, DB = DC / 32, NB = L::kBlocks;
-    __shared__ __attribute__((aligned(16))) char lds_bytes[L::kLds];
-    __shared__ float lds_ml[FEW ? 2 * 32 * L::kWaves : 1];
+    __shared__ __attribute__((aligned(512))) char lds_bytes[L::kLds];
+    __shared__ float lds_ml[FEW ? 2 * 32 * L::kSplit : 1];
     SDGP_SHARED char* lds = (SDGP_SHARED char*)lds_bytes;
 
     const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
@@ -55,7 +57,7 @@ __global__ void __launch_bounds__(256, DT == SDGP_F32 && DC > 64 ? 1 : 2) attent
     const int last = rows - 1 < row0 + L::kRows - 1 ? rows - 1 : row0 + L::kRows - 1;
     const int most = seen(last);                                        // of the workgroup
     const int most_mine = FEW ? most : seen(last < first_row + 31 ? last : first_row + 31);   // of the wavefront (rows in front of last)
-    const bool any_row = first_row < rows;
+    const bool any_row = first_row < rows && !(FEW && wave >= L::kSplit);
 
     const int t = row < rows ? (int)divide((uint32_t)row, a.by_group) : 0, g = row < rows ? row - t * a.G : 0;
     const int64_t out_row = (int64_t)(s.q0 + t) * a.H + head * a.G + g;
@@ -63,7 +65,7 @@ __global__ void __launch_bounds__(256, DT == SDGP_F32 && DC > 64 ? 1 : 2) attent
     {
         const char* p = static_cast<const char*>(a.q) + ((int64_t)(s.q0 + t) * a.q_token + (int64_t)(head * a.G + g) * a.q_head) * SIZE;
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i) q[i] = load_operand<DT>(p, 16 * i + 8 * half, row < rows ? a.D : 0);
+        for (int i = 0; i < STEPS; ++i) q[i] = load_operand<DT, FAST>(p, 16 * i + 8 * half, row < rows ? a.D : 0);
     }
     const char* keys = static_cast<const char*>(a.k) + ((int64_t)s.k0 * a.k_token + (int64_t)head * a.k_head) * SIZE;
     const char* values = static_cast<const char*>(a.v) + ((int64_t)s.k0 * a.v_token + (int64_t)head * a.v_head) * SIZE;
@@ -73,11 +75,7 @@ __global__ void __launch_bounds__(256, DT == SDGP_F32 && DC > 64 ? 1 : 2) attent
     const int all = (most + L::kKeys - 1) / L::kKeys, per = (all + a.parts - 1) / a.parts;
     const int begin = part * per < all ? part * per : all, end = begin + per < all ? begin + per : all;
 
-    Stage<DT, DC, L::kKeys, L::kThreads> sk, sv;
-    const auto fetch = [&](int n) {
-        sk.load([&](int r) { const int at = n * L::kKeys + r; return at < s.nk ? keys + at * k_row : nullptr; }, a.D);
-        sv.load([&](int r) { const int at = n * L::kKeys + r; return at < s.nk ? values + at * v_row : nullptr; }, a.D);
-    };
+    Feed<DT, DC, L::kKeys, FAST> fk(keys, k_row, a.D), fv(values, v_row, a.D);
     attn_f32x16 o[DB];
 #pragma unroll
     for (int d = 0; d < DB; ++d)
@@ -85,69 +83,80 @@ __global__ void __launch_bounds__(256, DT == SDGP_F32 && DC > 64 ? 1 : 2) attent
         for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
     float m = -INFINITY, l = 0.0f;
     const float slack = 8.0f / a.c;
-    if (begin < end) fetch(begin);
-    for (int n = begin; n < end; ++n) {
-        SDGP_SHARED char* kt = lds + (L::kBuffers == 2 ? (n & 1) * L::kBuffer : 0);
-        SDGP_SHARED char* vt = kt + L::kTile;
-        if (L::kBuffers == 1) __syncthreads();
-        sk.store(kt);
-        sv.store(vt);
+    const auto buffer = [&](int n) { return lds + (n & 1) * L::kBuffer; };
+    const auto start = [&](int n) {
+        fk.start(buffer(n), n * L::kKeys, s.nk);
+        fv.start(buffer(n) + L::kTile, n * L::kKeys, s.nk);
+    };
+    const auto finish = [&](int n) {
+        fk.finish(buffer(n));
+        fv.finish(buffer(n) + L::kTile);
         __syncthreads();
-        if (n + 1 < end) fetch(n + 1);
+    };
+    if (begin < end) {
+        start(begin);
+        finish(begin);
+    }
+    for (int n = begin; n < end; ++n) {
+        SDGP_SHARED char *kt = buffer(n), *vt = kt + L::kTile;
+        if (n + 1 < end) start(n + 1);
         const int key0 = n * L::kKeys + (FEW ? 32 * wave : 0);
-        if (key0 >= most_mine || !any_row) continue;                    // (every wavefront comes back to the barrier)
-        attn_f32x16 x[NB];
+        if (key0 < most_mine && any_row) {
+            const uint32_t k_at = T::rows_lane(kt, lane), v_at = T::columns_lane(vt, lane);
+            attn_f32x16 x[NB];
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            const int r0 = FEW ? 32 * wave : 32 * b;
+            for (int b = 0; b < NB; ++b) {
+                const int r0 = FEW ? 32 * wave : 32 * b;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[b][i] = 0.0f;
+                for (int i = 0; i < 16; ++i) x[b][i] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < STEPS; ++i) x[b] = multiply(T::rows(kt, r0, i, lane), q[i], x[b]);
-        }
-        if (key0 + 32 * NB > fewest) {                                  // some row does not see all of these
+                for (int i = 0; i < STEPS; ++i) x[b] = multiply(T::rows(k_at, r0, i), q[i], x[b]);
+            }
+            if (key0 + 32 * NB > fewest) {                                  // some row does not see all of these
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (key0 + 32 * b + result_row(i, half) >= mine) x[b][i] = -INFINITY;
+            }
+            float top = x[0][0];
 #pragma unroll
             for (int b = 0; b < NB; ++b)
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (key0 + 32 * b + result_row(i, half) >= mine) x[b][i] = -INFINITY;
-        }
-        float top = x[0][0];
+                for (int i = 0; i < 16; ++i) top = fmaxf(top, x[b][i]);
+            top = halves_max(top);
+            if (__any(top > m + slack)) {                                   // (true where m is -inf and a key is seen)
+                const float now = fmaxf(m, top);
+                const float factor = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - now) * a.c);
+                m = now;
+                l *= factor;
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+                for (int d = 0; d < DB; ++d)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, x[b][i]);
-        top = halves_max(top);
-        if (__any(top > m + slack)) {                                   // (true where m is -inf and a key is seen)
-            const float now = fmaxf(m, top);
-            const float factor = now == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - now) * a.c);
-            m = now;
-            l *= factor;
+                    for (int i = 0; i < 16; ++i) o[d][i] *= factor;
+            }
+            const float mc = m == -INFINITY ? 0.0f : m * a.c;
+            Operand<DT> p[NB][2];
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    float y[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        y[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][8 * u + i], a.c, -mc));
+                        l += y[i];
+                    }
+                    p[b][u].set(y);
+                }
 #pragma unroll
             for (int d = 0; d < DB; ++d)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) o[d][i] *= factor;
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) o[d] = multiply(T::columns(v_at, (FEW ? 32 * wave : 32 * b) + 16 * u, d), p[b][u], o[d]);
         }
-        const float mc = m == -INFINITY ? 0.0f : m * a.c;
-        Operand<DT> p[NB][2];
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                float y[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    y[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][8 * u + i], a.c, -mc));
-                    l += y[i];
-                }
-                p[b][u].set(y);
-            }
-#pragma unroll
-        for (int d = 0; d < DB; ++d)
-#pragma unroll
-            for (int b = 0; b < NB; ++b)
-#pragma unroll
-                for (int u = 0; u < 2; ++u) o[d] = multiply(T::columns(vt, (FEW ? 32 * wave : 32 * b) + 16 * u, d, lane), p[b][u], o[d]);
+        if (n + 1 < end) finish(n + 1);
     }
     l = halves_sum(l);
     float mc = m == -INFINITY ? 0.0f : m * a.c;
@@ -156,28 +165,29 @@ __global__ void __launch_bounds__(256, DT == SDGP_F32 && DC > 64 ? 1 : 2) attent
         // The wavefronts' sums over their keys, brought to one maximum and added up.
         __syncthreads();
         float* ml = lds_ml;
-        if (half == 0) ml[wave * 32 + lane] = l != 0.0f ? mc : -INFINITY;
+        if (half == 0 && any_row) ml[wave * 32 + lane] = l != 0.0f ? mc : -INFINITY;
         __syncthreads();
         float top = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < L::kWaves; ++w) top = fmaxf(top, ml[w * 32 + (lane & 31)]);
+        for (int w = 0; w < L::kSplit; ++w) top = fmaxf(top, ml[w * 32 + (lane & 31)]);
         const float factor = l != 0.0f ? __builtin_amdgcn_exp2f(mc - top) : 0.0f;
-        if (half == 0) ml[(L::kWaves + wave) * 32 + lane] = l * factor;
-        SDGP_SHARED float* sums = (SDGP_SHARED float*)lds;             // [waves, 32, DC]
+        if (half == 0 && any_row) ml[(L::kSplit + wave) * 32 + lane] = l * factor;
+        SDGP_SHARED float* sums = (SDGP_SHARED float*)lds;             // [kSplit, 32, DC]
+        if (any_row)
 #pragma unroll
-        for (int d = 0; d < DB; ++d)
+            for (int d = 0; d < DB; ++d)
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                sums[(wave * 32 + (lane & 31)) * DC + ((32 * d + result_row(i, half)) ^ (lane & 31))] = o[d][i] * factor;
+                for (int i = 0; i < 16; ++i)
+                    sums[(wave * 32 + (lane & 31)) * DC + ((32 * d + result_row(i, half)) ^ (lane & 31))] = o[d][i] * factor;
         __syncthreads();
         for (int e = threadIdx.x; e < 32 * DC; e += L::kThreads) {
             const int r = e / DC, d = e % DC, at = row0 + r;
             if (at >= rows || d >= a.D) continue;
             float sum = 0.0f, total = 0.0f, big = -INFINITY;
 #pragma unroll
-            for (int w = 0; w < L::kWaves; ++w) {
+            for (int w = 0; w < L::kSplit; ++w) {
                 sum += sums[(w * 32 + r) * DC + (d ^ r)];
-                total += ml[(L::kWaves + w) * 32 + r];
+                total += ml[(L::kSplit + w) * 32 + r];
                 big = fmaxf(big, ml[w * 32 + r]);
             }
             const int tok = (int)divide((uint32_t)at, a.by_group);
