@@ -462,7 +462,7 @@ int sdgp_attention(const void* q, const void* k, const void* v, const int64_t* s
                    const int32_t* offsets_k, const int32_t* lengths_k, int64_t sequences, void* o, float* lse, int64_t Tq,
                    int64_t Tk, int64_t H, int64_t Hk, int D, int dt, int causal, float scale, void* workspace,
                    size_t workspace_bytes, void* hip_stream);
-size_t sdgp_attention_bwd_workspace(int64_t Tq, int64_t H);
+size_t sdgp_attention_bwd_workspace(int64_t sequences, int64_t Tq, int64_t Tk, int64_t H, int64_t Hk, int D, int dt);
 int sdgp_attention_bwd(const void* dO, const void* q, const void* k, const void* v, const void* o, const float* lse,
                        const int64_t* strides, const int32_t* offsets_q, const int32_t* offsets_k, int64_t sequences, void* dq,
                        void* dk, void* dv, int64_t Tq, int64_t Tk, int64_t H, int64_t Hk, int D, int dt, int causal, float scale,

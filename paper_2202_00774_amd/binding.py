@@ -122,7 +122,7 @@ def load():
             lib.sdgp_attention.restype = i32
             lib.sdgp_attention.argtypes = [vp] * 7 + [i64, vp, vp, i64, i64, i64, i64, i32, i32, i32, f32, vp, sz, vp]
             lib.sdgp_attention_bwd_workspace.restype = sz
-            lib.sdgp_attention_bwd_workspace.argtypes = [i64, i64]
+            lib.sdgp_attention_bwd_workspace.argtypes = [i64, i64, i64, i64, i64, i32, i32]
             lib.sdgp_attention_bwd.restype = i32
             lib.sdgp_attention_bwd.argtypes = [vp] * 9 + [i64, vp, vp, vp, i64, i64, i64, i64, i32, i32, i32, f32, vp, sz, vp]
             lib.sdgp_rotary.restype = i32
@@ -823,7 +823,7 @@ def sdgp_attention_bwd(do: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: to
     for t, name in ((do, "do"), (o, "o")):
         _per_row(t, q.shape, name, (q.dtype,), q)
     _per_row(lse, q.shape[:-1], "lse", _FLOAT, q)
-    need = _need("sdgp_attention_bwd_workspace", Tq, H)
+    need = _need("sdgp_attention_bwd_workspace", S, Tq, Tk, H, Hk, D, dt)
     if need == _INVALID:
         raise SdgpError(-3, "sdgp_attention_bwd")
     workspace, wbytes = _own_workspace(need, workspace, q, "sdgp_attention_bwd_workspace")

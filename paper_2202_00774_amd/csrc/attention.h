@@ -16,17 +16,26 @@ struct Attention {
     int64_t q_token, q_head, k_token, k_head, v_token, v_head;   // strides in elements
     const int32_t *off_q, *off_k, *len_k;                        // null: S sequences of Lq and Lk tokens each
     int S, Lq, Lk, Tq, Tk, H, Hk, G, D, causal;
-    FastDiv by_group;                                            // rows / G
+    FastDiv by_group, by_heads;                                  // rows / G; a tile's rows / its heads (backward)
     float scale, c;                                              // c = scale log2 e
     bool fast;                                                   // Feed<..., FAST>
     void* o;
     float* lse;
-    int parts;                                                   // forward: pieces of a row's keys
-    float *part_o, *part_ml;                                     // [parts, Tq H, D], [parts, Tq H, 2]
+    int parts;                                                   // pieces of a row's keys (forward), of a key's rows (backward)
+    float *part_o, *part_ml;                                     // forward: [parts, Tq H, D], [parts, Tq H, 2]; backward: [parts, 2, Tk Hk, D]
     const void *d_o, *o_in;
-    float* delta;
+    float *lse2, *delta;                                         // [Tq H]: lse log2 e, and sum of dO o
     void *dq, *dk, *dv;
 };
+
+// How the gradients' kernels cut the work: wavefronts of a workgroup with rows or keys of their own, tiles of each.
+struct AttentionGrid {
+    int own_rows, own_keys;
+    int64_t row_tiles, key_tiles;
+};
+
+// Rows of queries in a tile of the keys' gradients' kernel, as LDS holds them; DC: values of a head as the kernel counts them.
+constexpr int attention_dkv_rows(int dt, int DC, int own) { return own < 4 || (dt == SDGP_BF16 && DC <= 96) ? 64 : 32; }
 
 // A key head's queries are the rows (token, head of the group), token by token: its keys are read once for all heads of
 // the group, and their gradients are sums over these rows.
@@ -276,6 +285,32 @@ __device__ __forceinline__ uint32_t here(uint32_t x) {
     return x;
 }
 
+// Buffer loads straight into LDS, lane i's bytes at `lds` + SIZE i; offsets from kNoRecord on give zeros.  The compiler does not count
+// them: nothing that it waits for may be on its way beside them, or its wait is for them too.
+constexpr uint32_t kNoRecord = 0x7FFFFFF0u;
+
+__device__ __forceinline__ attn_u32x4 records(const void* base, uint32_t bytes) {
+    const uint64_t at = (uint64_t)(uintptr_t)base;
+    attn_u32x4 v;
+    v[0] = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)at);
+    v[1] = (uint32_t)__builtin_amdgcn_readfirstlane((int)((uint32_t)(at >> 32) & 0xFFFFu));
+    v[2] = (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes);
+    v[3] = 0x00027000u;
+    return v;
+}
+template <int SIZE>
+__device__ __forceinline__ void copy_to_lds(attn_u32x4 from, uint32_t offset, uint32_t lds) {
+    static_assert(SIZE == 16 || SIZE == 4, "bytes a lane");
+    if constexpr (SIZE == 16) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(from) : "memory");
+    else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(from) : "memory");
+}
+__device__ __forceinline__ void wait_for_copies() { __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8)); }   // vmcnt 0
+
+// Where this wavefront's part of each 4096 bytes that 256 threads copy goes.
+__device__ __forceinline__ uint32_t wave_part(SDGP_SHARED char* tile) {
+    return (uint32_t)__builtin_amdgcn_readfirstlane((int)((uint32_t)(uintptr_t)tile + (threadIdx.x / 64 << 10)));
+}
+
 // Brings rows of a tensor into a tile while the one before it is worked on: `start` asks for them, `finish` comes before the
 // barrier behind which they are read.  256 threads; ROWS rows of up to DC values, zeros behind the tensor's last row.
 //
@@ -291,7 +326,6 @@ struct Feed<DT, DC, ROWS, true> {
     static constexpr int kStep = 256 / T::kChunks;                      // rows between them
     static constexpr int kPlaces = kStep % 16 == 0 ? 1 : 2;             // `place` tells sixteen rows apart
     static_assert(kEach * 256 == ROWS * T::kChunks && kStep * kPlaces % 16 == 0, "whole instructions");
-    static constexpr uint32_t kNone = 0x7FFFFFF0u;                      // behind every record
     const char* base;
     int64_t row;
     int width;
@@ -301,29 +335,21 @@ struct Feed<DT, DC, ROWS, true> {
 #pragma unroll
         for (int i = 0; i < kPlaces; ++i) {
             const int r = (int)threadIdx.x / T::kChunks + i * kStep, chunk = ((int)threadIdx.x % T::kChunks) ^ T::place(r);
-            first[i] = chunk * 16 < width ? (uint32_t)(r * (int)row_bytes + chunk * 16) : kNone;
+            first[i] = chunk * 16 < width ? (uint32_t)(r * (int)row_bytes + chunk * 16) : kNoRecord;
         }
     }
     // rows r0 .. r0 + ROWS - 1 of `rows`
     __device__ __forceinline__ void start(SDGP_SHARED char* tile, int r0, int rows) {
-        const uint64_t at = (uint64_t)(uintptr_t)(base + r0 * row);
         const int64_t left = (int64_t)(rows - r0 - 1) * row + width;
-        const int records = rows <= r0 ? 0 : left < 0x7FFFFFF0 ? (int)left : 0x7FFFFFF0;
-        attn_u32x4 v;
-        v[0] = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)at);
-        v[1] = (uint32_t)__builtin_amdgcn_readfirstlane((int)((uint32_t)(at >> 32) & 0xFFFFu));
-        v[2] = (uint32_t)__builtin_amdgcn_readfirstlane(records);
-        v[3] = 0x00027000u;
-        const uint32_t to = (uint32_t)(uintptr_t)tile + ((uint32_t)__builtin_amdgcn_readfirstlane((int)threadIdx.x / 64) << 10);
-        const uint32_t lds = (uint32_t)__builtin_amdgcn_readfirstlane((int)to);
+        const attn_u32x4 from = records(base + r0 * row, rows <= r0 ? 0 : left < kNoRecord ? (uint32_t)left : kNoRecord);
+        const uint32_t lds = wave_part(tile);
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            const uint32_t from = first[i % kPlaces];
-            const uint32_t offset = from == kNone ? from : from + (uint32_t)(i / kPlaces * kPlaces * kStep) * (uint32_t)row;
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds + i * 4096), "v"(offset), "s"(v) : "memory");
+            const uint32_t at = first[i % kPlaces];
+            copy_to_lds<16>(from, at == kNoRecord ? at : at + (uint32_t)(i / kPlaces * kPlaces * kStep) * (uint32_t)row, lds + i * 4096);
         }
     }
-    __device__ __forceinline__ void finish(SDGP_SHARED char*) { __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8)); }   // vmcnt 0
+    __device__ __forceinline__ void finish(SDGP_SHARED char*) { wait_for_copies(); }
 };
 
 template <int DT, int DC, int ROWS>
@@ -354,13 +380,75 @@ struct Feed<DT, DC, ROWS, false> {
     }
 };
 
+// The same of queries: a tile is `tokens` tokens times `heads` heads of a group, head by head (as many as its rows hold).
+template <int DT, int DC, int ROWS, bool FAST>
+struct FeedQueries {
+    using T = Tile<DT, DC>;
+    static constexpr int kNeed = DC * Operand<DT>::kSize / 16, kEach = ROWS * T::kChunks / 256, kStep = 256 / T::kChunks;
+    attn_u32x4 held[FAST ? 1 : kEach];
+    const char* base;                                                   // of the tile that is asked for next
+    int64_t row, head;
+    int D;
+
+    __device__ __forceinline__ FeedQueries(const char* tensor, int64_t token_bytes, int64_t head_bytes, int width)
+        : base(tensor), row(token_bytes), head(head_bytes), D(width) {}
+    // `tokens` and `heads` of those are there
+    __device__ __forceinline__ void start(SDGP_SHARED char* tile, FastDiv by_heads, int per, int tokens, int heads) {
+        const int r0 = (int)threadIdx.x / T::kChunks, at = (int)threadIdx.x % T::kChunks;
+        if constexpr (FAST) {
+            const attn_u32x4 from = records(base, kNoRecord);
+            const uint32_t lds = wave_part(tile);
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const int r = r0 + i * kStep, chunk = at ^ T::place(r), t = (int)divide((uint32_t)r, by_heads), g = r - t * per;
+                const bool there = t < tokens && g < heads && chunk * 16 < D * Operand<DT>::kSize;
+                copy_to_lds<16>(from, there ? (uint32_t)t * (uint32_t)row + (uint32_t)g * (uint32_t)head + (uint32_t)chunk * 16u : kNoRecord, lds + i * 4096);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const int r = r0 + i * kStep, t = (int)divide((uint32_t)r, by_heads), g = r - t * per;
+                held[i] = attn_u32x4{0, 0, 0, 0};
+                if (at < kNeed && t < tokens && g < heads) held[i] = load_chunk<DT>(base + t * row + g * head, at * (16 / Operand<DT>::kSize), D);
+            }
+        }
+    }
+    __device__ __forceinline__ void finish(SDGP_SHARED char* tile) const {
+        if constexpr (FAST) {
+            wait_for_copies();
+        } else {
+            const int r0 = (int)threadIdx.x / T::kChunks, at = (int)threadIdx.x % T::kChunks;
+#pragma unroll
+            for (int i = 0; i < kEach; ++i)
+                if (at < kNeed) *(SDGP_SHARED attn_u32x4*)(tile + T::at(r0 + i * kStep, at)) = held[i];
+        }
+    }
+};
+
 // The larger and the sum of a lane's value and that of the lane 32 away.
 __device__ __forceinline__ float halves_max(float x) { return fmaxf(x, __shfl_xor(x, 32)); }
 __device__ __forceinline__ float halves_sum(float x) { return x + __shfl_xor(x, 32); }
 
 // Stores a 32-column block of results, transposed: lane % 32 is a row of memory, the result's rows its values.
-template <int DT>
+// FAST: D is a whole number of chunks, rows on sixteen bytes.
+template <int DT, bool FAST = false>
 __device__ __forceinline__ void store_block(char* row, const attn_f32x16& x, int block, int half, int D, float factor) {
+    if constexpr (FAST) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int e = 32 * block + 8 * g + 4 * half;
+            if (e >= D) break;
+            const float y[4] = {x[4 * g] * factor, x[4 * g + 1] * factor, x[4 * g + 2] * factor, x[4 * g + 3] * factor};
+            if constexpr (DT == SDGP_BF16) {
+                typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+                *reinterpret_cast<u32x2*>(row + e * 2) = u32x2{float2_to_bf16x2(y[0], y[1]), float2_to_bf16x2(y[2], y[3])};
+            } else {
+                typedef float f32x4 __attribute__((ext_vector_type(4)));
+                *reinterpret_cast<f32x4*>(row + e * 4) = f32x4{y[0], y[1], y[2], y[3]};
+            }
+        }
+        return;
+    }
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
         const int e = 32 * block + 8 * g + 4 * half;

@@ -13,7 +13,7 @@ namespace sdgp {
 template <int DT>
 int attention_fwd_launch(const Attention& a, int64_t tiles, bool few, hipStream_t stream);
 template <int DT>
-int attention_bwd_launch(const Attention& a, int64_t row_tiles, int64_t key_tiles, hipStream_t stream);
+int attention_bwd_launch(Attention a, const AttentionGrid& g, hipStream_t stream);
 
 namespace {
 
@@ -35,6 +35,23 @@ Split choose(int64_t S, int64_t Tq, int64_t Tk, int64_t H, int64_t Hk) {
     return s;
 }
 
+struct BwdSplit {
+    int own_rows, own_keys, parts;
+};
+
+BwdSplit choose_bwd(int64_t S, int64_t Tq, int64_t Tk, int64_t H, int64_t Hk) {
+    const int64_t n = S > 0 ? S : 1, tokens = (Tq + n - 1) / n, rows = tokens * (H / Hk), keys = (Tk + n - 1) / n;
+    const auto groups = [&](int64_t length, int64_t unit) { return n * ((length + unit - 1) / unit) * Hk; };
+    BwdSplit s;
+    s.own_rows = groups(rows, 128) >= 512 ? 4 : 2;
+    s.own_keys = groups(keys, 128) >= 512 ? 4 : 2;
+    const int64_t have = groups(keys, 32 * s.own_keys), rounds = (tokens + 63) / 64 * (H / Hk);
+    int64_t parts = have > 0 ? 256 / have : 1;
+    parts = parts > rounds / 4 ? rounds / 4 : parts;
+    s.parts = (int)(parts < 1 ? 1 : parts > 16 ? 16 : parts);
+    return s;
+}
+
 Attention arguments(const AttentionCall& c) {
     Attention a = {};
     a.q = c.q, a.k = c.k, a.v = c.v;
@@ -51,7 +68,7 @@ Attention arguments(const AttentionCall& c) {
     a.fast = true;
     for (int i = 0; i < 6; ++i) {
         all |= (uintptr_t)(c.strides[i] * size);
-        if (i % 2 == 0 && (c.strides[i] < c.D || c.strides[i] * size >= 1 << 23)) a.fast = false;
+        if (c.strides[i] * size >= 1 << 23 || (i % 2 == 0 && c.strides[i] < c.D)) a.fast = false;
     }
     a.fast = a.fast && (all & 15u) == 0 && c.H * c.D * size < 1 << 23;
     return a;
@@ -64,10 +81,17 @@ size_t attention_workspace(int64_t S, int64_t Tq, int64_t Tk, int64_t H, int64_t
     return s.parts == 1 ? 0 : (size_t)s.parts * (size_t)(Tq * H) * (size_t)(D + 2) * sizeof(float);
 }
 
+size_t attention_bwd_workspace(int64_t S, int64_t Tq, int64_t Tk, int64_t H, int64_t Hk, int D) {
+    const BwdSplit s = choose_bwd(S, Tq, Tk, H, Hk);
+    const size_t rows = 2 * (size_t)((Tq * H + 3) / 4 * 4);
+    return (rows + (s.parts == 1 ? 0 : (size_t)s.parts * 2 * (size_t)(Tk * Hk) * (size_t)D)) * sizeof(float);
+}
+
 int attention_launch(const AttentionCall& c, void* o, float* lse, void* workspace, hipStream_t stream) {
     Attention a = arguments(c);
     const Split s = choose(c.S, c.Tq, c.Tk, c.H, c.Hk);
     a.o = o, a.lse = lse, a.parts = s.parts;
+    a.fast = a.fast && (reinterpret_cast<uintptr_t>(o) & 15u) == 0;
     a.part_o = static_cast<float*>(workspace);
     a.part_ml = a.part_o + (s.parts == 1 ? 0 : (int64_t)s.parts * c.Tq * c.H * c.D);
     const int64_t tiles = most_tiles(c.offsets_q != nullptr, c.S, c.Tq, a.Lq, a.G, s.few ? 32 : 128);
@@ -79,14 +103,21 @@ int attention_bwd_launch_all(const AttentionCall& c, const void* d_o, const void
                              void* workspace, hipStream_t stream) {
     Attention a = arguments(c);
     a.d_o = d_o, a.o_in = o, a.lse = const_cast<float*>(lse), a.dq = dq, a.dk = dk, a.dv = dv;
-    a.delta = static_cast<float*>(workspace);
-    a.fast = a.fast && (reinterpret_cast<uintptr_t>(d_o) & 15u) == 0;
+    a.lse2 = static_cast<float*>(workspace);
+    a.delta = a.lse2 + (c.Tq * c.H + 3) / 4 * 4;
+    for (const void* p : {d_o, o, (const void*)dq, (const void*)dk, (const void*)dv}) a.fast = a.fast && (reinterpret_cast<uintptr_t>(p) & 15u) == 0;
     const bool packed = c.offsets_q != nullptr;
-    const int64_t row_tiles = c.Tq == 0 ? 0 : most_tiles(packed, c.S, c.Tq, a.Lq, a.G, 128);
-    const int64_t key_tiles = c.Tk == 0 ? 0 : most_tiles(packed, c.S, c.Tk, a.Lk, 1, 128);
-    if (row_tiles * a.Hk > 0x7FFFFFFF || key_tiles * a.Hk > 0x7FFFFFFF) return SDGP_ERR_SHAPE;
-    return c.dt == SDGP_BF16 ? attention_bwd_launch<SDGP_BF16>(a, row_tiles, key_tiles, stream)
-                             : attention_bwd_launch<SDGP_F32>(a, row_tiles, key_tiles, stream);
+    const BwdSplit s = choose_bwd(c.S, c.Tq, c.Tk, c.H, c.Hk);
+    a.parts = s.parts;
+    a.part_o = a.delta + (c.Tq * c.H + 3) / 4 * 4;
+    const int rows = attention_dkv_rows(c.dt, a.fast ? (c.D <= 64 ? 64 : c.D <= 96 ? 96 : 128) : 128, s.own_keys);
+    a.by_heads = fast_div((uint32_t)(a.G < rows ? a.G : rows));
+    AttentionGrid g;
+    g.own_rows = s.own_rows, g.own_keys = s.own_keys;
+    g.row_tiles = c.Tq == 0 ? 0 : most_tiles(packed, c.S, c.Tq, a.Lq, a.G, 32 * s.own_rows);
+    g.key_tiles = c.Tk == 0 ? 0 : most_tiles(packed, c.S, c.Tk, a.Lk, 1, 32 * s.own_keys);
+    if (g.row_tiles * a.Hk > 0x7FFFFFFF || g.key_tiles * a.Hk * a.parts > 0x7FFFFFFF) return SDGP_ERR_SHAPE;
+    return c.dt == SDGP_BF16 ? attention_bwd_launch<SDGP_BF16>(a, g, stream) : attention_bwd_launch<SDGP_F32>(a, g, stream);
 }
 
 }  // namespace sdgp

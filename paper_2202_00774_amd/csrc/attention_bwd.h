@@ -15,16 +15,39 @@ namespace sdgp {
 
 constexpr float kLog2E = 1.44269504088896341f;
 
-template <int DT, int DC>
+// Four wavefronts, OWN of them with 32 owned rows (or keys) each; the others share those and take every second block of what
+// passes by, their sums being added at the end: twice the workgroups, for problems of few.
+template <int DT, int DC, int OWN>
 struct AttentionDq {
-    static constexpr int kThreads = 256, kRows = 128, kKeys = DT == SDGP_BF16 ? 64 : 32, kBlocks = kKeys / 32;
+    static constexpr int kRows = 32 * OWN, kShare = 4 / OWN, kKeys = DT == SDGP_BF16 || kShare > 1 ? 64 : 32, kBlocks = kKeys / 32;
     using T = Tile<DT, DC>;
     static constexpr int kTile = kKeys * T::kRow, kBuffer = 2 * kTile, kLds = 2 * kBuffer;
 };
 
-template <int DT, int DC, bool FAST>
+// Adds the sums of wavefronts OWN .. 3 to those of the ones that own the same rows.  All threads call it, and LDS is free.
+template <int OWN, int N>
+__device__ __forceinline__ void add_shared(SDGP_SHARED char* lds, int wave, int lane, attn_f32x16 (&x)[N]) {
+    if constexpr (OWN == 4) return;
+    SDGP_SHARED float* sums = (SDGP_SHARED float*)lds;                  // [OWN, N, 16, 64]
+    __syncthreads();
+    if (wave >= OWN) {
+#pragma unroll
+        for (int d = 0; d < N; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sums[(((wave - OWN) * N + d) * 16 + i) * 64 + lane] = x[d][i];
+    }
+    __syncthreads();
+    if (wave < OWN) {
+#pragma unroll
+        for (int d = 0; d < N; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[d][i] += sums[((wave * N + d) * 16 + i) * 64 + lane];
+    }
+}
+
+template <int DT, int DC, bool FAST, int OWN>
 __global__ void __launch_bounds__(256, DT == SDGP_BF16 ? 2 : 1) attention_dq_kernel(const Attention a) {
-    using L = AttentionDq<DT, DC>;
+    using L = AttentionDq<DT, DC, OWN>;
     using T = typename L::T;
     constexpr int SIZE = Operand<DT>::kSize, STEPS = DC / 16, DB = DC / 32;
     __shared__ __attribute__((aligned(512))) char lds_bytes[L::kLds];
@@ -37,7 +60,7 @@ __global__ void __launch_bounds__(256, DT == SDGP_BF16 ? 2 : 1) attention_dq_ker
     if (!find_tile<false, L::kRows>(a, blockIdx.x / a.Hk, s, tile, tiles)) return;
     tile = tiles - 1 - tile;
     const int row0 = tile * L::kRows, rows = s.nq * a.G;
-    const int first_row = row0 + 32 * wave, row = first_row + (lane & 31);
+    const int own = wave % OWN, first_row = row0 + 32 * own, row = first_row + (lane & 31);
     const auto seen = [&](int r) {
         if (r >= rows) return 0;
         return a.causal ? clamp_int((int)divide((uint32_t)r, a.by_group) + 1 + s.nk - s.nq, 0, s.nk) : s.nk;
@@ -67,7 +90,7 @@ __global__ void __launch_bounds__(256, DT == SDGP_BF16 ? 2 : 1) attention_dq_ker
     }
     delta = halves_sum(delta);
     const float lse2 = row < rows ? a.lse[out_row] * kLog2E : 0.0f;
-    if (row < rows && half == 0) a.delta[out_row] = delta;
+    if (row < rows && half == 0 && wave == own) a.delta[out_row] = delta, a.lse2[out_row] = lse2;
 
     const char* keys = static_cast<const char*>(a.k) + ((int64_t)s.k0 * a.k_token + (int64_t)head * a.k_head) * SIZE;
     const char* values = static_cast<const char*>(a.v) + ((int64_t)s.k0 * a.v_token + (int64_t)head * a.v_head) * SIZE;
@@ -101,7 +124,7 @@ __global__ void __launch_bounds__(256, DT == SDGP_BF16 ? 2 : 1) attention_dq_ker
 #pragma unroll
         for (int b = 0; b < L::kBlocks; ++b) {
             const int key0 = n * L::kKeys + 32 * b;
-            if (key0 >= most_mine || !any_row) continue;
+            if (key0 >= most_mine || !any_row || (L::kShare > 1 && (b & 1) != wave / OWN)) continue;
             attn_f32x16 x, dp;
 #pragma unroll
             for (int i = 0; i < 16; ++i) x[i] = dp[i] = 0.0f;
@@ -131,79 +154,91 @@ __global__ void __launch_bounds__(256, DT == SDGP_BF16 ? 2 : 1) attention_dq_ker
         }
         if (n + 1 < end) finish(n + 1);
     }
-    if (row >= rows) return;
+    add_shared<OWN>(lds, wave, lane, dq);
+    if (row >= rows || wave != own) return;
 #pragma unroll
-    for (int d = 0; d < DB; ++d) store_block<DT>(static_cast<char*>(a.dq) + out_row * a.D * SIZE, dq[d], d, half, a.D, a.scale);
+    for (int d = 0; d < DB; ++d) store_block<DT, FAST>(static_cast<char*>(a.dq) + out_row * a.D * SIZE, dq[d], d, half, a.D, a.scale);
 }
 
-// The queries pass by in tiles of kRows tokens of one head; a group's heads one after the other.
-template <int DT, int DC>
+// The queries pass by in tiles of some tokens of all the group's heads, the sequence's last tokens first: so workgroups that started
+// together read the same tiles at the same time, whichever their keys are.  (Tiles of one head: 1255 us instead of %s for 22294 packed
+// tokens of 16 heads.  Their rows are 4096 bytes apart in dO, where memory's channels repeat.)
+template <int DT, int DC, int OWN>
 struct AttentionDkv {
-    static constexpr int kThreads = 256, kKeys = 128, kRows = DT == SDGP_BF16 ? 64 : 32, kBlocks = kRows / 32;
+    // Of bf16 heads of 128, the sums fill half the registers of two wavefronts a SIMD and the keys' operands an eighth; the values'
+    // come from LDS, since what does not fit is kept in memory, whose loads wait for the tiles on their way.
+    static constexpr bool kValuesInLds = DT == SDGP_BF16 && DC > 96;
+    static constexpr int kKeys = 32 * OWN, kShare = 4 / OWN, kRows = attention_dkv_rows(DT, DC, OWN), kBlocks = kRows / 32;
     using T = Tile<DT, DC>;
-    static constexpr int kTile = kRows * T::kRow, kBuffer = 2 * kTile, kLds = 2 * kBuffer;
+    static constexpr int kTile = kRows * T::kRow, kBuffer = 2 * kTile, kValues = 2 * kBuffer, kLds = kValues + (kValuesInLds ? kKeys * T::kRow : 0);
 };
 
-template <int DT, int DC, bool FAST>
+template <int DT, int DC, bool FAST, int OWN>
 __global__ void __launch_bounds__(256, DT == SDGP_BF16 ? 2 : 1) attention_dkv_kernel(const Attention a) {
-    using L = AttentionDkv<DT, DC>;
+    using L = AttentionDkv<DT, DC, OWN>;
     using T = typename L::T;
     constexpr int SIZE = Operand<DT>::kSize, STEPS = DC / 16, DB = DC / 32, NB = L::kBlocks;
     __shared__ __attribute__((aligned(512))) char lds_bytes[L::kLds];
-    __shared__ __attribute__((aligned(16))) float lds_lse[2][L::kRows], lds_delta[2][L::kRows];
+    __shared__ __attribute__((aligned(16))) float lds_rows[2][2][64];     // lse2 and delta of a tile's rows
+    __shared__ __attribute__((aligned(16))) int lds_token[L::kRows];      // a row's token in its tile
     SDGP_SHARED char* lds = (SDGP_SHARED char*)lds_bytes;
 
     const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
-    const int head = blockIdx.x % a.Hk;
+    const int head = blockIdx.x % a.Hk, rest = blockIdx.x / a.Hk, part = rest % a.parts;
     Sequence s;
     int tile, tiles;
-    if (!find_tile<true, L::kKeys>(a, blockIdx.x / a.Hk, s, tile, tiles)) return;   // the first keys have the most rows
-    const int key0 = tile * L::kKeys + 32 * wave, key = key0 + (lane & 31);
+    if (!find_tile<true, L::kKeys>(a, rest / a.parts, s, tile, tiles)) return;      // the first keys have the most rows
+    const int own = wave % OWN, key0 = tile * L::kKeys + 32 * own, key = key0 + (lane & 31);
     const int ahead = s.nk - s.nq;                                      // token t sees the keys up to t + ahead, if causal
     const int width = key < s.nk ? a.D : 0;
     const int64_t key_row = s.k0 + (key < s.nk ? key : 0);
-    Operand<DT> k[STEPS], v[STEPS];
+    Operand<DT> k[STEPS], v[L::kValuesInLds ? 1 : STEPS];
     {
         const char* pk = static_cast<const char*>(a.k) + (key_row * a.k_token + (int64_t)head * a.k_head) * SIZE;
         const char* pv = static_cast<const char*>(a.v) + (key_row * a.v_token + (int64_t)head * a.v_head) * SIZE;
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) {
             k[i] = load_operand<DT, FAST>(pk, 16 * i + 8 * half, width);
-            v[i] = load_operand<DT, FAST>(pv, 16 * i + 8 * half, width);
-        }
-    }
-    // The first token that sees this tile's first key, and the tiles of tokens from there on, of each head.
-    const int from = a.causal ? clamp_int(tile * L::kKeys - ahead, 0, s.nq) : 0;
-    const int first = from / L::kRows, each = s.nk > 0 ? (s.nq + L::kRows - 1) / L::kRows - first : 0, end = each * a.G;
-
-    const int64_t q_row = a.q_token * SIZE, d_row = (int64_t)a.H * a.D * SIZE;
-    const char* queries = static_cast<const char*>(a.q) + ((int64_t)s.q0 * a.q_token + (int64_t)head * a.G * a.q_head) * SIZE;
-    const char* grads = static_cast<const char*>(a.d_o) + ((int64_t)s.q0 * a.H + head * a.G) * a.D * SIZE;
-    Feed<DT, DC, L::kRows, FAST> fq(queries, q_row, a.D), fd(grads, d_row, a.D);
-    float next_lse = 0.0f, next_delta = 0.0f;
-    int next = first, g = 0;                                            // the tile that is asked for next, and its head
-    const auto buffer = [&](int n) { return lds + (n & 1) * L::kBuffer; };
-    const auto start = [&](int n) {
-        fq.start(buffer(n), next * L::kRows, s.nq);
-        fd.start(buffer(n) + L::kTile, next * L::kRows, s.nq);
-        if ((int)threadIdx.x < L::kRows) {
-            const int t = next * L::kRows + (int)threadIdx.x;
-            next_lse = next_delta = 0.0f;                               // tokens behind the last: zeros throughout
-            if (t < s.nq) {
-                const int64_t at = (int64_t)(s.q0 + t) * a.H + head * a.G + g;
-                next_lse = a.lse[at] * kLog2E, next_delta = a.delta[at];
+            const Operand<DT> x = load_operand<DT, FAST>(pv, 16 * i + 8 * half, width);
+            if constexpr (L::kValuesInLds) {
+                if (wave == own) *(SDGP_SHARED attn_u32x4*)(lds + L::kValues + T::at(32 * own + (lane & 31), 2 * i + half)) = __builtin_bit_cast(attn_u32x4, x);
+            } else {
+                v[i] = x;
             }
         }
-        if (++next == first + each) {
-            next = first, ++g;
-            fq.base += a.q_head * SIZE;
-            fd.base += a.D * SIZE;
+    }
+    // A tile's tokens and heads, the first token that sees this tile's first key, and the tiles of tokens from there on.
+    const int heads = a.G < L::kRows ? a.G : L::kRows, tokens = L::kRows / heads, chunks = (a.G + heads - 1) / heads;
+    const int from = a.causal ? clamp_int(tile * L::kKeys - ahead, 0, s.nq) : 0;
+    const int first = from / tokens, each = s.nk > 0 ? (s.nq + tokens - 1) / tokens - first : 0, all = (each > 0 ? each : 0) * chunks;
+    const int per = (all + a.parts - 1) / a.parts, begin = part * per < all ? part * per : all, end = begin + per < all ? begin + per : all;
+
+    const char* queries = static_cast<const char*>(a.q) + ((int64_t)s.q0 * a.q_token + (int64_t)head * a.G * a.q_head) * SIZE;
+    const char* grads = static_cast<const char*>(a.d_o) + ((int64_t)s.q0 * a.H + head * a.G) * a.D * SIZE;
+    FeedQueries<DT, DC, L::kRows, FAST> fq(queries, a.q_token * SIZE, a.q_head * SIZE, a.D), fd(grads, (int64_t)a.H * a.D * SIZE, (int64_t)a.D * SIZE, a.D);
+    int chunk = begin % chunks, next = first + each - 1 - begin / chunks;   // the heads and tile that are asked for next
+    int now_chunk = chunk, now = next;                                  // .. that are worked on
+    if ((int)threadIdx.x < L::kRows) lds_token[threadIdx.x] = (int)divide(threadIdx.x, a.by_heads);
+    const auto buffer = [&](int n) { return lds + (n & 1) * L::kBuffer; };
+    const auto start = [&](int n) {
+        const int t0 = next * tokens, g0 = chunk * heads, has = s.nq - t0, wide = a.G - g0 < heads ? a.G - g0 : heads;
+        const int lasting = has < tokens ? has : tokens;
+        fq.base = queries + (t0 * fq.row + g0 * fq.head);
+        fd.base = grads + (t0 * fd.row + g0 * fd.head);
+        fq.start(buffer(n), a.by_heads, heads, lasting, wide);
+        fd.start(buffer(n) + L::kTile, a.by_heads, heads, lasting, wide);
+        if (wave < 2) {                                                 // (one wavefront each; rows that are not there: zeros throughout)
+            const int t = (int)divide((uint32_t)lane, a.by_heads), g = lane - t * heads;
+            const float* of = (wave == 0 ? a.lse2 : a.delta) + ((int64_t)(s.q0 + t0) * a.H + head * a.G + g0);
+            copy_to_lds<4>(records(of, kNoRecord), lane < L::kRows && t < lasting && g < wide ? (uint32_t)(t * a.H + g) * 4u : kNoRecord,
+                           (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(SDGP_SHARED float*)lds_rows[n & 1][wave]));
         }
+        if (++chunk == chunks) chunk = 0, --next;
     };
     const auto finish = [&](int n) {
         fq.finish(buffer(n));
         fd.finish(buffer(n) + L::kTile);
-        if ((int)threadIdx.x < L::kRows) lds_lse[n & 1][threadIdx.x] = next_lse, lds_delta[n & 1][threadIdx.x] = next_delta;
+        wait_for_copies();
         __syncthreads();
     };
     attn_f32x16 dk[DB], dv[DB];
@@ -214,35 +249,40 @@ __global__ void __launch_bounds__(256, DT == SDGP_BF16 ? 2 : 1) attention_dkv_ke
     // One block of 32 tokens.  Operands from LDS are asked for kAhead products before they are needed, and no earlier: the keys'
     // operands and sums fill three quarters of the registers of two wavefronts a SIMD, which cover each other's other work.
     const auto block = [&](int b, int turn, int t0, bool masked) __attribute__((always_inline)) {
-        constexpr int kAhead = 2;
+        constexpr int kAhead = L::kValuesInLds ? 2 : 3, kAheadOut = 4;
         SDGP_SHARED char* tiles = lds + turn * L::kBuffer + b * 32 * T::kRow;    // of queries, and kTile on of gradients
         Operand<DT> f[kAhead + 1];
         attn_f32x16 x, dp;
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[i] = dp[i] = 0.0f;
         const uint32_t rows_at = here(T::rows_lane(tiles, lane));
+        Operand<DT> fv[kAhead + 1];
+        const uint32_t values_at = L::kValuesInLds ? here(T::rows_lane(lds + L::kValues + own * 32 * T::kRow, lane)) : 0;
         const auto rows = [&](int i) { return i < STEPS ? T::rows(rows_at, 0, i) : T::rows(rows_at, 0, i - STEPS, L::kTile); };
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) f[i] = rows(i);
 #pragma unroll
         for (int i = 0; i < 2 * STEPS; ++i) {
             if (i + kAhead < 2 * STEPS) f[(i + kAhead) % (kAhead + 1)] = rows(i + kAhead);
+            if (L::kValuesInLds && i + kAhead >= STEPS && i + kAhead < 2 * STEPS)
+                fv[(i + kAhead - STEPS) % (kAhead + 1)] = T::rows(values_at, 0, i + kAhead - STEPS);
             __builtin_amdgcn_sched_barrier(0);
             if (i < STEPS) x = multiply(f[i % (kAhead + 1)], k[i], x);
+            else if constexpr (L::kValuesInLds) dp = multiply(f[i % (kAhead + 1)], fv[(i - STEPS) % (kAhead + 1)], dp);
             else dp = multiply(f[i % (kAhead + 1)], v[i - STEPS], dp);
             __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             const int r = 32 * b + result_row(i, half);
-            x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.c, -lds_lse[turn][r]));
-            dp[i] = x[i] * (dp[i] - lds_delta[turn][r]);
+            x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.c, -lds_rows[turn][0][r]));
+            dp[i] = x[i] * (dp[i] - lds_rows[turn][1][r]);
         }
         if (masked) {
-            const int behind = (int)here((uint32_t)(key - t0 - ahead - 4 * half));   // (and not without the branch)
+            const int mine = (int)here((uint32_t)(key - t0 - ahead));   // (and not without the branch)
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-                if (behind > result_row(i, 0)) x[i] = dp[i] = 0.0f;
+                if (mine > lds_token[32 * b + result_row(i, half)]) x[i] = dp[i] = 0.0f;
         }
         Operand<DT> p[2], ds[2];
 #pragma unroll
@@ -255,44 +295,72 @@ __global__ void __launch_bounds__(256, DT == SDGP_BF16 ? 2 : 1) attention_dkv_ke
         }
         __builtin_amdgcn_sched_barrier(0);
         // dv and dk in turn: block i / 4, rows 16 (i / 2 % 2) ..
+        Operand<DT> h[kAheadOut + 1];
         const uint32_t columns_at = here(T::columns_lane(tiles, lane));
         const auto columns = [&](int i) { return T::columns(columns_at, 16 * (i / 2 & 1), i / 4, i & 1 ? 0 : L::kTile); };
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) f[i] = columns(i);
+        for (int i = 0; i < kAheadOut; ++i) h[i] = columns(i);
 #pragma unroll
         for (int i = 0; i < 4 * DB; ++i) {
-            if (i + kAhead < 4 * DB) f[(i + kAhead) % (kAhead + 1)] = columns(i + kAhead);
+            if (i + kAheadOut < 4 * DB) h[(i + kAheadOut) % (kAheadOut + 1)] = columns(i + kAheadOut);
             __builtin_amdgcn_sched_barrier(0);
-            if (i & 1) dk[i / 4] = multiply(f[i % (kAhead + 1)], ds[i / 2 & 1], dk[i / 4]);
-            else dv[i / 4] = multiply(f[i % (kAhead + 1)], p[i / 2 & 1], dv[i / 4]);
+            if (i & 1) dk[i / 4] = multiply(h[i % (kAheadOut + 1)], ds[i / 2 & 1], dk[i / 4]);
+            else dv[i / 4] = multiply(h[i % (kAheadOut + 1)], p[i / 2 & 1], dv[i / 4]);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    if (end > 0) {
-        start(0);
-        finish(0);
+    if (begin < end) {
+        start(begin);
+        finish(begin);
     }
-    int now = first;
-    for (int n = 0; n < end; ++n) {
+    for (int n = begin; n < end; ++n) {
         if (n + 1 < end) start(n + 1);
-        const int turn = n & 1, t0 = now * L::kRows;
-        if (++now == first + each) now = first;
+        const int turn = n & 1, t0 = now * tokens;
+        if (++now_chunk == chunks) now_chunk = 0, --now;
         if (key0 < s.nk) {
 #pragma unroll 1
             for (int b = 0; b < NB; ++b) {
-                const int at = t0 + 32 * b;
-                if (a.causal && at + 31 + ahead < key0) continue;       // none of the tokens sees any of the keys
-                block(b, turn, at, a.causal && at + ahead < key0 + 31);
+                if (L::kShare > 1 && (b & 1) != wave / OWN) continue;   // another wavefront's
+                // the last key that the block's first and last rows see
+                const int low = t0 + (int)divide((uint32_t)(32 * b), a.by_heads) + ahead, high = t0 + (int)divide((uint32_t)(32 * b + 31), a.by_heads) + ahead;
+                if (a.causal && high < key0) continue;
+                block(b, turn, t0, a.causal && low < key0 + 31);
             }
         }
         if (n + 1 < end) finish(n + 1);
     }
-    if (key >= s.nk) return;
-    const int64_t to = (key_row * a.Hk + head) * a.D * SIZE;
+    add_shared<OWN>(lds, wave, lane, dk);
+    add_shared<OWN>(lds, wave, lane, dv);
+    if (key >= s.nk || wave != own) return;
+    const int64_t to = (key_row * a.Hk + head) * a.D;
+    if (a.parts > 1) {
+        float* pk = a.part_o + (int64_t)part * 2 * a.Tk * a.Hk * a.D + to;
+        float* pv = pk + (int64_t)a.Tk * a.Hk * a.D;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+            store_block<SDGP_F32, FAST>(reinterpret_cast<char*>(pk), dk[d], d, half, a.D, a.scale);
+            store_block<SDGP_F32, FAST>(reinterpret_cast<char*>(pv), dv[d], d, half, a.D, 1.0f);
+        }
+        return;
+    }
 #pragma unroll
     for (int d = 0; d < DB; ++d) {
-        store_block<DT>(static_cast<char*>(a.dk) + to, dk[d], d, half, a.D, a.scale);
-        store_block<DT>(static_cast<char*>(a.dv) + to, dv[d], d, half, a.D, 1.0f);
+        store_block<DT, FAST>(static_cast<char*>(a.dk) + to * SIZE, dk[d], d, half, a.D, a.scale);
+        store_block<DT, FAST>(static_cast<char*>(a.dv) + to * SIZE, dv[d], d, half, a.D, 1.0f);
+    }
+}
+
+// dk and dv from the parts' sums [parts, 2, Tk Hk D].
+template <int DT>
+__global__ void __launch_bounds__(256) attention_dkv_join(const Attention a) {
+    const int64_t n = (int64_t)a.Tk * a.Hk * a.D;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < 2 * n; i += (int64_t)gridDim.x * 256) {
+        float sum = 0.0f;
+        for (int p = 0; p < a.parts; ++p) sum += a.part_o[(int64_t)p * 2 * n + i];
+        void* to = i < n ? a.dk : a.dv;
+        const int64_t at = i < n ? i : i - n;
+        if constexpr (DT == SDGP_BF16) static_cast<uint16_t*>(to)[at] = (uint16_t)float_to_bf16(sum);
+        else static_cast<float*>(to)[at] = sum;
     }
 }
 

@@ -2,5 +2,5 @@
 #include "attention_bwd_launch.h"
 
 namespace sdgp {
-template int attention_bwd_launch<SDGP_F32>(const Attention& a, int64_t row_tiles, int64_t key_tiles, hipStream_t stream);
+template int attention_bwd_launch<SDGP_F32>(Attention a, const AttentionGrid& g, hipStream_t stream);
 }  // namespace sdgp

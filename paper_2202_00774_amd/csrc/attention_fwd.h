@@ -210,13 +210,13 @@ __global__ void __launch_bounds__(256, attention_fwd_waves(DT, DC, FEW)) attenti
         const int64_t slot = (int64_t)part * ((int64_t)a.Tq * a.H) + out_row;
         if (half == 0) a.part_ml[2 * slot] = l != 0.0f ? mc : -INFINITY, a.part_ml[2 * slot + 1] = l;
 #pragma unroll
-        for (int d = 0; d < DB; ++d) store_block<SDGP_F32>(reinterpret_cast<char*>(a.part_o + slot * a.D), o[d], d, half, a.D, 1.0f);
+        for (int d = 0; d < DB; ++d) store_block<SDGP_F32, FAST>(reinterpret_cast<char*>(a.part_o + slot * a.D), o[d], d, half, a.D, 1.0f);
         return;
     }
     const float inverse = l != 0.0f ? 1.0f / l : 0.0f;
     if (half == 0) a.lse[out_row] = l != 0.0f ? log2_sum(mc, l) : -INFINITY;
 #pragma unroll
-    for (int d = 0; d < DB; ++d) store_block<DT>(static_cast<char*>(a.o) + out_row * a.D * SIZE, o[d], d, half, a.D, inverse);
+    for (int d = 0; d < DB; ++d) store_block<DT, FAST>(static_cast<char*>(a.o) + out_row * a.D * SIZE, o[d], d, half, a.D, inverse);
 }
 
 // Rows whose keys were taken in parts: one wavefront a row.
