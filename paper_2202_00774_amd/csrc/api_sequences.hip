@@ -100,7 +100,7 @@ int sdgp_attention(const void* q, const void* k, const void* v, const int64_t* s
 
 size_t sdgp_attention_bwd_workspace(int64_t sequences, int64_t Tq, int64_t Tk, int64_t H, int64_t Hk, int D, int dt) {
     if (check_attention_sizes(sequences, Tq, Tk, H, Hk, D, dt) != SDGP_OK) return (size_t)-1;
-    return sdgp::attention_bwd_workspace(sequences, Tq, Tk, H, Hk, D);
+    return sdgp::attention_bwd_workspace(sequences, Tq, Tk, H, Hk, D, dt);
 }
 
 int sdgp_attention_bwd(const void* dO, const void* q, const void* k, const void* v, const void* o, const float* lse,
@@ -114,7 +114,7 @@ int sdgp_attention_bwd(const void* dO, const void* q, const void* k, const void*
     for (const void* p : {dO, o, (const void*)dq, (const void*)dk, (const void*)dv})
         if (!aligned(p, element(dt))) return SDGP_ERR_SHAPE;
     if (!aligned(lse, 4)) return SDGP_ERR_SHAPE;
-    const size_t need = sdgp::attention_bwd_workspace(sequences, Tq, Tk, H, Hk, D);
+    const size_t need = sdgp::attention_bwd_workspace(sequences, Tq, Tk, H, Hk, D, dt);
     if (need > 0 && (!workspace || workspace_bytes < need || !aligned(workspace, 16))) return SDGP_ERR_WORKSPACE;
     return sdgp::attention_bwd_launch_all(c, dO, o, lse, dq, dk, dv, workspace, static_cast<hipStream_t>(hip_stream));
 }

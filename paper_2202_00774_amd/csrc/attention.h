@@ -15,7 +15,7 @@ struct Attention {
     const void *q, *k, *v;
     int64_t q_token, q_head, k_token, k_head, v_token, v_head;   // strides in elements
     const int32_t *off_q, *off_k, *len_k;                        // null: S sequences of Lq and Lk tokens each
-    int S, Lq, Lk, Tq, Tk, H, Hk, G, D, causal;
+    int S, Lq, Lk, Tq, Tk, H, Hk, G, D, causal, buckets;
     FastDiv by_group, by_heads;                                  // rows / G; a tile's rows / its heads (backward)
     float scale, c;                                              // c = scale log2 e
     bool fast;                                                   // Feed<..., FAST>
@@ -28,9 +28,12 @@ struct Attention {
     void *dq, *dk, *dv;
 };
 
-// How the gradients' kernels cut the work: wavefronts of a workgroup with rows or keys of their own, tiles of each.
+// Wavefronts of the keys' gradients' workgroups with keys of their own (fp32: two, whose tiles fill LDS already).
+constexpr int attention_own_keys(int dt) { return dt == SDGP_BF16 ? 4 : 2; }
+
+// How the gradients' kernels cut the work: wavefronts of a workgroup with rows of their own, tiles of each.
 struct AttentionGrid {
-    int own_rows, own_keys;
+    int own_rows;
     int64_t row_tiles, key_tiles;
 };
 
@@ -72,8 +75,23 @@ __device__ __forceinline__ Sequence rows_outside(const Attention& a, bool behind
     return s;
 }
 
-// Tile `index` of all sequences' tiles of UNIT rows (KEYS: of keys; else of queries, G a token): false behind the last.  With
-// offsets, a wavefront adds up the sequences' tiles 64 at a time (every wavefront for itself; the results are uniform).
+// How many of a sequence's tiles of UNIT rows (KEYS: of keys; else of queries, G a token) have at least `work` to do: of keys,
+// the tokens that see the first one; of queries, the keys that the last one sees.
+template <bool KEYS, int UNIT>
+__device__ __forceinline__ int tiles_of_work(const Attention& a, const Sequence& s, int work) {
+    const int tiles = ((KEYS ? s.nk : s.nq * a.G) + UNIT - 1) / UNIT;
+    if (work <= 0) return tiles;
+    if (work > (KEYS ? s.nq : s.nk)) return 0;
+    if (!a.causal) return tiles;
+    if (KEYS) return s.nk < work ? 0 : clamp_int((s.nk - work) / UNIT + 1, 0, tiles);
+    const int token = work - 1 - s.nk + s.nq;                           // the first one that sees so many
+    return token <= 0 ? tiles : token >= s.nq ? 0 : tiles - token * a.G / UNIT;
+}
+
+// Tile `index` of all sequences' tiles of UNIT rows: false behind the last.  `tile` counts a sequence's tiles from the one with the
+// most work.  With offsets, a wavefront adds up the sequences' tiles 64 at a time (every wavefront for itself; the results are
+// uniform), first those with three quarters of the most work there is, then those with half of it, and so on (a.buckets): the
+// long ones start first, and workgroups that run together share their sequences' rows as far as they can.
 template <bool KEYS, int UNIT>
 __device__ __forceinline__ bool find_tile(const Attention& a, int index, Sequence& s, int& tile, int& tiles) {
     if (a.off_q == nullptr) {
@@ -86,28 +104,47 @@ __device__ __forceinline__ bool find_tile(const Attention& a, int index, Sequenc
         return true;
     }
     const int lane = threadIdx.x & 63;
-    int before = 0;
-    for (int first = -1; first <= a.S; first += 64) {
-        const int i = first + lane;
-        Sequence mine = {0, 0, 0, 0};
-        if (i <= a.S) mine = i >= 0 && i < a.S ? sequence_at(a, i) : rows_outside<KEYS>(a, i >= 0);
-        const int n = ((KEYS ? mine.nk : mine.nq * a.G) + UNIT - 1) / UNIT;
-        int upto = n;
+    const auto sequence = [&](int i) {
+        Sequence x = {0, 0, 0, 0};
+        if (i <= a.S) x = i >= 0 && i < a.S ? sequence_at(a, i) : rows_outside<KEYS>(a, i >= 0);
+        return x;
+    };
+    Sequence mine = sequence(lane - 1);
+    int most = 0;
+    if (a.buckets > 1) {
+        for (int first = -1; first <= a.S; first += 64) {
+            const Sequence x = first == -1 ? mine : sequence(first + lane);
+            most = most < (KEYS ? x.nq : x.nk) ? (KEYS ? x.nq : x.nk) : most;
+        }
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
-            const int x = __shfl_up(upto, o);
-            if (lane >= o) upto += x;
+            const int x = __shfl_xor(most, o);
+            most = most < x ? x : most;
         }
-        const uint64_t past = __ballot(before + upto > index);
-        if (past != 0) {
-            const int at = __builtin_ctzll(past);
-            s.q0 = __builtin_amdgcn_readlane(mine.q0, at), s.nq = __builtin_amdgcn_readlane(mine.nq, at);
-            s.k0 = __builtin_amdgcn_readlane(mine.k0, at), s.nk = __builtin_amdgcn_readlane(mine.nk, at);
-            tiles = __builtin_amdgcn_readlane(n, at);
-            tile = index - before - (__builtin_amdgcn_readlane(upto, at) - tiles);
-            return true;
+    }
+    int before = 0;
+    for (int b = a.buckets - 1; b >= 0; --b) {
+        const int low = (int)((int64_t)most * b / a.buckets), high = b == a.buckets - 1 ? 0x7FFFFFFF : (int)((int64_t)most * (b + 1) / a.buckets);
+        for (int first = -1; first <= a.S; first += 64) {
+            if (a.S > 62) mine = sequence(first + lane);
+            const int above = tiles_of_work<KEYS, UNIT>(a, mine, high), n = tiles_of_work<KEYS, UNIT>(a, mine, b == 0 ? 0 : low) - above;
+            int upto = n;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const int x = __shfl_up(upto, o);
+                if (lane >= o) upto += x;
+            }
+            const uint64_t past = __ballot(before + upto > index);
+            if (past != 0) {
+                const int at = __builtin_ctzll(past);
+                s.q0 = __builtin_amdgcn_readlane(mine.q0, at), s.nq = __builtin_amdgcn_readlane(mine.nq, at);
+                s.k0 = __builtin_amdgcn_readlane(mine.k0, at), s.nk = __builtin_amdgcn_readlane(mine.nk, at);
+                tiles = ((KEYS ? s.nk : s.nq * a.G) + UNIT - 1) / UNIT;
+                tile = index - before - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(n, at)) + __builtin_amdgcn_readlane(above, at);
+                return true;
+            }
+            before += __builtin_amdgcn_readlane(upto, 63);
         }
-        before += __builtin_amdgcn_readlane(upto, 63);
     }
     return false;
 }

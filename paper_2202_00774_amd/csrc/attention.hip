@@ -36,17 +36,16 @@ Split choose(int64_t S, int64_t Tq, int64_t Tk, int64_t H, int64_t Hk) {
 }
 
 struct BwdSplit {
-    int own_rows, own_keys, parts;
+    int own_rows, parts;
 };
 
-BwdSplit choose_bwd(int64_t S, int64_t Tq, int64_t Tk, int64_t H, int64_t Hk) {
+BwdSplit choose_bwd(int64_t S, int64_t Tq, int64_t Tk, int64_t H, int64_t Hk, int dt) {
     const int64_t n = S > 0 ? S : 1, tokens = (Tq + n - 1) / n, rows = tokens * (H / Hk), keys = (Tk + n - 1) / n;
     const auto groups = [&](int64_t length, int64_t unit) { return n * ((length + unit - 1) / unit) * Hk; };
     BwdSplit s;
     s.own_rows = groups(rows, 128) >= 512 ? 4 : 2;
-    s.own_keys = groups(keys, 128) >= 512 ? 4 : 2;
-    const int64_t have = groups(keys, 32 * s.own_keys), rounds = (tokens + 63) / 64 * (H / Hk);
-    int64_t parts = have > 0 ? 256 / have : 1;
+    const int64_t have = groups(keys, 32 * attention_own_keys(dt)), rounds = (tokens + 63) / 64 * (H / Hk);
+    int64_t parts = have > 0 ? (dt == SDGP_BF16 ? 1024 : 512) / have : 1;
     parts = parts > rounds / 4 ? rounds / 4 : parts;
     s.parts = (int)(parts < 1 ? 1 : parts > 16 ? 16 : parts);
     return s;
@@ -62,6 +61,7 @@ Attention arguments(const AttentionCall& c) {
     a.by_group = fast_div((uint32_t)a.G);
     a.scale = c.scale, a.c = c.scale * 1.44269504088896341f;
     a.parts = 1;
+    a.buckets = 1;
     // Feed<..., FAST>: whole chunks on sixteen bytes, a token's distance of at least a head and within what a tile's offsets count
     const int64_t size = c.dt == SDGP_BF16 ? 2 : 4;
     uintptr_t all = reinterpret_cast<uintptr_t>(c.q) | reinterpret_cast<uintptr_t>(c.k) | reinterpret_cast<uintptr_t>(c.v) | (uintptr_t)(c.D * size);
@@ -76,13 +76,19 @@ Attention arguments(const AttentionCall& c) {
 
 }  // namespace
 
+// Workgroups by the work they have, where there are more of them than run at once and sequences long enough to differ (finding
+// their place takes them up to 8 us).
+static int in_order_of_work(const AttentionCall& c, int64_t workgroups) {
+    return c.offsets_q != nullptr && c.S > 1 && workgroups > 512 && c.Tq >= 512 * c.S ? 4 : 1;
+}
+
 size_t attention_workspace(int64_t S, int64_t Tq, int64_t Tk, int64_t H, int64_t Hk, int D) {
     const Split s = choose(S, Tq, Tk, H, Hk);
     return s.parts == 1 ? 0 : (size_t)s.parts * (size_t)(Tq * H) * (size_t)(D + 2) * sizeof(float);
 }
 
-size_t attention_bwd_workspace(int64_t S, int64_t Tq, int64_t Tk, int64_t H, int64_t Hk, int D) {
-    const BwdSplit s = choose_bwd(S, Tq, Tk, H, Hk);
+size_t attention_bwd_workspace(int64_t S, int64_t Tq, int64_t Tk, int64_t H, int64_t Hk, int D, int dt) {
+    const BwdSplit s = choose_bwd(S, Tq, Tk, H, Hk, dt);
     const size_t rows = 2 * (size_t)((Tq * H + 3) / 4 * 4);
     return (rows + (s.parts == 1 ? 0 : (size_t)s.parts * 2 * (size_t)(Tk * Hk) * (size_t)D)) * sizeof(float);
 }
@@ -96,6 +102,7 @@ int attention_launch(const AttentionCall& c, void* o, float* lse, void* workspac
     a.part_ml = a.part_o + (s.parts == 1 ? 0 : (int64_t)s.parts * c.Tq * c.H * c.D);
     const int64_t tiles = most_tiles(c.offsets_q != nullptr, c.S, c.Tq, a.Lq, a.G, s.few ? 32 : 128);
     if (tiles * a.Hk * a.parts > 0x7FFFFFFF) return SDGP_ERR_SHAPE;
+    a.buckets = in_order_of_work(c, tiles * a.Hk * a.parts);
     return c.dt == SDGP_BF16 ? attention_fwd_launch<SDGP_BF16>(a, tiles, s.few, stream) : attention_fwd_launch<SDGP_F32>(a, tiles, s.few, stream);
 }
 
@@ -107,15 +114,16 @@ int attention_bwd_launch_all(const AttentionCall& c, const void* d_o, const void
     a.delta = a.lse2 + (c.Tq * c.H + 3) / 4 * 4;
     for (const void* p : {d_o, o, (const void*)dq, (const void*)dk, (const void*)dv}) a.fast = a.fast && (reinterpret_cast<uintptr_t>(p) & 15u) == 0;
     const bool packed = c.offsets_q != nullptr;
-    const BwdSplit s = choose_bwd(c.S, c.Tq, c.Tk, c.H, c.Hk);
+    const BwdSplit s = choose_bwd(c.S, c.Tq, c.Tk, c.H, c.Hk, c.dt);
     a.parts = s.parts;
     a.part_o = a.delta + (c.Tq * c.H + 3) / 4 * 4;
-    const int rows = attention_dkv_rows(c.dt, a.fast ? (c.D <= 64 ? 64 : c.D <= 96 ? 96 : 128) : 128, s.own_keys);
+    const int rows = attention_dkv_rows(c.dt, a.fast ? (c.D <= 64 ? 64 : c.D <= 96 ? 96 : 128) : 128, attention_own_keys(c.dt));
     a.by_heads = fast_div((uint32_t)(a.G < rows ? a.G : rows));
     AttentionGrid g;
-    g.own_rows = s.own_rows, g.own_keys = s.own_keys;
+    g.own_rows = s.own_rows;
     g.row_tiles = c.Tq == 0 ? 0 : most_tiles(packed, c.S, c.Tq, a.Lq, a.G, 32 * s.own_rows);
-    g.key_tiles = c.Tk == 0 ? 0 : most_tiles(packed, c.S, c.Tk, a.Lk, 1, 32 * s.own_keys);
+    g.key_tiles = c.Tk == 0 ? 0 : most_tiles(packed, c.S, c.Tk, a.Lk, 1, 32 * attention_own_keys(c.dt));
+    a.buckets = in_order_of_work(c, g.key_tiles * a.Hk * a.parts);
     if (g.row_tiles * a.Hk > 0x7FFFFFFF || g.key_tiles * a.Hk * a.parts > 0x7FFFFFFF) return SDGP_ERR_SHAPE;
     return c.dt == SDGP_BF16 ? attention_bwd_launch<SDGP_BF16>(a, g, stream) : attention_bwd_launch<SDGP_F32>(a, g, stream);
 }

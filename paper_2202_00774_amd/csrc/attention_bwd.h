@@ -350,17 +350,35 @@ __global__ void __launch_bounds__(256, DT == SDGP_BF16 ? 2 : 1) attention_dkv_ke
     }
 }
 
-// dk and dv from the parts' sums [parts, 2, Tk Hk D].
+// dk and dv from the parts' sums [parts, 2, Tk Hk D], four values a thread (fewer at the end of each).
 template <int DT>
 __global__ void __launch_bounds__(256) attention_dkv_join(const Attention a) {
-    const int64_t n = (int64_t)a.Tk * a.Hk * a.D;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < 2 * n; i += (int64_t)gridDim.x * 256) {
-        float sum = 0.0f;
-        for (int p = 0; p < a.parts; ++p) sum += a.part_o[(int64_t)p * 2 * n + i];
-        void* to = i < n ? a.dk : a.dv;
-        const int64_t at = i < n ? i : i - n;
-        if constexpr (DT == SDGP_BF16) static_cast<uint16_t*>(to)[at] = (uint16_t)float_to_bf16(sum);
-        else static_cast<float*>(to)[at] = sum;
+    typedef float f32x4 __attribute__((ext_vector_type(4), aligned(4), may_alias));
+    const int64_t n = (int64_t)a.Tk * a.Hk * a.D, fours = (n + 3) / 4;
+    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < 2 * fours; e += (int64_t)gridDim.x * 256) {
+        const int64_t at = (e < fours ? e : e - fours) * 4;
+        const float* from = a.part_o + (e < fours ? 0 : n) + at;
+        const int left = (int)(n - at < 4 ? n - at : 4);
+        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (left == 4) {
+#pragma unroll 4
+            for (int p = 0; p < a.parts; ++p) {
+                const f32x4 x = *reinterpret_cast<const f32x4*>(from + (int64_t)p * 2 * n);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum[i] += x[i];
+            }
+        } else {
+            for (int p = 0; p < a.parts; ++p)
+                for (int i = 0; i < 3; ++i)
+                    if (i < left) sum[i] += from[(int64_t)p * 2 * n + i];
+        }
+        void* to = e < fours ? a.dk : a.dv;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (i >= left) break;
+            if constexpr (DT == SDGP_BF16) static_cast<uint16_t*>(to)[at + i] = (uint16_t)float_to_bf16(sum[i]);
+            else static_cast<float*>(to)[at + i] = sum[i];
+        }
     }
 }
 

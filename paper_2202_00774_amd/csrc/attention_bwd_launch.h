@@ -20,9 +20,7 @@ int attention_bwd_launch(Attention a, const AttentionGrid& g, hipStream_t stream
             rc = launch_status();
         }
         if (rc != SDGP_OK || g.key_tiles == 0) return;
-        const dim3 grid((unsigned)(g.key_tiles * a.Hk * parts));
-        if (g.own_keys == 4) hipLaunchKernelGGL((attention_dkv_kernel<DT, DC, FAST, 4>), grid, block, 0, stream, a);
-        else hipLaunchKernelGGL((attention_dkv_kernel<DT, DC, FAST, 2>), grid, block, 0, stream, a);
+        hipLaunchKernelGGL((attention_dkv_kernel<DT, DC, FAST, attention_own_keys(DT)>), dim3((unsigned)(g.key_tiles * a.Hk * parts)), block, 0, stream, a);
         rc = launch_status();
     };
     if (!a.fast) launch(std::integral_constant<int, 128>{}, std::false_type{});
@@ -30,7 +28,7 @@ int attention_bwd_launch(Attention a, const AttentionGrid& g, hipStream_t stream
     else if (a.D <= 96) launch(std::integral_constant<int, 96>{}, std::true_type{});
     else launch(std::integral_constant<int, 128>{}, std::true_type{});
     if (rc != SDGP_OK || parts == 1 || g.key_tiles == 0) return rc;
-    const int64_t values = 2 * (int64_t)a.Tk * a.Hk * a.D, blocks = (values + 255) / 256;
+    const int64_t values = 2 * (int64_t)a.Tk * a.Hk * a.D, blocks = (values + 1023) / 1024 + 1;
     hipLaunchKernelGGL((attention_dkv_join<DT>), dim3((unsigned)(blocks < 16384 ? blocks : 16384)), block, 0, stream, a);
     return launch_status();
 }

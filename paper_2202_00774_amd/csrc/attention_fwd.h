@@ -12,12 +12,13 @@
 
 namespace sdgp {
 
-// FEW: a workgroup's wavefronts share 32 rows and split the keys (single tokens); else each has 32 rows of its own.
+// FEW: a workgroup's wavefronts share 32 rows (single tokens): two halves of the keys, each for two halves of a head's values, so that
+// two workgroups fit a CU and one's loads fly while the other begins or ends.  Else each wavefront has 32 rows of its own.
 template <int DT, int DC, bool FEW>
 struct AttentionFwd {
     static constexpr int kWaves = 4, kThreads = 64 * kWaves;
     static constexpr int kRows = FEW ? 32 : 32 * kWaves;
-    static constexpr int kSplit = Tile<DT, DC>::kRow == 512 ? 2 : 4;   // FEW: wavefronts that have keys (two where LDS holds no more)
+    static constexpr int kSplit = 2;                                   // FEW: of the keys
     static constexpr int kKeys = FEW ? 32 * kSplit : (DT == SDGP_BF16 ? 64 : 32);
     static constexpr int kBlocks = FEW ? 1 : kKeys / 32;               // of 32 keys, a wavefront
     using T = Tile<DT, DC>;
@@ -25,12 +26,12 @@ struct AttentionFwd {
 };
 
 // Wavefronts a SIMD, as LDS and registers allow.
-constexpr int attention_fwd_waves(int dt, int dc, bool few) { return (few || dt == SDGP_F32) && (dc > 64 || (few && dt == SDGP_F32)) ? 1 : 2; }
+constexpr int attention_fwd_waves(int dt, int dc) { return dt == SDGP_F32 && dc > 64 ? 1 : 2; }
 
 __device__ __forceinline__ float log2_sum(float mc, float l) { return (mc + __builtin_amdgcn_logf(l)) * 0.693147180559945309f; }
 
 template <int DT, int DC, bool FEW, bool FAST>
-__global__ void __launch_bounds__(256, attention_fwd_waves(DT, DC, FEW)) attention_fwd_kernel(const Attention a) {
+__global__ void __launch_bounds__(256, attention_fwd_waves(DT, DC)) attention_fwd_kernel(const Attention a) {
     using L = AttentionFwd<DT, DC, FEW>;
     using T = typename L::T;
     constexpr int SIZE = Operand<DT>::kSize, STEPS = DC / 16, DB = DC / 32, NB = L::kBlocks;
@@ -57,7 +58,8 @@ __global__ void __launch_bounds__(256, attention_fwd_waves(DT, DC, FEW)) attenti
     const int last = rows - 1 < row0 + L::kRows - 1 ? rows - 1 : row0 + L::kRows - 1;
     const int most = seen(last);                                        // of the workgroup
     const int most_mine = FEW ? most : seen(last < first_row + 31 ? last : first_row + 31);   // of the wavefront (rows in front of last)
-    const bool any_row = first_row < rows && !(FEW && wave >= L::kSplit);
+    const bool any_row = first_row < rows;
+    const int split = FEW ? wave % L::kSplit : 0, side = FEW ? wave / L::kSplit : 0;   // FEW: whose keys, and which blocks of values
 
     const int t = row < rows ? (int)divide((uint32_t)row, a.by_group) : 0, g = row < rows ? row - t * a.G : 0;
     const int64_t out_row = (int64_t)(s.q0 + t) * a.H + head * a.G + g;
@@ -100,13 +102,13 @@ __global__ void __launch_bounds__(256, attention_fwd_waves(DT, DC, FEW)) attenti
     for (int n = begin; n < end; ++n) {
         SDGP_SHARED char *kt = buffer(n), *vt = kt + L::kTile;
         if (n + 1 < end) start(n + 1);
-        const int key0 = n * L::kKeys + (FEW ? 32 * wave : 0);
+        const int key0 = n * L::kKeys + 32 * split;
         if (key0 < most_mine && any_row) {
             const uint32_t k_at = T::rows_lane(kt, lane), v_at = T::columns_lane(vt, lane);
             attn_f32x16 x[NB];
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
-                const int r0 = FEW ? 32 * wave : 32 * b;
+                const int r0 = 32 * (FEW ? split : b);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) x[b][i] = 0.0f;
 #pragma unroll
@@ -150,11 +152,13 @@ __global__ void __launch_bounds__(256, attention_fwd_waves(DT, DC, FEW)) attenti
                     p[b][u].set(y);
                 }
 #pragma unroll
-            for (int d = 0; d < DB; ++d)
+            for (int d = 0; d < DB; ++d) {
+                if (FEW && d % 2 != side) continue;
 #pragma unroll
                 for (int b = 0; b < NB; ++b)
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) o[d] = multiply(T::columns(v_at, (FEW ? 32 * wave : 32 * b) + 16 * u, d), p[b][u], o[d]);
+                    for (int u = 0; u < 2; ++u) o[d] = multiply(T::columns(v_at, 32 * (FEW ? split : b) + 16 * u, d), p[b][u], o[d]);
+            }
         }
         if (n + 1 < end) finish(n + 1);
     }
@@ -165,20 +169,20 @@ __global__ void __launch_bounds__(256, attention_fwd_waves(DT, DC, FEW)) attenti
         // The wavefronts' sums over their keys, brought to one maximum and added up.
         __syncthreads();
         float* ml = lds_ml;
-        if (half == 0 && any_row) ml[wave * 32 + lane] = l != 0.0f ? mc : -INFINITY;
+        if (half == 0 && side == 0) ml[split * 32 + lane] = l != 0.0f ? mc : -INFINITY;
         __syncthreads();
         float top = -INFINITY;
 #pragma unroll
         for (int w = 0; w < L::kSplit; ++w) top = fmaxf(top, ml[w * 32 + (lane & 31)]);
         const float factor = l != 0.0f ? __builtin_amdgcn_exp2f(mc - top) : 0.0f;
-        if (half == 0 && any_row) ml[(L::kSplit + wave) * 32 + lane] = l * factor;
+        if (half == 0 && side == 0) ml[(L::kSplit + split) * 32 + lane] = l * factor;
         SDGP_SHARED float* sums = (SDGP_SHARED float*)lds;             // [kSplit, 32, DC]
-        if (any_row)
 #pragma unroll
-            for (int d = 0; d < DB; ++d)
+        for (int d = 0; d < DB; ++d)
+            if (d % 2 == side)
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    sums[(wave * 32 + (lane & 31)) * DC + ((32 * d + result_row(i, half)) ^ (lane & 31))] = o[d][i] * factor;
+                    sums[(split * 32 + (lane & 31)) * DC + ((32 * d + result_row(i, half)) ^ (lane & 31))] = o[d][i] * factor;
         __syncthreads();
         for (int e = threadIdx.x; e < 32 * DC; e += L::kThreads) {
             const int r = e / DC, d = e % DC, at = row0 + r;
@@ -219,7 +223,7 @@ __global__ void __launch_bounds__(256, attention_fwd_waves(DT, DC, FEW)) attenti
     for (int d = 0; d < DB; ++d) store_block<DT, FAST>(static_cast<char*>(a.o) + out_row * a.D * SIZE, o[d], d, half, a.D, inverse);
 }
 
-// Rows whose keys were taken in parts: one wavefront a row.
+// Rows whose keys were taken in parts: one wavefront a row.  Parts without keys hold nothing: what is read of them is not used.
 template <int DT>
 __global__ void __launch_bounds__(256) attention_join(const Attention a) {
     const int64_t rows = (int64_t)a.Tq * a.H, r = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
@@ -236,15 +240,31 @@ __global__ void __launch_bounds__(256) attention_join(const Attention a) {
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) total += __shfl_xor(total, o);
     const float weight = total != 0.0f ? factor / total : 0.0f;
-    for (int d = lane; d < (a.D + 63) / 64 * 64; d += 64) {
-        float y = 0.0f;
-        for (int p = 0; p < a.parts; ++p) {
-            const float w = __shfl(weight, p);
-            if (w != 0.0f && d < a.D) y += w * a.part_o[(p * rows + r) * a.D + d];   // (parts without keys hold nothing)
+    float y[2] = {0.0f, 0.0f};                                          // values lane and lane + 64: D <= 128
+    const int64_t step = rows * a.D;
+    const float* from = a.part_o + r * a.D;
+    for (int p0 = 0; p0 < a.parts; p0 += 4) {
+        float x[4][2];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                x[k][j] = 0.0f;
+                if (p0 + k < a.parts && lane + 64 * j < a.D) x[k][j] = from[(p0 + k) * step + lane + 64 * j];
+            }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float w = bits_to_float((uint32_t)__builtin_amdgcn_readlane((int)float_to_bits(weight), (p0 + k) & 63));
+#pragma unroll
+            for (int j = 0; j < 2; ++j) y[j] += w != 0.0f ? w * x[k][j] : 0.0f;
         }
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int d = lane + 64 * j;
         if (d >= a.D) continue;
-        if constexpr (DT == SDGP_BF16) static_cast<uint16_t*>(a.o)[r * a.D + d] = (uint16_t)float_to_bf16(y);
-        else static_cast<float*>(a.o)[r * a.D + d] = y;
+        if constexpr (DT == SDGP_BF16) static_cast<uint16_t*>(a.o)[r * a.D + d] = (uint16_t)float_to_bf16(y[j]);
+        else static_cast<float*>(a.o)[r * a.D + d] = y[j];
     }
     if (lane == 0) a.lse[r] = total != 0.0f ? log2_sum(top, total) : -INFINITY;
 }
