@@ -900,13 +900,15 @@ def sdgp_rotary(q: torch.Tensor, k: torch.Tensor | None, positions: torch.Tensor
         if x is None:
             out_strides += [0, 0]
             continue
+        if out is None:
+            out_strides += [x.shape[-2] * D, D]
+            continue
         if y.shape != x.shape:
             raise ValueError("outputs must have the shapes of q and k")
         token, head = _tokens(y, "out", q)
-        if out is not None:
-            _apart(y, x, name)
-            if T > 1 and token < D or x.shape[-2] > 1 and head < D:
-                raise ValueError("the heads of an output must not share memory")
+        _apart(y, x, name)
+        if T > 1 and token < D or x.shape[-2] > 1 and head < D:
+            raise ValueError("the heads of an output must not share memory")
         out_strides += [token, head]
     if H == 0:
         raise ValueError("expected q with heads")
