@@ -448,7 +448,8 @@ int sdgp_adamw_step(int count, void* const* params, const void* const* grads, vo
  *
  * Products of bf16 tensors are taken in bf16 with fp32 sums (probabilities rounded to bf16), those of fp32 tensors in fp32;
  * softmax statistics are fp32.  A NaN or infinity in k or v may reach all queries of its sequence and head group, also those that do
- * not see its token; one in q stays with its query.
+ * not see its token (masked products are 0 times it); one in q stays with its query.  In gradients one in any tensor may reach all of
+ * its sequence and head group.
  *
  * sdgp_attention_bwd -- dq [Tq, H, D], dk and dv [Tk, Hk, D] of `dt` from dO [Tq, H, D], the inputs and what the forward call
  *   left.  Everything that is contiguous above is so here; gradients of a key head are the sums over its query heads, in a fixed

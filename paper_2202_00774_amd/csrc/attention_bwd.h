@@ -1,12 +1,14 @@
 // Gradients of attention, from dO, the inputs, o and lse.
 //
-//   P = exp(scale q k^T - lse),  delta = sum_d dO o,  dS = P (dO V^T - delta)
+//   P = exp(scale q k^T - lse),  delta = sum_d dO o = sum over keys of P dP,  dP = dO V^T,  dS = P (dP - delta)
 //   dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO, the latter two summed over a key head's queries
 // Two kernels without atomics: one owns queries and passes over the keys (dQ, and delta on the way), one owns keys and passes
 // over the queries (dK, dV).  Each computes the scores again: 7 products of 2 D flops a pair instead of 5, for sums in
 // a fixed order that are read and written once.  As forward, every 32x32 result stands in the registers as the next
 // product's operand: with the owned rows in the results' columns, a lane holds sixteen of the passing rows.  P and dS are rounded
-// to bf16 for bf16 tensors, as operands of bf16 products; the sums are fp32.
+// to bf16 for bf16 tensors, as operands of bf16 products; the sums are fp32.  delta: dO o carries o's own rounding, which the other
+// sum does not; it is there once the keys have passed, so it is the keys' kernel's, and dQ's too where one tile holds all of a
+// workgroup's keys (64 sequences of 32 tokens: dQ and dK off by 0.0024 of their size against 64 bits, 0.0030 with dO o).
 #pragma once
 
 #include "attention.h"
@@ -90,7 +92,7 @@ __global__ void __launch_bounds__(256, DT == SDGP_BF16 ? 2 : 1) attention_dq_ker
     }
     delta = halves_sum(delta);
     const float lse2 = row < rows ? a.lse[out_row] * kLog2E : 0.0f;
-    if (row < rows && half == 0 && wave == own) a.delta[out_row] = delta, a.lse2[out_row] = lse2;
+    if (row < rows && half == 0 && wave == own) a.lse2[out_row] = lse2;
 
     const char* keys = static_cast<const char*>(a.k) + ((int64_t)s.k0 * a.k_token + (int64_t)head * a.k_head) * SIZE;
     const char* values = static_cast<const char*>(a.v) + ((int64_t)s.k0 * a.v_token + (int64_t)head * a.v_head) * SIZE;
@@ -108,6 +110,7 @@ __global__ void __launch_bounds__(256, DT == SDGP_BF16 ? 2 : 1) attention_dq_ker
         fv.finish(buffer(n) + L::kTile);
         __syncthreads();
     };
+    float passed = 0.0f;                                                // sum of P dP
     attn_f32x16 dq[DB];
 #pragma unroll
     for (int d = 0; d < DB; ++d)
@@ -121,47 +124,64 @@ __global__ void __launch_bounds__(256, DT == SDGP_BF16 ? 2 : 1) attention_dq_ker
         SDGP_SHARED char *kt = buffer(n), *vt = kt + L::kTile;
         if (n + 1 < end) start(n + 1);
         const uint32_t k_rows = T::rows_lane(kt, lane), v_rows = T::rows_lane(vt, lane), k_columns = T::columns_lane(kt, lane);
+        for (int pass = end == 1 ? 0 : 1; pass < 2; ++pass) {
+            const bool last_pass = pass == 1;
 #pragma unroll
-        for (int b = 0; b < L::kBlocks; ++b) {
-            const int key0 = n * L::kKeys + 32 * b;
-            if (key0 >= most_mine || !any_row || (L::kShare > 1 && (b & 1) != wave / OWN)) continue;
-            attn_f32x16 x, dp;
+            for (int b = 0; b < L::kBlocks; ++b) {
+                const int key0 = n * L::kKeys + 32 * b;
+                if (key0 >= most_mine || !any_row || (L::kShare > 1 && last_pass && (b & 1) != wave / OWN)) continue;
+                attn_f32x16 x, dp;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = dp[i] = 0.0f;
+                for (int i = 0; i < 16; ++i) x[i] = dp[i] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < STEPS; ++i) x = multiply(T::rows(k_rows, 32 * b, i), q[i], x);
+                for (int i = 0; i < STEPS; ++i) x = multiply(T::rows(k_rows, 32 * b, i), q[i], x);
 #pragma unroll
-            for (int i = 0; i < STEPS; ++i) dp = multiply(T::rows(v_rows, 32 * b, i), dO[i], dp);
+                for (int i = 0; i < STEPS; ++i) dp = multiply(T::rows(v_rows, 32 * b, i), dO[i], dp);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.c, -lse2)) * (dp[i] - delta);
-            if (key0 + 32 > fewest) {
+                for (int i = 0; i < 16; ++i) x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], a.c, -lse2));
+                if (key0 + 32 > fewest) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (key0 + result_row(i, half) >= mine) x[i] = 0.0f;
+                    for (int i = 0; i < 16; ++i)
+                        if (key0 + result_row(i, half) >= mine) x[i] = 0.0f;
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) passed = __builtin_fmaf(x[i], dp[i], passed);
+                if (!last_pass) continue;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[i] *= dp[i] - delta;
+                Operand<DT> ds[2];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    float y[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) y[i] = x[8 * u + i];
+                    ds[u].set(y);
+                }
+#pragma unroll
+                for (int d = 0; d < DB; ++d)
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) dq[d] = multiply(T::columns(k_columns, 32 * b + 16 * u, d), ds[u], dq[d]);
             }
-            Operand<DT> ds[2];
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                float y[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] = x[8 * u + i];
-                ds[u].set(y);
-            }
-#pragma unroll
-            for (int d = 0; d < DB; ++d)
-#pragma unroll
-                for (int u = 0; u < 2; ++u) dq[d] = multiply(T::columns(k_columns, 32 * b + 16 * u, d), ds[u], dq[d]);
+            if (!last_pass) delta = halves_sum(passed), passed = 0.0f;  // (of all the keys: no wavefront has left any out)
         }
         if (n + 1 < end) finish(n + 1);
     }
     add_shared<OWN>(lds, wave, lane, dq);
+    passed = halves_sum(passed);
+    if constexpr (L::kShare > 1) {
+        __shared__ float lds_passed[32 * OWN];
+        if (wave >= OWN && half == 0) lds_passed[32 * own + lane] = passed;
+        __syncthreads();
+        if (wave < OWN) passed += lds_passed[32 * own + (lane & 31)];
+    }
     if (row >= rows || wave != own) return;
+    if (half == 0) a.delta[out_row] = passed;
 #pragma unroll
     for (int d = 0; d < DB; ++d) store_block<DT, FAST>(static_cast<char*>(a.dq) + out_row * a.D * SIZE, dq[d], d, half, a.D, a.scale);
 }
 
 // The queries pass by in tiles of some tokens of all the group's heads, the sequence's last tokens first: so workgroups that started
-// together read the same tiles at the same time, whichever their keys are.  (Tiles of one head: 1255 us instead of %s for 22294 packed
+// together read the same tiles at the same time, whichever their keys are.  (Tiles of one head: 1255 us instead of 820 for 22294 packed
 // tokens of 16 heads.  Their rows are 4096 bytes apart in dO, where memory's channels repeat.)
 template <int DT, int DC, int OWN>
 struct AttentionDkv {

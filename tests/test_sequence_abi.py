@@ -1,0 +1,224 @@
+"""Argument checks of the operators on packed sequences, at the C boundary and in the binding, without a GPU."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+import paper_2202_00774_amd as sdgp
+from paper_2202_00774_amd import binding
+
+OK, E_NULL, E_SHAPE, E_DTYPE, E_WS, E_VALUE = 0, -1, -3, -4, -6, -8
+P, P2, ODD = ctypes.c_void_p(16), ctypes.c_void_p(18), ctypes.c_void_p(17)       # never dereferenced
+BAD = ctypes.c_size_t(-1).value
+INF, NAN = math.inf, math.nan
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return binding.load()
+
+
+def strides(*s):
+    return (ctypes.c_int64 * len(s))(*s)
+
+
+ATTENTION = dict(q=P, k=P, v=P, st=strides(256, 64, 128, 64, 128, 64), off_q=P, off_k=P, S=2, Tq=8, Tk=8, H=4, Hk=2, D=64, dt=1, causal=1, scale=0.1,
+                 ws=P, wbytes=1 << 40)
+
+WRONG_ATTENTION = [(dict(dt=2), E_DTYPE), (dict(dt=-1), E_DTYPE), (dict(S=-1), E_SHAPE), (dict(Tq=-1), E_SHAPE), (dict(Tk=-8), E_SHAPE), (dict(H=0), E_SHAPE),
+                   (dict(Hk=0), E_SHAPE), (dict(H=3), E_SHAPE), (dict(D=0), E_SHAPE), (dict(D=129), E_SHAPE), (dict(Tq=2 ** 30), E_SHAPE), (dict(Tk=2 ** 29), E_SHAPE),
+                   (dict(scale=0.0), E_VALUE), (dict(scale=-1.0), E_VALUE), (dict(scale=INF), E_VALUE), (dict(scale=NAN), E_VALUE), (dict(scale=1e-31), E_VALUE),
+                   (dict(off_q=None), E_NULL), (dict(off_k=None), E_NULL), (dict(off_q=None, off_k=None, Tq=7), E_SHAPE), (dict(off_q=None, off_k=None, Tk=9), E_SHAPE),
+                   (dict(off_q=None, off_k=None, S=0), E_SHAPE), (dict(off_q=P2), E_SHAPE), (dict(st=None), E_NULL), (dict(st=strides(-1, 64, 128, 64, 128, 64)), E_SHAPE),
+                   (dict(st=strides(256, 64, 128, 64, 2 ** 41, 64)), E_SHAPE), (dict(q=None), E_NULL), (dict(k=None), E_NULL), (dict(v=None), E_NULL), (dict(q=ODD), E_SHAPE),
+                   (dict(v=P2, dt=0), E_SHAPE)]
+
+
+def test_attention_argument_errors(lib):
+    def call(o=P, lse=P, lengths=None, **k):
+        a = {**ATTENTION, **k}
+        return lib.sdgp_attention(a["q"], a["k"], a["v"], a["st"], a["off_q"], a["off_k"], lengths, a["S"], o, lse, a["Tq"], a["Tk"], a["H"], a["Hk"], a["D"], a["dt"],
+                                  a["causal"], a["scale"], a["ws"], a["wbytes"], None)
+
+    for args, code in WRONG_ATTENTION:
+        assert call(**args) == code, args
+    assert call(lengths=P) == E_VALUE                                            # packed keys have their lengths
+    assert call(lengths=P2, off_q=None, off_k=None) == E_SHAPE
+    assert call(o=None) == E_NULL and call(lse=None) == E_NULL and call(o=ODD) == E_SHAPE and call(lse=P2) == E_SHAPE
+    assert call(Tq=0, q=None, o=None, lse=None) == OK
+    few = dict(S=1, Tq=1, Tk=1 << 16, H=4, Hk=1)
+    need = lib.sdgp_attention_workspace(1, 1, 1 << 16, 4, 1, 64, 1)
+    assert 0 < need < 1 << 24
+    assert call(ws=None, **few) == E_WS and call(wbytes=need - 1, **few) == E_WS and call(ws=ctypes.c_void_p(24), **few) == E_WS
+    assert lib.sdgp_attention_workspace(64, 1 << 16, 1 << 16, 16, 4, 128, 1) == 0
+    for args in ((1, 1, 1, 3, 2, 64, 1), (1, 1, 1, 4, 2, 200, 1), (1, 1, 1, 4, 2, 64, 5), (-1, 1, 1, 4, 2, 64, 1), (1, 1 << 30, 1, 4, 2, 64, 1)):
+        assert lib.sdgp_attention_workspace(*args) == BAD and lib.sdgp_attention_bwd_workspace(*args) == BAD
+
+
+def test_attention_bwd_argument_errors(lib):
+    def call(do=P, o=P, lse=P, dq=P, dk=P, dv=P, **k):
+        a = {**ATTENTION, **k}
+        return lib.sdgp_attention_bwd(do, a["q"], a["k"], a["v"], o, lse, a["st"], a["off_q"], a["off_k"], a["S"], dq, dk, dv, a["Tq"], a["Tk"], a["H"], a["Hk"], a["D"],
+                                      a["dt"], a["causal"], a["scale"], a["ws"], a["wbytes"], None)
+
+    for args, code in WRONG_ATTENTION:
+        assert call(**args) == code, args
+    for name in ("do", "o", "lse", "dq", "dk", "dv"):
+        assert call(**{name: None}) == E_NULL and call(**{name: ODD}) == E_SHAPE
+    need = lib.sdgp_attention_bwd_workspace(2, 8, 8, 4, 2, 64, 1)
+    assert need >= 2 * 8 * 4 * 4
+    assert call(ws=None) == E_WS and call(wbytes=need - 1) == E_WS and call(ws=P2) == E_WS
+    assert call(Tq=0, Tk=0, q=None, k=None, v=None, do=None, o=None, lse=None, dq=None, dk=None, dv=None) == OK
+
+
+def test_rotary_argument_errors(lib):
+    def call(q=P, k=P, qo=P, ko=P, st=(256, 64, 128, 64, 256, 64, 128, 64), pos=P, bits=64, freqs=P, pairs=(16, 16), axes=None, T=8, H=4, Hk=2, D=64, dt=1):
+        n = len(pairs) if pairs is not None else 2
+        return lib.sdgp_rotary(q, k, qo, ko, strides(*st) if st else None, pos, bits, freqs, (ctypes.c_int32 * n)(*pairs) if pairs is not None else None,
+                               n if axes is None else axes, T, H, Hk, D, dt, 0, 0, None)
+
+    assert call(dt=2) == E_DTYPE and call(bits=16) == E_DTYPE
+    for args in (dict(T=-1), dict(H=0), dict(Hk=-1), dict(D=1), dict(D=4097), dict(H=5000), dict(axes=0), dict(pairs=(1,) * 9), dict(T=2 ** 31), dict(H=4096, D=4096),
+                 dict(pairs=(16, 0)), dict(pairs=(16, 17)), dict(pairs=(2 ** 30, 2 ** 30)), dict(st=(-1, 64, 128, 64, 256, 64, 128, 64)), dict(q=ODD), dict(ko=ODD), dict(pos=P2),
+                 dict(freqs=P2), dict(st=(256, 64, 128, 64, 0, 64, 128, 64)), dict(st=(256, 64, 128, 64, 256, 0, 128, 64)), dict(st=(256, 64, 128, 64, 256, 64, 128, 63))):
+        assert call(**args) == E_SHAPE, args
+    for args in (dict(st=None), dict(pairs=None), dict(q=None), dict(qo=None), dict(k=None), dict(ko=None), dict(pos=None), dict(freqs=None), dict(Hk=0), dict(Hk=0, k=None)):
+        assert call(**args) == E_NULL, args
+    assert call(T=0, q=None) == OK
+
+
+def test_policy_loss_argument_errors(lib):
+    def given(logp=P, old=P, ref=P, adv=P, each=1, mask=P, off=P, S=2, T=8, low=0.2, high=0.2, kl=0.1):
+        return logp, old, ref, adv, each, mask, off, S, T, low, high, kl
+
+    def call(out=P, w=P, ws=P, wbytes=1 << 30, **k):
+        return lib.sdgp_policy_loss(*given(**k), 0, out, w, ws, wbytes, None)
+
+    def back(g=P, w=P, d=P, **k):
+        return lib.sdgp_policy_loss_bwd(g, w, *given(**k), d, None)
+
+    for f in (call, back):
+        for args in (dict(T=-1), dict(S=-1), dict(T=2 ** 31), dict(off=None, T=9), dict(off=None, S=0), dict(S=2 ** 31), dict(logp=P2), dict(old=P2), dict(ref=P2), dict(adv=ODD),
+                     dict(off=P2)):
+            assert f(**args) == E_SHAPE, args
+        for args in (dict(low=-0.1), dict(low=1.1), dict(low=NAN), dict(high=-0.1), dict(high=NAN), dict(kl=-1.0), dict(kl=INF), dict(kl=NAN), dict(ref=None)):
+            assert f(**args) == E_VALUE, args
+        for args in (dict(logp=None), dict(old=None), dict(adv=None), dict(w=None)):
+            assert f(**args) == E_NULL, args
+    assert call(out=None) == E_NULL and back(g=None) == E_NULL and back(d=None) == E_NULL
+    assert call(out=P2) == E_SHAPE and back(g=P2) == E_SHAPE and back(d=P2) == E_SHAPE
+    need = lib.sdgp_sequence_loss_workspace(8, 2)
+    assert need > 0 and call(ws=None) == E_WS and call(wbytes=need - 1) == E_WS and call(ws=P2) == E_WS
+    assert back(T=0, logp=None, old=None, g=None, d=None) == OK
+    assert lib.sdgp_sequence_loss_workspace(-1, 2) == BAD and lib.sdgp_sequence_loss_workspace(8, -1) == BAD and lib.sdgp_sequence_loss_workspace(2 ** 41, 1) == BAD
+
+
+def test_preference_loss_argument_errors(lib):
+    def call(logp=P, ref=P, mask=P, off=P, S=2, T=8, beta=0.1, margin=0.0, smoothing=0.0, loss=P, margins=P, w=P, ws=P, wbytes=1 << 30):
+        return lib.sdgp_preference_loss(logp, ref, mask, off, S, T, beta, margin, smoothing, 0, loss, margins, w, ws, wbytes, None)
+
+    for args in (dict(T=-1), dict(S=3), dict(S=-2), dict(T=2 ** 31), dict(off=None, T=9), dict(logp=P2), dict(ref=P2), dict(off=P2), dict(loss=P2), dict(w=ODD)):
+        assert call(**args) == E_SHAPE, args
+    for args in (dict(beta=INF), dict(beta=NAN), dict(margin=INF), dict(smoothing=-0.1), dict(smoothing=1.0), dict(smoothing=NAN)):
+        assert call(**args) == E_VALUE, args
+    for name in ("logp", "loss", "margins", "w"):
+        assert call(**{name: None}) == E_NULL
+    assert call(ws=None) == E_WS and call(wbytes=8) == E_WS
+
+    def back(g=P, w=P, mask=P, off=P, S=2, T=8, d=P):
+        return lib.sdgp_preference_loss_bwd(g, w, mask, off, S, T, d, None)
+
+    assert back(T=-1) == E_SHAPE and back(off=None, T=9) == E_SHAPE and back(g=P2) == E_SHAPE and back(d=P2) == E_SHAPE
+    assert back(g=None) == E_NULL and back(w=None) == E_NULL and back(d=None) == E_NULL and back(T=0, g=None, d=None) == OK
+
+
+# ------------------------------------------------------------------------- the binding, with tensors that say they are on a GPU
+
+class OnGpu(torch.Tensor):
+    gpu = 0
+    is_cuda = property(lambda self: True)
+
+    def get_device(self):
+        return self.gpu
+
+
+def on(gpu, *shape, dtype=torch.float32):
+    t = torch.zeros(shape, dtype=dtype).as_subclass(OnGpu)
+    t.gpu = gpu
+    return t
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    seen = []
+    monkeypatch.setattr(binding, "_launch", lambda name, x, *a: seen.append(name))
+    monkeypatch.setattr(binding, "_need", lambda *a: 64)
+    return seen
+
+
+I32 = torch.int32
+CALLS = {
+    "attention": lambda **k: sdgp.sdgp_attention(**{**dict(q=on(0, 6, 4, 8), k=on(0, 6, 2, 8), v=on(0, 6, 2, 8), offsets=on(0, 3, dtype=I32), offsets_k=on(0, 3, dtype=I32),
+                                                           workspace=on(0, 64, dtype=torch.uint8)), **k}),
+    "cache": lambda **k: sdgp.sdgp_attention(**{**dict(q=on(0, 2, 1, 4, 8), k=on(0, 2, 9, 2, 8), v=on(0, 2, 9, 2, 8), lengths=on(0, 2, dtype=I32)), **k}),
+    "attention_bwd": lambda **k: sdgp.sdgp_attention_bwd(**{**dict(do=on(0, 6, 4, 8), q=on(0, 6, 4, 8), k=on(0, 6, 2, 8), v=on(0, 6, 2, 8), o=on(0, 6, 4, 8), lse=on(0, 6, 4),
+                                                                   offsets=on(0, 3, dtype=I32), workspace=on(0, 64, dtype=torch.uint8)), **k}),
+    "rotary": lambda **k: sdgp.sdgp_rotary(**{**dict(q=on(0, 6, 4, 8), k=on(0, 6, 2, 8), positions=on(0, 6, dtype=I32), freqs=on(0, 4)), **k}),
+    "policy": lambda **k: sdgp.sdgp_policy_loss(**{**dict(logp=on(0, 6), old_logp=on(0, 6), advantages=on(0, 2), ref_logp=on(0, 6), mask=on(0, 6, dtype=torch.bool),
+                                                          offsets=on(0, 3, dtype=I32), kl=0.1, workspace=on(0, 64, dtype=torch.uint8)), **k}),
+    "policy_bwd": lambda **k: sdgp.sdgp_policy_loss_bwd(**{**dict(g=on(0), weights=on(0, 2), logp=on(0, 6), old_logp=on(0, 6), advantages=on(0, 6), offsets=on(0, 3, dtype=I32)), **k}),
+    "preference": lambda **k: sdgp.sdgp_preference_loss(**{**dict(logp=on(0, 6), ref_logp=on(0, 6), mask=on(0, 6, dtype=torch.uint8), offsets=on(0, 3, dtype=I32)), **k}),
+    "preference_bwd": lambda **k: sdgp.sdgp_preference_loss_bwd(**{**dict(g=on(0), weights=on(0, 2), logp=on(0, 6), mask=on(0, 6, dtype=torch.bool), offsets=on(0, 3, dtype=I32)), **k}),
+}
+TENSORS = {"attention": "q k v offsets offsets_k workspace", "cache": "q k v lengths", "attention_bwd": "do q k v o lse offsets workspace", "rotary": "q k positions freqs",
+           "policy": "logp old_logp advantages ref_logp mask offsets workspace", "policy_bwd": "g weights logp old_logp advantages offsets",
+           "preference": "logp ref_logp mask offsets", "preference_bwd": "g weights logp mask offsets"}
+SHAPES = {"attention": dict(q=(6, 4, 8), k=(6, 2, 8), v=(6, 2, 8), offsets=(3,), offsets_k=(3,), workspace=(64,)), "cache": dict(q=(2, 1, 4, 8), k=(2, 9, 2, 8), v=(2, 9, 2, 8), lengths=(2,)),
+          "attention_bwd": dict(do=(6, 4, 8), q=(6, 4, 8), k=(6, 2, 8), v=(6, 2, 8), o=(6, 4, 8), lse=(6, 4), offsets=(3,), workspace=(64,)),
+          "rotary": dict(q=(6, 4, 8), k=(6, 2, 8), positions=(6,), freqs=(4,)),
+          "policy": dict(logp=(6,), old_logp=(6,), advantages=(2,), ref_logp=(6,), mask=(6,), offsets=(3,), workspace=(64,)),
+          "policy_bwd": dict(g=(), weights=(2,), logp=(6,), old_logp=(6,), advantages=(6,), offsets=(3,)), "preference": dict(logp=(6,), ref_logp=(6,), mask=(6,), offsets=(3,)),
+          "preference_bwd": dict(g=(), weights=(2,), logp=(6,), mask=(6,), offsets=(3,))}
+DTYPES = {"offsets": I32, "offsets_k": I32, "lengths": I32, "positions": I32, "mask": torch.bool, "workspace": torch.uint8}
+
+
+@pytest.mark.parametrize("name", list(CALLS))
+def test_tensors_of_one_gpu(name, calls):
+    """Any one of the tensors on the host or on another GPU is refused."""
+    CALLS[name]()
+    assert len(calls) == 1
+    for t in TENSORS[name].split():
+        for gpu in (1, -1):
+            other = on(gpu, *SHAPES[name][t], dtype=DTYPES.get(t, torch.float32))
+            if gpu < 0:
+                other = other.as_subclass(torch.Tensor)
+            with pytest.raises(ValueError):
+                CALLS[name](**{t: other})
+    assert len(calls) == 1
+
+
+@pytest.mark.parametrize("name, wrong", [
+    ("attention", dict(q=on(0, 6, 3, 8))), ("attention", dict(k=on(0, 6, 2, 9))), ("attention", dict(v=on(0, 7, 2, 8))), ("attention", dict(q=on(0, 1, 6, 4, 8))),
+    ("attention", dict(offsets=on(0, 4, dtype=I32))), ("attention", dict(offsets=on(0, 3, dtype=torch.int64))), ("attention", dict(offsets=None)),
+    ("attention", dict(k=on(0, 6, 2, 8).bfloat16())), ("attention", dict(offsets_k=None, k=on(0, 7, 2, 8), v=on(0, 7, 2, 8))), ("attention", dict(lengths=on(0, 2, dtype=I32))),
+    ("attention", dict(q=on(0, 6, 8, 4).transpose(1, 2))), ("cache", dict(lengths=on(0, 3, dtype=I32))), ("cache", dict(k=on(0, 3, 9, 2, 8), v=on(0, 3, 9, 2, 8))),
+    ("cache", dict(offsets_k=on(0, 3, dtype=I32))), ("cache", dict(k=on(0, 9, 2, 2, 8).transpose(0, 1))), ("attention_bwd", dict(do=on(0, 6, 4, 8).bfloat16())),
+    ("attention_bwd", dict(lse=on(0, 6, 5))), ("attention_bwd", dict(o=on(0, 4, 6, 8).transpose(0, 1))), ("rotary", dict(freqs=on(0, 5))), ("rotary", dict(freqs=on(0, 0))),
+    ("rotary", dict(axes=(2, 1))), ("rotary", dict(axes=(2, 2))), ("rotary", dict(axes=(4, 0))), ("rotary", dict(positions=on(0, 5, dtype=I32))), ("rotary", dict(positions=on(0, 6))),
+    ("rotary", dict(k=on(0, 5, 2, 8))), ("rotary", dict(k=on(0, 6, 2, 10))), ("rotary", dict(out=(on(0, 6, 4, 8), None))), ("policy", dict(clip=(0.2, 0.2), ref_logp=None)),
+    ("policy", dict(average="token")), ("policy", dict(advantages=on(0, 3))), ("policy", dict(mask=on(0, 6))), ("policy", dict(logp=on(0, 6).double())), ("policy", dict(logp=on(0, 2, 3))),
+    ("policy_bwd", dict(g=on(0, 2))), ("policy_bwd", dict(weights=on(0, 3))), ("preference", dict(offsets=on(0, 4, dtype=I32))), ("preference", dict(ref_logp=on(0, 5))),
+    ("preference_bwd", dict(g=on(0).double()))])
+def test_what_the_binding_refuses(name, wrong, calls):
+    with pytest.raises(ValueError):
+        CALLS[name](**wrong)
+    assert not calls
+
+
+def test_token_strides_of_a_batch():
+    assert binding._heads(on(0, 2, 9, 4, 8), "q", False) == (32, 8)
+    assert binding._heads(on(0, 9, 4, 8)[:, :2], "q", True) == (32, 8)
+    assert binding._heads(on(0, 2, 1, 4, 8), "q", False) == (32, 8)
+    assert binding._tokens(on(0, 2, 9, 6, 8)[:, :, 1:5], "q") == (48, 8)
+    assert binding._tokens(on(0, 4, 8), "q") == (8, 8)                                # one token, whose distance is any
