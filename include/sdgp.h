@@ -456,7 +456,8 @@ int sdgp_adamw_step(int count, void* const* params, const void* const* grads, vo
  *   order: the same bits from call to call.  Tokens without a sequence, and keys that no query sees, have gradient 0.
  *
  * workspace: sdgp_attention_workspace(...) / sdgp_attention_bwd_workspace(...) bytes, 16-byte aligned, contents undefined
- * afterwards ((size_t)-1 for invalid arguments; 0 where the call needs none).  Tq * H and Tk * H at most 2^30.
+ * afterwards ((size_t)-1 for invalid arguments; 0 where the call needs none).  Tq * H and Tk * H at most 2^30, H at most 65536;
+ * scores beyond 2^30 in magnitude give NaN.
  */
 size_t sdgp_attention_workspace(int64_t sequences, int64_t Tq, int64_t Tk, int64_t H, int64_t Hk, int D, int dt);
 int sdgp_attention(const void* q, const void* k, const void* v, const int64_t* strides, const int32_t* offsets_q,
@@ -519,11 +520,11 @@ int sdgp_rotary(const void* q, const void* k, void* q_out, void* k_out, const in
  */
 size_t sdgp_sequence_loss_workspace(int64_t T, int64_t sequences);
 int sdgp_policy_loss(const float* logp, const float* old_logp, const float* ref_logp, const float* advantages, int each,
-                     const uint8_t* mask, const int32_t* offsets, int64_t sequences, int64_t T, float low, float high, float kl,
+                     const uint8_t* mask, const int32_t* offsets, int64_t sequences, int64_t T, double low, double high, float kl,
                      int by_sequence, float* out, float* weights, void* workspace, size_t workspace_bytes, void* hip_stream);
 int sdgp_policy_loss_bwd(const float* g, const float* weights, const float* logp, const float* old_logp, const float* ref_logp,
                          const float* advantages, int each, const uint8_t* mask, const int32_t* offsets, int64_t sequences,
-                         int64_t T, float low, float high, float kl, float* dlogp, void* hip_stream);
+                         int64_t T, double low, double high, float kl, float* dlogp, void* hip_stream);
 int sdgp_preference_loss(const float* logp, const float* ref_logp, const uint8_t* mask, const int32_t* offsets,
                          int64_t sequences, int64_t T, double beta, double margin, double smoothing, int average, float* loss,
                          float* margins, float* weights, void* workspace, size_t workspace_bytes, void* hip_stream);

@@ -130,9 +130,9 @@ def load():
             lib.sdgp_sequence_loss_workspace.restype = sz
             lib.sdgp_sequence_loss_workspace.argtypes = [i64, i64]
             lib.sdgp_policy_loss.restype = i32
-            lib.sdgp_policy_loss.argtypes = [vp] * 4 + [i32, vp, vp, i64, i64, f32, f32, f32, i32, vp, vp, vp, sz, vp]
+            lib.sdgp_policy_loss.argtypes = [vp] * 4 + [i32, vp, vp, i64, i64, f64, f64, f32, i32, vp, vp, vp, sz, vp]
             lib.sdgp_policy_loss_bwd.restype = i32
-            lib.sdgp_policy_loss_bwd.argtypes = [vp] * 6 + [i32, vp, vp, i64, i64, f32, f32, f32, vp, vp]
+            lib.sdgp_policy_loss_bwd.argtypes = [vp] * 6 + [i32, vp, vp, i64, i64, f64, f64, f32, vp, vp]
             lib.sdgp_preference_loss.restype = i32
             lib.sdgp_preference_loss.argtypes = [vp] * 4 + [i64, i64, f64, f64, f64, i32, vp, vp, vp, vp, sz, vp]
             lib.sdgp_preference_loss_bwd.restype = i32
@@ -854,13 +854,18 @@ def _tokens(t: torch.Tensor, name: str, x: torch.Tensor | None = None):
     return (shape[-1] if token is None else token), stride[-2]
 
 
-def _apart(out: torch.Tensor, x: torch.Tensor, name: str) -> None:
-    """``out`` is ``x`` itself, or their memory does not meet."""
-    if out.data_ptr() == x.data_ptr() and out.stride() == x.stride():
-        return
-    span = lambda t: sum((n - 1) * s for n, s in zip(t.shape, t.stride())) * t.element_size() + t.element_size()  # noqa: E731
-    if out.numel() and out.data_ptr() < x.data_ptr() + span(x) and x.data_ptr() < out.data_ptr() + span(out):
-        raise ValueError(f"the output for {name} must be {name} itself, or lie apart from it")
+def _apart(a: torch.Tensor, b: torch.Tensor) -> bool:
+    """Whether two tensors of heads share no memory: far from each other, or side by side in every token's values."""
+    span = lambda t: sum((n - 1) * s for n, s in zip(t.shape, t.stride())) + 1  # noqa: E731
+    size = a.element_size()
+    if not a.numel() or not b.numel() or a.data_ptr() + span(a) * size <= b.data_ptr() or b.data_ptr() + span(b) * size <= a.data_ptr():
+        return True
+    (step, _), (other, _) = _tokens(a, ""), _tokens(b, "")
+    if a.data_ptr() > b.data_ptr():
+        a, b = b, a
+    at = (b.data_ptr() - a.data_ptr()) // size
+    wide = lambda t: (t.shape[-2] - 1) * t.stride(-2) + t.shape[-1]  # noqa: E731
+    return step == other and at % step >= wide(a) and at % step + wide(b) <= step
 
 
 def sdgp_rotary(q: torch.Tensor, k: torch.Tensor | None, positions: torch.Tensor, freqs: torch.Tensor, axes=None, *,
@@ -906,10 +911,13 @@ def sdgp_rotary(q: torch.Tensor, k: torch.Tensor | None, positions: torch.Tensor
         if y.shape != x.shape:
             raise ValueError("outputs must have the shapes of q and k")
         token, head = _tokens(y, "out", q)
-        _apart(y, x, name)
+        if not (y.data_ptr() == x.data_ptr() and y.stride() == x.stride() or _apart(y, x)):
+            raise ValueError(f"the output for {name} must be {name} itself, or lie apart from it")
         if T > 1 and token < D or x.shape[-2] > 1 and head < D:
             raise ValueError("the heads of an output must not share memory")
         out_strides += [token, head]
+    if out is not None and k is not None and not (_apart(q_out, k_out) and _apart(q_out, k) and _apart(k_out, q)):
+        raise ValueError("the outputs for q and k must lie apart from each other and from the other input")
     if H == 0:
         raise ValueError("expected q with heads")
     _launch("sdgp_rotary", q, _ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out), (ctypes.c_int64 * 8)(*q_strides, *k_strides, *out_strides),

@@ -12,6 +12,8 @@ namespace {
 constexpr int64_t kMostRows = (int64_t)1 << 30;      // tokens times heads: counted in 32 bits
 constexpr int64_t kMostStride = (int64_t)1 << 40;
 constexpr int kMostHead = 128;
+constexpr int64_t kMostHeads = 65536;
+constexpr int64_t kMostGrid = 0xFFFFFF;              // workgroups of 256 threads: a launch counts threads in 32 bits
 
 bool valid_dtype(int dt) { return dt == SDGP_F32 || dt == SDGP_BF16; }
 bool aligned(const void* p, int64_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) == 0; }
@@ -19,7 +21,7 @@ int64_t element(int dt) { return dt == SDGP_BF16 ? 2 : 4; }
 
 int check_attention_sizes(int64_t S, int64_t Tq, int64_t Tk, int64_t H, int64_t Hk, int D, int dt) {
     if (!valid_dtype(dt)) return SDGP_ERR_DTYPE;
-    if (S < 0 || Tq < 0 || Tk < 0 || H < 1 || Hk < 1 || H % Hk != 0 || D < 1 || D > kMostHead) return SDGP_ERR_SHAPE;
+    if (S < 0 || Tq < 0 || Tk < 0 || H < 1 || H > kMostHeads || Hk < 1 || H % Hk != 0 || D < 1 || D > kMostHead) return SDGP_ERR_SHAPE;
     if (S > kMostRows / H || Tq > kMostRows / H || Tk > kMostRows / H) return SDGP_ERR_SHAPE;
     return SDGP_OK;
 }
@@ -42,11 +44,11 @@ int check_attention(const sdgp::AttentionCall& c) {
     return SDGP_OK;
 }
 
-constexpr int64_t kMostTokens = (int64_t)1 << 40;
+constexpr int64_t kMostTokens = kMostGrid * 1024, kMostSequences = kMostGrid * 4;   // a workgroup's
 
 // The sequences' tokens, without their addresses.
 int check_sequences(int64_t T, int64_t S, bool packed) {
-    if (T < 0 || S < 0 || S > 0x7FFFFFFF - 1024 || T > kMostTokens) return SDGP_ERR_SHAPE;
+    if (T < 0 || S < 0 || S > kMostSequences || T > kMostTokens) return SDGP_ERR_SHAPE;
     if (packed ? T > 0x7FFFFFFF : S == 0 ? T > 0 : T % S != 0 || T / S > 0x7FFFFFFF) return SDGP_ERR_SHAPE;   // offsets have 32 bits
     return SDGP_OK;
 }
@@ -60,18 +62,18 @@ sdgp::Sequences sequences_of(const float* logp, const float* ref, const uint8_t*
     return {logp, ref, mask, offsets, T, (int)S, S > 0 ? (int)(T / S < 0x7FFFFFFF ? T / S : 0x7FFFFFFF) : 0};
 }
 
-int check_policy(const sdgp::Sequences& s, int64_t S, const float* old, const float* advantages, int each, float low, float high, float kl) {
+int check_policy(const sdgp::Sequences& s, int64_t S, const float* old, const float* advantages, int each, double low, double high, float kl) {
     int rc = check_sequences(s.T, S, s.offsets != nullptr);
     if (rc != SDGP_OK) return rc;
-    if (!(low >= 0.0f && low <= 1.0f) || !(high >= 0.0f) || !isfinite(kl) || kl < 0.0f || (kl > 0.0f && s.T > 0 && !s.ref)) return SDGP_ERR_VALUE;
+    if (!(low >= 0.0 && low <= 1.0) || !(high >= 0.0) || !isfinite(kl) || kl < 0.0f || (kl > 0.0f && s.T > 0 && !s.ref)) return SDGP_ERR_VALUE;
     rc = check_tokens(s);
     if (rc != SDGP_OK) return rc;
     if ((s.T > 0 && !old) || ((each ? s.T : S) > 0 && !advantages)) return SDGP_ERR_NULL;
     return aligned(old, 4) && aligned(advantages, 4) ? SDGP_OK : SDGP_ERR_SHAPE;
 }
 
-sdgp::PolicyLoss policy_of(const sdgp::Sequences& s, const float* old, const float* advantages, int each, int by_sequence, float low, float high, float kl) {
-    return {s, old, advantages, each != 0, by_sequence != 0, kl, low, high, log1p(-(double)low), log1p((double)high)};
+sdgp::PolicyLoss policy_of(const sdgp::Sequences& s, const float* old, const float* advantages, int each, int by_sequence, double low, double high, float kl) {
+    return {s, old, advantages, each != 0, by_sequence != 0, kl, (float)(1.0 - low), (float)(1.0 + high), log1p(-low), log1p(high)};
 }
 
 }  // namespace
@@ -143,6 +145,7 @@ int sdgp_rotary(const void* q, const void* k, void* q_out, void* k_out, const in
     if (!aligned(positions, position_bits / 8) || !aligned(freqs, 4)) return SDGP_ERR_SHAPE;
     // every output element is written once
     if ((T > 1 && strides[4] < D) || (H > 1 && strides[5] < D) || (Hk > 0 && T > 1 && strides[6] < D) || (Hk > 1 && strides[7] < D)) return SDGP_ERR_SHAPE;
+    if ((T + sdgp::rotary_tokens(pairs) - 1) / sdgp::rotary_tokens(pairs) > kMostGrid) return SDGP_ERR_SHAPE;
     a.q = q, a.k = k, a.q_out = q_out, a.k_out = k_out;
     a.q_token = strides[0], a.q_head = strides[1], a.k_token = strides[2], a.k_head = strides[3];
     a.q_out_token = strides[4], a.q_out_head = strides[5], a.k_out_token = strides[6], a.k_out_head = strides[7];
@@ -152,12 +155,12 @@ int sdgp_rotary(const void* q, const void* k, void* q_out, void* k_out, const in
 }
 
 size_t sdgp_sequence_loss_workspace(int64_t T, int64_t sequences) {
-    if (T < 0 || sequences < 0 || sequences > 0x7FFFFFFF - 1024 || T > kMostTokens) return (size_t)-1;
+    if (T < 0 || sequences < 0 || sequences > kMostSequences || T > kMostTokens) return (size_t)-1;
     return sdgp::sequence_loss_workspace(T, sequences);
 }
 
 int sdgp_policy_loss(const float* logp, const float* old_logp, const float* ref_logp, const float* advantages, int each,
-                     const uint8_t* mask, const int32_t* offsets, int64_t sequences, int64_t T, float low, float high, float kl,
+                     const uint8_t* mask, const int32_t* offsets, int64_t sequences, int64_t T, double low, double high, float kl,
                      int by_sequence, float* out, float* weights, void* workspace, size_t workspace_bytes, void* hip_stream) {
     const sdgp::Sequences s = sequences_of(logp, ref_logp, mask, offsets, T, sequences);
     const int rc = check_policy(s, sequences, old_logp, advantages, each, low, high, kl);
@@ -172,7 +175,7 @@ int sdgp_policy_loss(const float* logp, const float* old_logp, const float* ref_
 
 int sdgp_policy_loss_bwd(const float* g, const float* weights, const float* logp, const float* old_logp, const float* ref_logp,
                          const float* advantages, int each, const uint8_t* mask, const int32_t* offsets, int64_t sequences, int64_t T,
-                         float low, float high, float kl, float* dlogp, void* hip_stream) {
+                         double low, double high, float kl, float* dlogp, void* hip_stream) {
     const sdgp::Sequences s = sequences_of(logp, ref_logp, mask, offsets, T, sequences);
     const int rc = check_policy(s, sequences, old_logp, advantages, each, low, high, kl);
     if (rc != SDGP_OK) return rc;

@@ -17,6 +17,8 @@ int attention_bwd_launch(Attention a, const AttentionGrid& g, hipStream_t stream
 
 namespace {
 
+constexpr int64_t kMostWorkgroups = 0xFFFFFF;   // of 256 threads: a launch counts threads in 32 bits
+
 struct Split {
     bool few;
     int parts;
@@ -101,7 +103,7 @@ int attention_launch(const AttentionCall& c, void* o, float* lse, void* workspac
     a.part_o = static_cast<float*>(workspace);
     a.part_ml = a.part_o + (s.parts == 1 ? 0 : (int64_t)s.parts * c.Tq * c.H * c.D);
     const int64_t tiles = most_tiles(c.offsets_q != nullptr, c.S, c.Tq, a.Lq, a.G, s.few ? 32 : 128);
-    if (tiles * a.Hk * a.parts > 0x7FFFFFFF) return SDGP_ERR_SHAPE;
+    if (tiles * a.Hk * a.parts > kMostWorkgroups) return SDGP_ERR_SHAPE;
     a.buckets = in_order_of_work(c, tiles * a.Hk * a.parts);
     return c.dt == SDGP_BF16 ? attention_fwd_launch<SDGP_BF16>(a, tiles, s.few, stream) : attention_fwd_launch<SDGP_F32>(a, tiles, s.few, stream);
 }
@@ -124,7 +126,7 @@ int attention_bwd_launch_all(const AttentionCall& c, const void* d_o, const void
     g.row_tiles = c.Tq == 0 ? 0 : most_tiles(packed, c.S, c.Tq, a.Lq, a.G, 32 * s.own_rows);
     g.key_tiles = c.Tk == 0 ? 0 : most_tiles(packed, c.S, c.Tk, a.Lk, 1, 32 * attention_own_keys(c.dt));
     a.buckets = in_order_of_work(c, g.key_tiles * a.Hk * a.parts);
-    if (g.row_tiles * a.Hk > 0x7FFFFFFF || g.key_tiles * a.Hk * a.parts > 0x7FFFFFFF) return SDGP_ERR_SHAPE;
+    if (g.row_tiles * a.Hk > kMostWorkgroups || g.key_tiles * a.Hk * a.parts > kMostWorkgroups) return SDGP_ERR_SHAPE;
     return c.dt == SDGP_BF16 ? attention_bwd_launch<SDGP_BF16>(a, g, stream) : attention_bwd_launch<SDGP_F32>(a, g, stream);
 }
 

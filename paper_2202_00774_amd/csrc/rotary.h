@@ -23,6 +23,9 @@ struct Rotary {
     FastDiv by_pairs, by_head, by_token;
 };
 
+// Tokens of a workgroup: a sine and cosine a thread.
+constexpr int rotary_tokens(int64_t pairs) { return pairs > 256 ? 1 : (int)(256 / pairs); }
+
 int rotary_launch(Rotary a, int dt, bool interleaved, hipStream_t stream);
 
 }  // namespace sdgp

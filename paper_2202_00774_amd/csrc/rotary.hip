@@ -102,8 +102,7 @@ int rotary_launch(Rotary a, int dt, bool interleaved, hipStream_t stream) {
     a.per_head = a.turned + (a.D - 2 * a.F + N - 1) / N;
     a.per_token = a.per_head * (a.H + a.Hk);
     a.by_pairs = fast_div((uint32_t)a.F), a.by_head = fast_div((uint32_t)a.per_head), a.by_token = fast_div((uint32_t)a.per_token);
-    // a sine and cosine a thread
-    a.tokens = kBlock / a.F < 1 ? 1 : kBlock / a.F;
+    a.tokens = rotary_tokens(a.F);
     if (a.tokens > a.T) a.tokens = (int)a.T;
     const dim3 grid((unsigned)((a.T + a.tokens - 1) / a.tokens)), block(kBlock);
     const size_t lds = (size_t)a.tokens * 2 * a.F * sizeof(float);

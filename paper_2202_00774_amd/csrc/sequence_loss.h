@@ -18,7 +18,7 @@ struct PolicyLoss {
     const float *old, *advantages;
     bool each;                     // an advantage a token, not a sequence
     bool by_sequence;              // mean over the sequences' means, not over the tokens
-    float kl, low, high;           // 1 - low and 1 + high bound the ratio
+    float kl, low, high;           // low and high bound the ratio
     double log_low, log_high;
 };
 

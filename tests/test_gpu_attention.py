@@ -193,3 +193,36 @@ def test_wrong_offsets_touch_nothing_outside(bad):
     good = offsets_of([30, 30, 40])
     ref = attention(q, k, v, spans_of([30, 30, 40], [30, 30, 40]), True, D ** -0.5)
     check(sdgp.sdgp_attention(q, k, v, good)[0], ref, "o")
+
+
+def test_offsets_that_pass_32_bits():
+    """A cache of more than 2^31 values (and 2^32 bytes): all keys score 0 but the last ones of the second sequence."""
+    L, Hk, D = (1 << 20) + 5, 8, 128
+    k, v = (torch.zeros(2, L, Hk, D, dtype=BF16, device="cuda") for _ in range(2))
+    q = randn(0, 2, 1, 16, D, dtype=BF16)
+    k[1, -1] = q[1, 0, ::2]
+    v[1, -1] = randn(1, Hk, D, dtype=BF16)
+    lengths = torch.tensor([L, L], dtype=torch.int32, device="cuda")
+    o, lse = sdgp.sdgp_attention(q, k, v, lengths=lengths, scale=1.0)
+    s = (q[1, 0].double() * k[1, -1].double().repeat_interleave(2, 0)).sum(1)
+    want = torch.logaddexp(s, torch.full_like(s, math.log(L - 1)))
+    assert float((lse[1, 0].double() - want).abs().max()) <= 2.0 ** -10 and float((lse[0, 0].double() - math.log(L)).abs().max()) <= 2.0 ** -10
+    p = torch.exp(s - want)[:, None]
+    value = p * v[1, -1].double().repeat_interleave(2, 0)
+    # p is rounded by 2^-8, and off by 2^-16 for a score of some hundred in 24 bits; storing rounds by 2^-8
+    assert bool(((o[1, 0].double() - value).abs() <= (2 * 2.0 ** -8 + 2.0 ** -15) * value.abs() + 1e-30).all()) and not o[0].any()
+    del k, v, o
+
+
+def test_gradients_whose_offsets_pass_32_bits():
+    """2^31 values of queries: 65536 short sequences, the last ones against 64 bits."""
+    B, L, H, D = 1 << 16, 16, 16, 128
+    g = torch.Generator(device="cuda").manual_seed(1)
+    q, k, v, do = (torch.randn(B, L, H, D, dtype=BF16, device="cuda", generator=g) for _ in range(4))
+    o, lse = sdgp.sdgp_attention(q, k, v)
+    grads = sdgp.sdgp_attention_bwd(do, q, k, v, o, lse)
+    flat = [t[-3:].reshape(3 * L, H, D) for t in (q, k, v, do)]
+    ref = attention(*flat[:3], spans_of([L] * 3, [L] * 3), True, D ** -0.5, flat[3])
+    check(o[-3:].reshape(3 * L, H, D), ref, "o")
+    for name, t in zip(("dq", "dk", "dv"), grads):
+        check(t[-3:].reshape(3 * L, H, D), ref, name)

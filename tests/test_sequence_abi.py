@@ -27,7 +27,7 @@ ATTENTION = dict(q=P, k=P, v=P, st=strides(256, 64, 128, 64, 128, 64), off_q=P, 
                  ws=P, wbytes=1 << 40)
 
 WRONG_ATTENTION = [(dict(dt=2), E_DTYPE), (dict(dt=-1), E_DTYPE), (dict(S=-1), E_SHAPE), (dict(Tq=-1), E_SHAPE), (dict(Tk=-8), E_SHAPE), (dict(H=0), E_SHAPE),
-                   (dict(Hk=0), E_SHAPE), (dict(H=3), E_SHAPE), (dict(D=0), E_SHAPE), (dict(D=129), E_SHAPE), (dict(Tq=2 ** 30), E_SHAPE), (dict(Tk=2 ** 29), E_SHAPE),
+                   (dict(Hk=0), E_SHAPE), (dict(H=3), E_SHAPE), (dict(H=65538), E_SHAPE), (dict(D=0), E_SHAPE), (dict(D=129), E_SHAPE), (dict(Tq=2 ** 30), E_SHAPE), (dict(Tk=2 ** 29), E_SHAPE),
                    (dict(scale=0.0), E_VALUE), (dict(scale=-1.0), E_VALUE), (dict(scale=INF), E_VALUE), (dict(scale=NAN), E_VALUE), (dict(scale=1e-31), E_VALUE),
                    (dict(off_q=None), E_NULL), (dict(off_k=None), E_NULL), (dict(off_q=None, off_k=None, Tq=7), E_SHAPE), (dict(off_q=None, off_k=None, Tk=9), E_SHAPE),
                    (dict(off_q=None, off_k=None, S=0), E_SHAPE), (dict(off_q=P2), E_SHAPE), (dict(st=None), E_NULL), (dict(st=strides(-1, 64, 128, 64, 128, 64)), E_SHAPE),
@@ -222,3 +222,21 @@ def test_token_strides_of_a_batch():
     assert binding._heads(on(0, 2, 1, 4, 8), "q", False) == (32, 8)
     assert binding._tokens(on(0, 2, 9, 6, 8)[:, :, 1:5], "q") == (48, 8)
     assert binding._tokens(on(0, 4, 8), "q") == (8, 8)                                # one token, whose distance is any
+
+
+def test_outputs_of_rotary_that_share_memory(calls):
+    """In place side by side in one tensor is fine; the same tensor twice, or the other input, is not."""
+    qkv = on(0, 6, 8, 8)
+    q, k = qkv[:, :4], qkv[:, 4:6]
+    for t in (q, k, qkv[:, 2:4]):
+        t.gpu = 0
+    how = dict(positions=on(0, 6, dtype=I32), freqs=on(0, 4))
+    sdgp.sdgp_rotary(q, k, **how, out=(q, k))
+    assert calls == ["sdgp_rotary"]
+    same, other = on(0, 6, 4, 8), on(0, 6, 4, 8)
+    for args, out in (((same, same), (same, same)), ((same, other), (other, same)), ((q, k), (q, qkv[:, 3:5])), ((q, k), (qkv[:, 1:5], k)), ((q, q), (q, on(0, 6, 4, 8)))):
+        for t in (*args, *out):
+            t.gpu = 0
+        with pytest.raises(ValueError, match="apart"):
+            sdgp.sdgp_rotary(*args, **how, out=out)
+    assert calls == ["sdgp_rotary"]
