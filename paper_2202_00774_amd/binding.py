@@ -808,8 +808,7 @@ def sdgp_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets: t
     wbytes = 0
     if need:
         workspace, wbytes = _own_workspace(need, workspace, q, "sdgp_attention_workspace")
-    o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    lse = torch.empty(q.shape[:-1], dtype=torch.float32, device=q.device)
+    o, lse = q.new_empty(q.shape), q.new_empty(q.shape[:-1], dtype=torch.float32)
     _launch("sdgp_attention", q, _ptr(q), _ptr(k), _ptr(v), strides, _ptr(offsets), _ptr(offsets_k), _ptr(lengths), S, _ptr(o), _ptr(lse),
             Tq, Tk, H, Hk, D, dt, int(causal), scale, _ptr(workspace) if need else None, wbytes)
     return o, lse
@@ -827,7 +826,7 @@ def sdgp_attention_bwd(do: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: to
     if need == _INVALID:
         raise SdgpError(-3, "sdgp_attention_bwd")
     workspace, wbytes = _own_workspace(need, workspace, q, "sdgp_attention_bwd_workspace")
-    dq, dk, dv = (torch.empty(t.shape, dtype=q.dtype, device=q.device) for t in (q, k, v))
+    dq, dk, dv = q.new_empty(q.shape), q.new_empty(k.shape), q.new_empty(k.shape)
     _launch("sdgp_attention_bwd", q, _ptr(do), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), strides, _ptr(offsets), _ptr(offsets_k), S,
             _ptr(dq), _ptr(dk), _ptr(dv), Tq, Tk, H, Hk, D, dt, int(causal), scale, _ptr(workspace), wbytes)
     return dq, dk, dv
@@ -894,8 +893,8 @@ def sdgp_rotary(q: torch.Tensor, k: torch.Tensor | None, positions: torch.Tensor
         if k.shape[:-2] != tokens or k.shape[-1] != D or Hk == 0:
             raise ValueError("k must have q's tokens and head size, and heads")
     if out is None:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        k_out = None if k is None else torch.empty(k.shape, dtype=q.dtype, device=q.device)
+        q_out = q.new_empty(q.shape)
+        k_out = None if k is None else q.new_empty(k.shape)
     else:
         q_out, k_out = out
         if (k_out is None) != (k is None):

@@ -30,7 +30,7 @@ Split choose(int64_t S, int64_t Tq, int64_t Tk, int64_t H, int64_t Hk) {
     Split s;
     s.few = rows <= 32;
     const int64_t unit = s.few ? 32 : 128, groups = n * ((rows + unit - 1) / unit) * Hk;
-    int64_t parts = groups > 0 ? (s.few ? 1024 : 512) / groups : 1;
+    int64_t parts = groups > 0 ? (s.few ? 1536 : 512) / groups : 1;
     const int64_t most = keys / 128;
     parts = parts > most ? most : parts;
     s.parts = (int)(parts < 1 ? 1 : parts > 64 ? 64 : parts);

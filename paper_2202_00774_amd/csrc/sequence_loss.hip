@@ -19,7 +19,14 @@ namespace sdgp {
 namespace {
 
 constexpr int kBlock = 256, kWaves = kBlock / 64, kChunk = 256, kTerms = 4, kFinish = 1024;
-constexpr int kOneLaunchTokens = 16384, kOneLaunchSequences = 128;
+constexpr int kOneLaunchSequences = 128;
+// Tokens of batches that one workgroup takes through all three steps.  The policy loss's wavefronts should have one chunk each.
+template <class Loss>
+constexpr int64_t one_launch_tokens();
+template <>
+constexpr int64_t one_launch_tokens<PolicyLoss>() { return 16 * kChunk; }
+template <>
+constexpr int64_t one_launch_tokens<PreferenceLoss>() { return 64 * kChunk; }
 
 struct Span {
     int64_t begin, end;
@@ -334,7 +341,7 @@ int loss_launch(const Loss& p, void* workspace, hipStream_t stream, Out... out) 
     const int64_t chunks = (p.s.T + kChunk - 1) / kChunk;
     double* slots = static_cast<double*>(workspace);
     double* sums = slots + (chunks + p.s.S) * kTerms;
-    if (p.s.T <= kOneLaunchTokens && p.s.S <= kOneLaunchSequences) {
+    if (p.s.T <= one_launch_tokens<Loss>() && p.s.S <= kOneLaunchSequences) {
         hipLaunchKernelGGL((loss_at_once<Loss, Out...>), dim3(1), dim3(kFinish), 0, stream, p, chunks, slots, sums, out...);
         return launch_status();
     }
