@@ -4,7 +4,8 @@ Structured Data Gradient Pruning (arXiv 2202.00774) keeps n of every m channels
 of the output data gradient (Alg. 1, Sec. III-B) and computes the input data
 gradient from the pruned tensor (Fig. 1-3).  Beside it stand the operators that a step of
 a language model with such layers needs: token log probabilities (the loss), block
-norms, and the AdamW step of ``optim``.  The work is done by hand-written
+norms, and the AdamW step of ``optim``; and, for packed sequences, attention, rotary positions,
+policy and preference losses.  The work is done by hand-written
 HIP kernels behind a C ABI (``include/sdgp.h``); this package is the thin Python
 binding over it.  There is no CPU fallback: without the built library every
 call raises.
