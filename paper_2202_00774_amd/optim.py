@@ -117,6 +117,7 @@ class AdamW:
         theirs = self.params if self.copies is None else self.params + self.copies
         now = list(map(torch.Tensor.data_ptr, theirs + self._followed))
         if now != self._seen or not self._same(*theirs):
+            self._seen = None                              # after a refusal all is looked at again, though it be where it was
             self._check_list("params", self.params)
             if self.copies is not None:
                 self._check_list("copies", self.copies)

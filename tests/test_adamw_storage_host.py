@@ -110,6 +110,21 @@ def test_states_that_are_not_there(calls):
     assert calls[1][2][0] == opt.state()["exp_avg"][0].data_ptr()
 
 
+def test_a_refusal_is_not_forgotten(calls, monkeypatch):
+    """Storage that was freed can come back smaller at the address it had: the step after a refusal checks it all."""
+    _, grads, opt = optimizer(calls, (600,), (5,))
+    t = opt.state()["exp_avg"][0]
+    storage, was, plain = t.untyped_storage(), t.data_ptr(), torch.Tensor.data_ptr
+    storage.resize_(0)
+    refused(opt, grads, calls)
+    storage.resize_(400)
+    there = plain(t)
+    monkeypatch.setattr(torch.Tensor, "data_ptr", lambda x: was if plain(x) == there else plain(x))
+    monkeypatch.setattr(opt, "_check_places", lambda: pytest.fail("looked at", pytrace=False))
+    with pytest.raises(pytest.fail.Exception, match="looked at"):
+        opt.step(grads)
+
+
 def test_tensors_that_share_memory(calls):
     room = torch.zeros(1000)
     ok = AdamW([room[:300], room[300:301], room[301:301], room[301:]])       # side by side
