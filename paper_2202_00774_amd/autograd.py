@@ -209,6 +209,7 @@ class _PolicyLossFn(torch.autograd.Function):
                                                                    average=average)
         ctx.save_for_backward(weights, logp, old_logp, advantages, ref_logp, mask, offsets)
         ctx.cfg = {"clip": clip, "kl": kl, "average": average}
+        loss, mean_kl, clipped = loss.data, mean_kl.data, clipped.data     # no views to autograd: callers may write to them (loss /= n)
         ctx.mark_non_differentiable(mean_kl, clipped)
         return loss, mean_kl, clipped
 

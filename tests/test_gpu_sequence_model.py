@@ -217,3 +217,20 @@ def test_gradients_that_are_not_asked_for():
     logp = randn(3, T).requires_grad_()
     loss, kl, clipped = ag.sdgp_policy_loss(logp, logp.detach(), randn(4, T), None, None, offsets)
     assert not kl.requires_grad and not clipped.requires_grad and loss.requires_grad
+
+
+def test_losses_that_are_written_to():
+    """loss /= n, and sums of what is reported: outputs are tensors of their own, and gradients scale with them."""
+    offsets, _, _, T = batch()
+    logp, old, adv = randn(3, T).requires_grad_(), randn(3, T), randn(4, len(LENS))
+    for call in (lambda: ag.sdgp_policy_loss(logp, old, adv, old, None, offsets, kl=0.1), lambda: ag.sdgp_preference_loss(logp, old, None, offsets)):
+        loss, *reported = call()
+        whole = torch.autograd.grad(loss, logp)[0]
+        loss, *reported = call()
+        kept = loss.item()
+        for r in reported:
+            r += 1
+        loss /= 4
+        loss += 1
+        assert math.isclose(loss.item(), kept / 4 + 1, rel_tol=1e-6)
+        assert torch.equal(torch.autograd.grad(loss, logp)[0], whole / 4)      # a power of two: exact
