@@ -946,7 +946,7 @@ def _policy_arguments(logp, old_logp, advantages, ref_logp, mask, offsets, clip,
         raise ValueError("kl needs ref_logp")
     _beside(advantages, "advantages", logp)
     each = advantages.shape == logp.shape
-    if advantages.dtype != torch.float32 or not each and advantages.shape != (S,):
+    if advantages.dtype != torch.float32 or not each and advantages.shape not in ((S,), (S, 1)):
         raise ValueError("advantages must be float32, one for each token or one for each sequence")
     low, high = clip
     return (_ptr(old_logp), _ptr(ref_logp), _ptr(advantages), int(each), _ptr(mask), _ptr(offsets), S, T, low, high, kl), S, T
@@ -961,7 +961,8 @@ def sdgp_policy_loss(logp: torch.Tensor, old_logp: torch.Tensor, advantages: tor
     """The clipped policy loss with a KL term: ``(loss, kl, clipped, weights)``.
 
     ``logp``, ``old_logp``, ``ref_logp``: fp32 [T] with ``offsets`` (int32 [sequences + 1]), [sequences, L] or [L] without.
-    ``advantages``: of that shape, or [sequences].  ``mask``: bool or uint8, which tokens count.  The mean is over tokens, or
+    ``advantages``: of that shape, or [sequences] or [sequences, 1], the last also where packed tokens happen to be as many as
+    their sequences.  ``mask``: bool or uint8, which tokens count.  The mean is over tokens, or
     with ``average="sequences"`` over the sequences' means.  ``kl`` and ``clipped`` are the mean divergence and the share of
     ratios that are cut; ``weights`` is for ``sdgp_policy_loss_bwd``."""
     if average not in _AVERAGES:

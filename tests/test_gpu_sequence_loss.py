@@ -115,6 +115,18 @@ def test_policy_on_a_batch_and_one_sequence():
     assert one[-1].shape == (1,) and torch.equal(one[0], sdgp.sdgp_policy_loss(logp, old, adv)[0])
 
 
+def test_as_many_tokens_as_sequences():
+    """[T] is each token's, as always; [sequences, 1] is the sequences', forward and backward."""
+    offsets = offsets_of([3, 0, 1, 0])
+    old, logp, adv = rand(0, 4) * 0.2, rand(1, 4) * 0.2, rand(2, 4)
+    g = torch.ones((), device="cuda")
+    for given, each in ((adv, adv), (adv[:, None], adv[[0, 0, 0, 2]])):
+        loss, _, _, weights = sdgp.sdgp_policy_loss(logp, old, given, None, None, offsets)
+        want = sdgp.sdgp_policy_loss(logp, old, each)
+        assert torch.equal(sdgp.sdgp_policy_loss_bwd(g, weights, logp, old, given, None, None, offsets), sdgp.sdgp_policy_loss_bwd(g, want[-1], logp, old, each))
+        near(loss, want[0].double(), 8 * F * (each.abs() * torch.exp(logp - old)).mean())
+
+
 def test_small_divergences_do_not_cancel():
     """x of 1e-4: e^x - 1 - x = x^2 / 2 of 5e-9, from log probabilities that hold it exactly."""
     x = torch.linspace(-6e-4, 6e-4, 1000, device="cuda")

@@ -207,7 +207,7 @@ def test_tensors_of_one_gpu(name, calls):
     ("attention_bwd", dict(lse=on(0, 6, 5))), ("attention_bwd", dict(o=on(0, 4, 6, 8).transpose(0, 1))), ("rotary", dict(freqs=on(0, 5))), ("rotary", dict(freqs=on(0, 0))),
     ("rotary", dict(axes=(2, 1))), ("rotary", dict(axes=(2, 2))), ("rotary", dict(axes=(4, 0))), ("rotary", dict(positions=on(0, 5, dtype=I32))), ("rotary", dict(positions=on(0, 6))),
     ("rotary", dict(k=on(0, 5, 2, 8))), ("rotary", dict(k=on(0, 6, 2, 10))), ("rotary", dict(out=(on(0, 6, 4, 8), None))), ("policy", dict(clip=(0.2, 0.2), ref_logp=None)),
-    ("policy", dict(average="token")), ("policy", dict(advantages=on(0, 3))), ("policy", dict(mask=on(0, 6))), ("policy", dict(logp=on(0, 6).double())), ("policy", dict(logp=on(0, 2, 3))),
+    ("policy", dict(average="token")), ("policy", dict(advantages=on(0, 3))), ("policy", dict(advantages=on(0, 3, 1))), ("policy", dict(mask=on(0, 6))), ("policy", dict(logp=on(0, 6).double())), ("policy", dict(logp=on(0, 2, 3))),
     ("policy_bwd", dict(g=on(0, 2))), ("policy_bwd", dict(weights=on(0, 3))), ("preference", dict(offsets=on(0, 4, dtype=I32))), ("preference", dict(ref_logp=on(0, 5))),
     ("preference_bwd", dict(g=on(0).double()))])
 def test_what_the_binding_refuses(name, wrong, calls):
