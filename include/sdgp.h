@@ -501,7 +501,8 @@ int sdgp_rotary(const void* q, const void* k, void* q_out, void* k_out, const in
  * sdgp_policy_loss -- the clipped policy loss with a KL term.
  *   r = exp(logp - old_logp);  l = -min(r A, clip(r, 1 - low, 1 + high) A) + kl (e^x - 1 - x),  x = ref_logp - logp
  *   advantages A [T] with `each`, else [sequences];  0 <= low <= 1, high >= 0 (infinity: no bound), kl >= 0; ref_logp may be NULL
- *              with kl = 0.  Whether a ratio is cut is decided on logp - old_logp in 64 bits.
+ *              with kl = 0, where the divergence is reported but no term, infinite or not.  Whether a ratio is cut is decided on
+ *              logp - old_logp in 64 bits.
  *   by_sequence  0: the loss is the mean of l over the tokens that count; else the mean of the sequences' means, over the
  *              sequences that have such tokens.  Without any the loss is 0.
  *   out        [3] fp32: the loss, the mean of e^x - 1 - x and the share of tokens whose ratio is cut

@@ -176,12 +176,13 @@ int sdgp_policy_loss(const float* logp, const float* old_logp, const float* ref_
 int sdgp_policy_loss_bwd(const float* g, const float* weights, const float* logp, const float* old_logp, const float* ref_logp,
                          const float* advantages, int each, const uint8_t* mask, const int32_t* offsets, int64_t sequences, int64_t T,
                          double low, double high, float kl, float* dlogp, void* hip_stream) {
-    const sdgp::Sequences s = sequences_of(logp, ref_logp, mask, offsets, T, sequences);
+    sdgp::Sequences s = sequences_of(logp, ref_logp, mask, offsets, T, sequences);
     const int rc = check_policy(s, sequences, old_logp, advantages, each, low, high, kl);
     if (rc != SDGP_OK) return rc;
     if (T == 0) return SDGP_OK;
     if (!g || (sequences > 0 && !weights) || !dlogp) return SDGP_ERR_NULL;
     if (!aligned(g, 4) || !aligned(weights, 4) || !aligned(dlogp, 4)) return SDGP_ERR_SHAPE;
+    s.ref = kl > 0.0f ? s.ref : nullptr;                                // nothing of it is in the gradient
     return sdgp::policy_loss_bwd_launch(policy_of(s, old_logp, advantages, each, 0, low, high, kl), g, weights, dlogp,
                                         static_cast<hipStream_t>(hip_stream));
 }

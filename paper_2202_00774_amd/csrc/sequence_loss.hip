@@ -120,7 +120,7 @@ __device__ __forceinline__ PolicyTerms policy_terms(const PolicyLoss& p, const T
     const float ra = A == 0.0f ? 0.0f : t.ratio * A;                   // (an infinite ratio times no advantage)
     PolicyTerms r;
     r.cut = cut ? 1.0f : 0.0f;
-    r.loss = (cut ? -A * (A > 0.0f ? p.high : p.low) : -ra) + p.kl * t.kl;
+    r.loss = (cut ? -A * (A > 0.0f ? p.high : p.low) : -ra) + (p.kl == 0.0f ? 0.0f : p.kl * t.kl);   // (it may be infinite)
     r.slope = (cut ? 0.0f : -ra) - p.kl * t.rise;
     return r;
 }

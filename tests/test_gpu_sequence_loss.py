@@ -147,6 +147,9 @@ def test_policy_borders_and_extremes():
     assert loss.item() == -0.25 and clipped.item() == 0.25 and d.tolist() == [-0.25, 0.25, 0.0, 0.0]
     loss, _, clipped, weights = sdgp.sdgp_policy_loss(logp[:2], z[:2], adv[:2], clip=(1.0, math.inf))
     assert loss.item() == 0.0 and clipped.item() == 0.0
+    far = [torch.tensor([x], device="cuda") for x in (-100.0, -100.0, 1.0, 0.0)]                    # e^100 passes 32 bits
+    loss, kl, _, weights = sdgp.sdgp_policy_loss(*far, kl=0.0)
+    assert loss.item() == -1.0 and kl.item() == math.inf and sdgp.sdgp_policy_loss_bwd(one, weights, *far, kl=0.0).item() == -1.0
 
 
 def preference_reference(logp, ref, mask, offsets, beta, margin, smoothing, average, g):
