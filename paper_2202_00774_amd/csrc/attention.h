@@ -88,10 +88,15 @@ __device__ __forceinline__ int tiles_of_work(const Attention& a, const Sequence&
     return token <= 0 ? tiles : token >= s.nq ? 0 : tiles - token * a.G / UNIT;
 }
 
-// Tile `index` of all sequences' tiles of UNIT rows: false behind the last.  `tile` counts a sequence's tiles from the one with the
-// most work.  With offsets, a wavefront adds up the sequences' tiles 64 at a time (every wavefront for itself; the results are
-// uniform), first those with three quarters of the most work there is, then those with half of it, and so on (a.buckets): the
-// long ones start first, and workgroups that run together share their sequences' rows as far as they can.
+// Workgroup `index`'s tile of UNIT rows: false if it has none.  `tile` counts a sequence's tiles from the one with the most work.
+//
+// With offsets, each sequence has the tiles from (rows in front of it) / UNIT + its number on, which leaves it room for the one that
+// is not full: a wavefront looks at 64 places at once (every wavefront for itself; the results are uniform; adding up the sequences'
+// tiles instead took 250 us a call, waited for, on 4096 sequences of one token, 2500 on 16384, and this 85 and 200).  With a.buckets, of up to
+// kInOrder sequences, a lane has one of them, and those tiles come first that have three quarters of the most work there is, then those
+// with half of it, and so on: the long ones start first, and workgroups that run together share their sequences' rows as far as they can.
+constexpr int kInOrder = 62;                                     // and the rows in front of the first and behind the last
+
 template <bool KEYS, int UNIT>
 __device__ __forceinline__ bool find_tile(const Attention& a, int index, Sequence& s, int& tile, int& tiles) {
     if (a.off_q == nullptr) {
@@ -109,47 +114,57 @@ __device__ __forceinline__ bool find_tile(const Attention& a, int index, Sequenc
         if (i <= a.S) x = i >= 0 && i < a.S ? sequence_at(a, i) : rows_outside<KEYS>(a, i >= 0);
         return x;
     };
-    Sequence mine = sequence(lane - 1);
-    int most = 0;
-    if (a.buckets > 1) {
-        for (int first = -1; first <= a.S; first += 64) {
-            const Sequence x = first == -1 ? mine : sequence(first + lane);
-            most = most < (KEYS ? x.nq : x.nk) ? (KEYS ? x.nq : x.nk) : most;
+    if (a.buckets == 1) {
+        const int T = KEYS ? a.Tk : a.Tq;
+        const int32_t* off = KEYS ? a.off_k : a.off_q;
+        const auto place = [&](int i) { return (i == 0 ? 0 : clamp_int(off[i - 1], 0, T)) * (KEYS ? 1 : a.G) / UNIT + i; };
+        int low = 0, high = a.S + 2;                             // the last of these whose place is not behind index
+        while (high - low > 1) {
+            const int step = (high - low + 63) / 64, at = low + lane * step;
+            const uint64_t there = __ballot(at < high && place(at < high ? at : low) <= index);
+            low += there == 0 ? 0 : (63 - __builtin_clzll(there)) * step;
+            high = low + step < high ? low + step : high;
         }
+        s = sequence(low - 1);                                   // (one for all lanes, which the compiler does not see)
+        s.q0 = __builtin_amdgcn_readfirstlane(s.q0), s.nq = __builtin_amdgcn_readfirstlane(s.nq);
+        s.k0 = __builtin_amdgcn_readfirstlane(s.k0), s.nk = __builtin_amdgcn_readfirstlane(s.nk);
+        low = __builtin_amdgcn_readfirstlane(low);
+        tiles = ((KEYS ? s.nk : s.nq * a.G) + UNIT - 1) / UNIT;
+        tile = index - place(low);
+        return tile >= 0 && tile < tiles;
+    }
+    const Sequence mine = sequence(lane - 1);
+    int most = KEYS ? mine.nq : mine.nk;
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int x = __shfl_xor(most, o);
-            most = most < x ? x : most;
-        }
+    for (int o = 1; o < 64; o <<= 1) {
+        const int x = __shfl_xor(most, o);
+        most = most < x ? x : most;
     }
     int before = 0;
     for (int b = a.buckets - 1; b >= 0; --b) {
         const int low = (int)((int64_t)most * b / a.buckets), high = b == a.buckets - 1 ? 0x7FFFFFFF : (int)((int64_t)most * (b + 1) / a.buckets);
-        for (int first = -1; first <= a.S; first += 64) {
-            if (a.S > 62) mine = sequence(first + lane);
-            const int above = tiles_of_work<KEYS, UNIT>(a, mine, high), n = tiles_of_work<KEYS, UNIT>(a, mine, b == 0 ? 0 : low) - above;
-            int upto = n;
+        const int above = tiles_of_work<KEYS, UNIT>(a, mine, high), n = tiles_of_work<KEYS, UNIT>(a, mine, b == 0 ? 0 : low) - above;
+        int upto = n;
 #pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const int x = __shfl_up(upto, o);
-                if (lane >= o) upto += x;
-            }
-            const uint64_t past = __ballot(before + upto > index);
-            if (past != 0) {
-                const int at = __builtin_ctzll(past);
-                s.q0 = __builtin_amdgcn_readlane(mine.q0, at), s.nq = __builtin_amdgcn_readlane(mine.nq, at);
-                s.k0 = __builtin_amdgcn_readlane(mine.k0, at), s.nk = __builtin_amdgcn_readlane(mine.nk, at);
-                tiles = ((KEYS ? s.nk : s.nq * a.G) + UNIT - 1) / UNIT;
-                tile = index - before - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(n, at)) + __builtin_amdgcn_readlane(above, at);
-                return true;
-            }
-            before += __builtin_amdgcn_readlane(upto, 63);
+        for (int o = 1; o < 64; o <<= 1) {
+            const int x = __shfl_up(upto, o);
+            if (lane >= o) upto += x;
         }
+        const uint64_t past = __ballot(before + upto > index);
+        if (past != 0) {
+            const int at = __builtin_ctzll(past);
+            s.q0 = __builtin_amdgcn_readlane(mine.q0, at), s.nq = __builtin_amdgcn_readlane(mine.nq, at);
+            s.k0 = __builtin_amdgcn_readlane(mine.k0, at), s.nk = __builtin_amdgcn_readlane(mine.nk, at);
+            tiles = ((KEYS ? s.nk : s.nq * a.G) + UNIT - 1) / UNIT;
+            tile = index - before - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(n, at)) + __builtin_amdgcn_readlane(above, at);
+            return true;
+        }
+        before += __builtin_amdgcn_readlane(upto, 63);
     }
     return false;
 }
 
-// Upper bound of what find_tile finds.
+// Workgroups that have all of find_tile's tiles.
 inline int64_t most_tiles(bool packed, int64_t S, int64_t T, int64_t L, int64_t each, int64_t unit) {
     return packed ? T * each / unit + S + 2 : S * ((L * each + unit - 1) / unit);
 }

@@ -85,7 +85,7 @@ Attention arguments(const AttentionCall& c) {
 // Workgroups by the work they have, where there are more of them than run at once and sequences long enough to differ (finding
 // their place takes them up to 8 us).
 static int in_order_of_work(const AttentionCall& c, int64_t workgroups) {
-    return c.offsets_q != nullptr && c.S > 1 && workgroups > 512 && c.Tq >= 512 * c.S ? 4 : 1;
+    return c.offsets_q != nullptr && c.S > 1 && c.S <= kInOrder && workgroups > 512 && c.Tq >= 512 * c.S ? 4 : 1;
 }
 
 size_t attention_workspace(int64_t S, int64_t Tq, int64_t Tk, int64_t H, int64_t Hk, int D) {

@@ -93,6 +93,27 @@ def test_many_sequences():
     packed(lens, lens, BF16, 2, 1, 64, True)
 
 
+@pytest.mark.parametrize("first, behind", [(0, 0), (7, 300)])
+def test_thousands_of_sequences(first, behind):
+    """As batches of the sequences of each length: one block of keys and rows each, so the same sums, to the bit."""
+    lens = [(7 * i) % 5 for i in range(9000)]
+    T, (H, Hk, D) = first + sum(lens) + behind, (4, 2, 64)
+    q, k, v, do = (randn(i, T, h, D, dtype=BF16) for i, h in enumerate((H, Hk, Hk, H)))
+    offsets = offsets_of(lens, first)
+    o, lse = sdgp.sdgp_attention(q, k, v, offsets)
+    out = (o, lse, *sdgp.sdgp_attention_bwd(do, q, k, v, o, lse, offsets))
+    starts, n_of = offsets[:-1].long(), torch.tensor(lens, device="cuda")
+    for n in range(1, 5):
+        at = starts[n_of == n][:, None] + torch.arange(n, device="cuda")
+        batch = [t[at] for t in (q, k, v, do)]
+        bo, blse = sdgp.sdgp_attention(*batch[:3])
+        for got, want in zip(out, (bo, blse, *sdgp.sdgp_attention_bwd(batch[3], *batch[:3], bo, blse))):
+            assert torch.equal(got[at], want)
+    for t in (o, *out[2:]):
+        assert not t[:first].any() and not t[T - behind:].any()
+    assert bool((lse[:first] == -math.inf).all()) and bool((lse[T - behind:] == -math.inf).all())
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("heads", [(4, 4, 64), (8, 1, 128), (5, 1, 80), (40, 1, 32)])
 @pytest.mark.parametrize("tokens", [1, 3])
