@@ -190,6 +190,37 @@ def test_captured_and_replayed():
             assert torch.equal(a, b) or torch.equal(a.isnan(), b.isnan()) and torch.equal(a[~a.isnan()], b[~b.isnan()])
 
 
+def test_gradients_captured_and_replayed():
+    """The model's forward pass, losses and their gradients in one graph; no eager graph of its weights lives meanwhile."""
+    offsets, tokens, positions, T = batch()
+    w = weights(torch.bfloat16)
+    freqs = 50.0 ** (-torch.arange(D // 2, device="cuda") / (D // 2))
+    old, ref, adv = (torch.zeros(n, device="cuda") for n in (T, T, len(LENS)))
+
+    def step():
+        logp = own_logp(w, tokens, positions, offsets, freqs)
+        loss = ag.sdgp_policy_loss(logp, old, adv, ref, None, offsets, kl=0.1)[0] + ag.sdgp_preference_loss(logp, ref, None, offsets)[0]
+        return [loss.detach(), *torch.autograd.grad(loss, list(w.values()))]
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = step()
+    for seed in (1, 2, 3):
+        for i, t in enumerate((old, ref, adv)):
+            t.copy_(randn(10 * seed + i, *t.shape))
+        graph.replay()
+        eager = step()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], eager[0])
+        for a, b in list(zip(outs, eager))[2:]:                            # (the embedding's are another kernel's, with atomics)
+            assert torch.equal(a, b)
+
+
 def test_another_stream():
     offsets, _, positions, T = batch()
     q, k, v = (randn(i, T, h, D) for i, h in enumerate((H, HK, HK)))
