@@ -338,7 +338,8 @@ __device__ __forceinline__ uint32_t here(uint32_t x) {
 }
 
 // Buffer loads straight into LDS, lane i's bytes at `lds` + SIZE i; offsets from kNoRecord on give zeros.  The compiler does not count
-// them: nothing that it waits for may be on its way beside them, or its wait is for them too.
+// them: nothing that it waits for may be on its way beside them, or its wait is for them too.  Nor does it keep the five wait states between
+// a vector instruction that writes a scalar register (`records` makes some) and a memory instruction that reads it: s_mov_b32 and s_nop 3 do.
 constexpr uint32_t kNoRecord = 0x7FFFFFF0u;
 
 __device__ __forceinline__ attn_u32x4 records(const void* base, uint32_t bytes) {
@@ -353,8 +354,8 @@ __device__ __forceinline__ attn_u32x4 records(const void* base, uint32_t bytes) 
 template <int SIZE>
 __device__ __forceinline__ void copy_to_lds(attn_u32x4 from, uint32_t offset, uint32_t lds) {
     static_assert(SIZE == 16 || SIZE == 4, "bytes a lane");
-    if constexpr (SIZE == 16) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(from) : "memory");
-    else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(from) : "memory");
+    if constexpr (SIZE == 16) asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(from) : "memory");
+    else asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(from) : "memory");
 }
 __device__ __forceinline__ void wait_for_copies() { __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8)); }   // vmcnt 0
 
