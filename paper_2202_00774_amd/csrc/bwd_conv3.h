@@ -94,9 +94,10 @@ __device__ __forceinline__ void copy16_to_lds(const void* gptr, uint32_t lds_bas
 }
 
 // Same, with the address split into a wave-uniform base and a 32-bit byte offset per lane (no address arithmetic on
-// the vector unit when only the base moves).
+// the vector unit when only the base moves).  s_nop 3: a scalar register that a vector instruction has written may be read by a memory
+// instruction five wait states later, which the compiler does not keep in front of inline assembly.
 __device__ __forceinline__ void copy16_to_lds(const void* sbase, uint32_t voff, uint32_t lds_base) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_base), "v"(voff), "s"(sbase)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_base), "v"(voff), "s"(sbase)
                  : "memory");
 }
 

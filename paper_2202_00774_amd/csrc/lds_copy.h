@@ -18,7 +18,9 @@ __device__ __forceinline__ void lds_copy4(const void* gptr, uint32_t lds_base) {
     const uint32_t base = __builtin_amdgcn_readfirstlane(lds_base);
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(base), "v"(gptr) : "memory");
 }
-// Same, address = wave-uniform base + 32-bit byte offset per lane.
+// Same, address = wave-uniform base + 32-bit byte offset per lane.  The compiler, which does not look into inline assembly, does not keep
+// the five wait states between a vector instruction that writes a scalar register (the base's words) and a memory instruction that
+// reads it: s_mov_b32 and s_nop 3 do.
 __device__ __forceinline__ void lds_copy16(const void* sbase, uint32_t voff, uint32_t lds_base) {
     const uint32_t base = __builtin_amdgcn_readfirstlane(lds_base);
     const uint64_t a = (uint64_t)(uintptr_t)sbase;
@@ -26,7 +28,7 @@ __device__ __forceinline__ void lds_copy16(const void* sbase, uint32_t voff, uin
     const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)a);
     const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32));
     const uint64_t ua = ((uint64_t)hi << 32) | (uint64_t)lo;
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(base), "v"(voff), "s"(ua) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(base), "v"(voff), "s"(ua) : "memory");
 }
 // Waits until at most N of this wavefront's vector-memory operations are outstanding.
 template <int N>

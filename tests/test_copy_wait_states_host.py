@@ -53,3 +53,8 @@ def late(copies, kind):
 def test_copies_of_tiles_by_buffer_records(copies):
     reads, short = late(copies, "buffer_")
     assert len(reads) > 300 and short == []
+
+
+def test_copies_from_a_scalar_address(copies):
+    reads, short = late(copies, "global_")
+    assert len(reads) > 300 and short == []
