@@ -352,14 +352,17 @@ int loss_launch(const Loss& p, void* workspace, hipStream_t stream, Out... out) 
         hipLaunchKernelGGL((loss_at_once<Loss, Out...>), dim3(1), dim3(kFinish), 0, stream, p, chunks, slots, sums, out...);
         return launch_status();
     }
-    if (chunks > 0) {
+    int rc = SDGP_OK;
+    if (p.s.S > 0 && chunks > 0) {
         hipLaunchKernelGGL((loss_chunks<Loss>), dim3((unsigned)((chunks + kWaves - 1) / kWaves)), dim3(kBlock), 0, stream, p, chunks, slots);
-        const int rc = launch_status();
+        rc = launch_status();
         if (rc != SDGP_OK) return rc;
     }
-    hipLaunchKernelGGL((loss_sequences<Loss>), dim3((unsigned)((p.s.S + kWaves - 1) / kWaves)), dim3(kBlock), 0, stream, p, slots, sums);
-    const int rc = launch_status();
-    if (rc != SDGP_OK) return rc;
+    if (p.s.S > 0) {                                                    // (a launch has workgroups)
+        hipLaunchKernelGGL((loss_sequences<Loss>), dim3((unsigned)((p.s.S + kWaves - 1) / kWaves)), dim3(kBlock), 0, stream, p, slots, sums);
+        rc = launch_status();
+        if (rc != SDGP_OK) return rc;
+    }
     hipLaunchKernelGGL((loss_finish<Loss, Out...>), dim3(1), dim3(kFinish), 0, stream, p, sums, out...);
     return launch_status();
 }
