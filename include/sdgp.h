@@ -516,7 +516,8 @@ int sdgp_rotary(const void* q, const void* k, void* q_out, void* k_out, const in
  *   Without pairs the loss is 0; a sequence without tokens that count scores 0.
  * sdgp_preference_loss_bwd -- dlogp [T] = g * weights.  (margins have none.)
  *
- * Sums are taken in 64 bits and in a fixed order: the same bits from call to call.
+ * Each token's terms are fp32 (infinite beyond its range); their sums, from the first two on, are taken in 64 bits and in a fixed
+ * order: the same bits from call to call.
  * workspace: sdgp_sequence_loss_workspace(...) bytes, 16-byte aligned, contents undefined afterwards.
  */
 size_t sdgp_sequence_loss_workspace(int64_t T, int64_t sequences);

@@ -186,20 +186,18 @@ __device__ __forceinline__ void chunk_sums(const Loss& p, int64_t chunk, double*
         float A = 0.0f;
         if constexpr (std::is_same<Loss, PolicyLoss>::value) A = p.each ? 0.0f : p.advantages[i];
         int count = 0;
-        float four[3] = {0.0f, 0.0f, 0.0f};                             // (four terms of 32 bits add up in 32)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             if (!(f.on[k] && at + k >= span.begin && at + k < span.end)) continue;
             ++count;
             if constexpr (std::is_same<Loss, PolicyLoss>::value) {
                 const PolicyTerms r = policy_terms(p, t[k], p.each ? f.adv[k] : A);
-                four[0] += r.loss, four[1] += t[k].kl, four[2] += r.cut;
+                sums[1] += (double)r.loss, sums[2] += (double)t[k].kl, sums[3] += (double)r.cut;
             } else {
                 sums[1] += s.ref != nullptr ? (double)f.logp[k] - (double)f.ref[k] : (double)f.logp[k];
             }
         }
         sums[0] = (double)count;
-        if constexpr (std::is_same<Loss, PolicyLoss>::value) sums[1] = (double)four[0], sums[2] = (double)four[1], sums[3] = (double)four[2];
         constexpr int used = std::is_same<Loss, PolicyLoss>::value ? 4 : 2;
 #pragma unroll
         for (int k = 0; k < used; ++k) sums[k] = sum_over_wave(sums[k]);
