@@ -456,8 +456,10 @@ int sdgp_adamw_step(int count, void* const* params, const void* const* grads, vo
  *   order: the same bits from call to call.  Tokens without a sequence, and keys that no query sees, have gradient 0.
  *
  * workspace: sdgp_attention_workspace(...) / sdgp_attention_bwd_workspace(...) bytes, 16-byte aligned, contents undefined
- * afterwards ((size_t)-1 for invalid arguments; 0 where the call needs none).  Tq * H and Tk * H at most 2^30, H at most 65536;
- * scores beyond 2^30 in magnitude give NaN.
+ * afterwards ((size_t)-1 for invalid arguments; 0 where the call needs none).  Tq * H and Tk * H at most 2^30, H at most 65536, and
+ * SDGP_ERR_SHAPE where a launch would have 2^24 workgroups or more: at most Hk (max(Tq H / Hk, Tk) / 32 + sequences + 2) of them.
+ * Scores beyond 2^30 in magnitude may give NaN, and values of v beyond 2^119 / (keys that a query sees) infinity: the sums are taken of
+ * exp(s - m) v with an m that may stay 8 ln 2 behind the largest s, and divided at the end.
  */
 size_t sdgp_attention_workspace(int64_t sequences, int64_t Tq, int64_t Tk, int64_t H, int64_t Hk, int D, int dt);
 int sdgp_attention(const void* q, const void* k, const void* v, const int64_t* strides, const int32_t* offsets_q,
