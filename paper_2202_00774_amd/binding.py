@@ -795,7 +795,8 @@ def sdgp_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets: t
 
     With ``offsets`` (int32 [sequences + 1]) q is [T, H, D], k and v [T, Hk, D], sequences one behind the other; ``offsets_k``
     where the keys' differ.  Without, q is [B, L, H, D], k and v [B, Lk, Hk, D], and ``lengths`` (int32 [B]) says how many
-    of the Lk keys there are (a cache).  Tokens and heads may be strided.  ``causal``: the last query sees all keys, the one
+    of the Lk keys there are (a cache).  Tokens and heads may be strided, a batch's tokens evenly: a cache is given whole, with
+    ``lengths``.  Plans go by mean lengths: a long prompt and a few single tokens are faster as two calls.  ``causal``: the last query sees all keys, the one
     before all but the last, and so on.  ``scale``: D ** -0.5 by default."""
     strides, offsets, offsets_k, S, Tq, Tk, H, Hk, D, dt, scale = _attention_sizes(q, k, v, offsets, offsets_k, scale)
     if lengths is not None:

@@ -50,7 +50,7 @@ BwdSplit choose_bwd(int64_t S, int64_t Tq, int64_t Tk, int64_t H, int64_t Hk, in
     // Parts cost their sums, written and read, and their own first copies.  8192 tokens, 256 workgroups: 618 us and 23 for the sums in
     // four parts, 590 and 36 in six; 4096 tokens, 64 workgroups: 99 and 12 in eight, 95 and 22 in sixteen; twice 2000 tokens, 128
     // workgroups of D = 64: 23 and 7 in four, 31 and 12 in eight; 1024 tokens, 64 workgroups: 24 and 7 in four (the limit by rounds), 29
-    // and 6 in two.  22294 packed tokens, 736 workgroups: a pass takes 1436 us with one part and with two, at the power the card has.
+    // and 6 in two.  22294 packed tokens, 736 workgroups: a pass takes 1465 us with one part and 1463 with two, at the power the card has.
     int64_t parts = have > 0 ? (dt == SDGP_BF16 && have >= 256 ? 1024 : 512) / have : 1;
     parts = parts > rounds / 4 ? rounds / 4 : parts;
     s.parts = (int)(parts < 1 ? 1 : parts > 16 ? 16 : parts);

@@ -92,7 +92,7 @@ __device__ __forceinline__ TokenTerms token_terms(const PolicyLoss& p, float log
     t.ratio = expf((float)t.d);
     t.kl = t.rise = 0.0f;
     if (p.s.ref != nullptr) {
-        // e^x - 1 - x: its series where the differences would cancel (its eleventh power adds less than 2^-24 of it)
+        // e^x - 1 - x: its series where the differences would cancel (what is left out, from x^11 on, is at most 1.05 x 2^-24 of it, at x = -1)
         const float x = (float)((double)ref - (double)logp);
         float series = 1.0f / 3628800.0f;
         series = __builtin_fmaf(series, x, 1.0f / 362880.0f);
